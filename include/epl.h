@@ -320,6 +320,118 @@ epl_status epl_layout_dispatch_noalloc(const epl_config *cfg, const int32_t *top
 epl_status epl_combine(const epl_config *cfg, const void *y, const float *topk_w, const epl_layout_buffers *L,
                        void *out, void *stream);
 
+/* ---- Router -------------------------------------------------------------------------------------
+ * From a token's logits to the choices and gate weights that epl_layout and epl_combine take:
+ *   score   s_e = softmax(l)_e or sigmoid(l_e);
+ *   choice  the topk experts by l_e, or, with a selection bias, by s_e + bias_e; in descending order, equal
+ *           values by the lowest expert index;
+ *   weight  w_j = scale * s_{e_j}, divided first by the sum of the chosen scores if normalize is set (all zero
+ *           where the chosen sigmoids are 0 in 64 bits, below about -709).
+ * An expert whose logit (or whose s_e + bias_e) is -inf or NaN is masked: it is never chosen and its score is 0. A
+ * token with fewer than topk experts left gets expert id -1 and weight 0 in the remaining places, which the layout
+ * skips: a padded token is a row of -inf. Of several logits of +inf each counts as the maximum.
+ * The order of s_e + bias_e is that of 64-bit arithmetic; scores, sums and weights are fp32.          */
+typedef enum { EPL_SCORE_SOFTMAX = 0, EPL_SCORE_SIGMOID = 1 } epl_score;
+typedef enum { EPL_LOGITS_F32 = 0, EPL_LOGITS_BF16 = 1 } epl_logits;
+typedef struct {
+  int32_t logits;    /* epl_logits: type of logits and dlogits */
+  int32_t score;     /* epl_score                              */
+  int32_t normalize; /* 0 or 1                                 */
+  float scale;       /* finite                                 */
+} epl_route_opts;
+
+/*   logits  [T*E] row-major, read-only; aligned to its type.
+ *   bias    [E] fp32 or NULL.
+ *   topk_idx [T*k] int32, topk_w [T*k] fp32: outputs, fully written.
+ * Uses num_experts, topk and the token count of cfg. One launch.                                      */
+epl_status epl_route(const epl_config *cfg, const epl_route_opts *opts, const void *logits, const float *bias,
+                     int32_t *topk_idx, float *topk_w, void *stream);
+
+/* Gradient of the logits, given the choices (which it takes as constants; the bias has no gradient).
+ *   topk_idx [T*k]  the choices; ids outside [0, E) count for nothing, an id that occurs twice counts twice.
+ *   dtopk_w  [T*k]  fp32 gradient of topk_w.
+ *   dlogits  [T*E]  output in the type of logits, fully written; must not alias logits.               */
+epl_status epl_route_backward(const epl_config *cfg, const epl_route_opts *opts, const void *logits,
+                              const int32_t *topk_idx, const float *dtopk_w, void *dlogits, void *stream);
+
+/* ---- The experts' products on the packed rows -----------------------------------------------------
+ * Rows [expert_off[e], expert_off[e+1]) of the packed buffers are expert e's. Every packed buffer below has
+ * `rows` rows, rows >= T*k (EPL_ERR_CAPACITY otherwise); rows >= P are neither used nor written. expert_off is
+ * the only field of L that is read, on the device; whatever it holds, no access leaves the buffers. Products
+ * are summed in fp32 and rounded once to bf16 (RNE), with no atomics: identical inputs give identical outputs.
+ * Weights are [E] row-major matrices [out][in] (as a linear layer keeps them), expert_stride elements apart.
+ * Matrices, rows and biases are bf16 unless stated, 16-byte aligned; feature counts and pitches are multiples of
+ * 8 (expert_stride and pitches of 16 for E4M3), feature counts at most EPL_MAX_HIDDEN.                 */
+typedef enum { EPL_ACT_NONE = 0, EPL_ACT_SILU = 1, EPL_ACT_GELU = 2, EPL_ACT_RELU = 3 } epl_activation; /* GELU: erf */
+
+typedef struct {
+  int32_t inner;         /* I: features between the up and the down projection  */
+  int32_t activation;    /* epl_activation of the gate                          */
+  int64_t expert_stride; /* elements between experts' matrices; 0 means I*H     */
+} epl_gated;
+
+/* Gated up projection: h[r] = act(g[r]) * u[r], g = recv w_gate[e]^T, u = recv w_up[e]^T.
+ *   recv    rows of H elements, cfg's pitch apart, in cfg's payload format, as dispatch wrote them.
+ *   recv_scale, gate_scale, up_scale  fp8 payload only (else ignored): recv's scales [rows*H/128], and one fp32
+ *           scale for each output feature of the E4M3 matrices w_gate and w_up [E*I].
+ *   h       [rows][I] bf16, packed without gaps.
+ *   pre     NULL, or [rows][2*I] bf16: g in columns [0, I) and u in [I, 2I), kept for the backward pass.
+ * EPL_ERR_UNSUPPORTED for fp8 with H % 128 != 0.                                                      */
+epl_status epl_experts_gated(const epl_config *cfg, const epl_gated *gated, const void *recv, const float *recv_scale,
+                             int64_t rows, const epl_layout_buffers *L, const void *w_gate, const void *w_up,
+                             const float *gate_scale, const float *up_scale, void *h, void *pre, void *stream);
+
+/* Its gradients (bf16 payloads; EPL_ERR_UNSUPPORTED for fp8):
+ *   dpre    [rows][2*I] bf16: dh * u * act'(g) and dh * act(g), rounded to bf16 as the operands of the products
+ *           that follow. May be pre itself.
+ *   drecv   rows of H, cfg's pitch apart: dpre_g w_gate[e] + dpre_u w_up[e].
+ *   dw_gate, dw_up  [E][I][H] bf16 without gaps: the experts' dpre^T recv; zero for an expert without rows.
+ * drecv must not alias recv.                                                                          */
+epl_status epl_experts_gated_backward(const epl_config *cfg, const epl_gated *gated, const void *dh, const void *pre,
+                                      const void *recv, int64_t rows, const epl_layout_buffers *L, const void *w_gate,
+                                      const void *w_up, void *dpre, void *drecv, void *dw_gate, void *dw_up,
+                                      void *stream);
+
+typedef struct {
+  int32_t in_features;    /* K                                                                     */
+  int32_t out_features;   /* N                                                                     */
+  int32_t in_pitch;       /* elements from one row of a (and da) to the next; 0 means K; else >= K */
+  int32_t out_pitch;      /* the same for out; 0 means N; else >= N                                */
+  int32_t residual_pitch; /* the same for residual                                                 */
+  int32_t activation;     /* epl_activation                                                        */
+  int32_t payload;        /* epl_payload of a and w (cfg's own payload is not used)                */
+  int64_t expert_stride;  /* elements between experts' matrices; 0 means N*K                       */
+} epl_linear;
+
+/* out[r] = act(a[r] w[e]^T + bias[e]) + residual[r].
+ *   a_scale, w_scale  E4M3 only (else ignored): [rows*K/128] and [E*N] fp32.
+ *   bias     [E*N] or NULL.   residual  rows of N, or NULL; may be out.
+ *   pre      NULL, or [rows][N]: the activation's argument, kept for the backward pass.
+ * EPL_ERR_UNSUPPORTED for E4M3 with K % 128 != 0.                                                     */
+epl_status epl_experts_linear(const epl_config *cfg, const epl_linear *lin, const void *a, const float *a_scale,
+                              int64_t rows, const epl_layout_buffers *L, const void *w, const float *w_scale,
+                              const void *bias, const void *residual, void *out, void *pre, void *stream);
+
+/* Its gradients (bf16; EPL_ERR_UNSUPPORTED for E4M3). The residual's gradient is dy itself.
+ *   dy       [rows][N] without gaps (out_pitch is not used).
+ *   pre      what the forward call kept; ignored (may be NULL) for EPL_ACT_NONE.
+ *   dpre     [rows][N]: dy * act'(pre), rounded to bf16. May be pre or dy. Ignored (may be NULL) for EPL_ACT_NONE.
+ *   da       rows of K, in_pitch apart: dpre w[e].   dw  [E][N][K] without gaps: dpre^T a.
+ *   dbias    NULL, or [E*N] bf16: the sum of the unrounded dpre over the expert's rows.
+ * da must not alias a.                                                                                */
+epl_status epl_experts_linear_backward(const epl_config *cfg, const epl_linear *lin, const void *dy, const void *pre,
+                                       const void *a, int64_t rows, const epl_layout_buffers *L, const void *w,
+                                       void *dpre, void *da, void *dw, void *dbias, void *stream);
+
+/* Gradient of epl_combine:
+ *   dout     [T*H] bf16;   y, topk_w  as epl_combine read them.
+ *   dy       rows of cfg's pitch: dy[pair_row[p]] = topk_w[p] * dout[g] (bf16, RNE); rows >= P untouched. `rows`
+ *            rows, rows >= T*k. May be y itself.
+ *   dtopk_w  [T*k] fp32: the fp32 product sum of dout[g] and y[pair_row[p]]; 0 for an invalid pair.
+ * bf16 rows, whatever cfg's payload. (Dispatch's gradient is epl_combine of drecv with weights of one.) */
+epl_status epl_combine_backward(const epl_config *cfg, const void *dout, const void *y, const float *topk_w,
+                                const epl_layout_buffers *L, void *dy, int64_t rows, float *dtopk_w, void *stream);
+
 /* Row location (Hierarchical Token-level Scheduling, Token-level Load Partition; Algorithm 1,
  * Quaternary Search): for each position r, the expert whose cumulative range in the packed rows
  * covers r and r's offset inside that expert's rows. For a consumer that cuts the P packed rows

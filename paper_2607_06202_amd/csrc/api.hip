@@ -1,10 +1,13 @@
 // C ABI of libepl: host-side argument checks, layout geometry, workspace sizing and kernel
 // launches on the caller's stream. Stateless and reentrant; allocates nothing.
 #include <limits.h>
+#include <math.h>
 
+#include <initializer_list>
 #include <mutex>
 
 #include "epl_internal.h"
+#include "experts.h"
 
 #define EPL_EXPORT extern "C" __attribute__((visibility("default")))
 
@@ -430,6 +433,295 @@ EPL_EXPORT epl_status epl_combine(const epl_config* cfg, const void* y, const fl
   if (!aligned(y, 16) || !aligned(out, 16) || !aligned(topk_w, 4)) return EPL_ERR_ALIGN;
   return from_hip(epl::launch_combine(y, topk_w, L->pair_row, out, T, cfg->topk, cfg->hidden, pitch_of(cfg),
                                       static_cast<hipStream_t>(stream)));
+}
+
+// ------------------------------------------------------------------ router, experts' products, combine's gradient
+namespace {
+
+int64_t tokens_of(const epl_config* cfg) { return (int64_t)cfg->num_ranks * cfg->tokens_per_rank; }
+
+epl_status check_route(const epl_config* cfg, const epl_route_opts* o, const void* logits, const void* idx,
+                       const void* w) {
+  const epl_status st = check_config(cfg);
+  if (st != EPL_OK) return st;
+  if (!o || (o->score != EPL_SCORE_SOFTMAX && o->score != EPL_SCORE_SIGMOID)) return EPL_ERR_INVALID_ARG;
+  if (o->logits != EPL_LOGITS_F32 && o->logits != EPL_LOGITS_BF16) return EPL_ERR_INVALID_ARG;
+  if ((o->normalize != 0 && o->normalize != 1) || !isfinite(o->scale)) return EPL_ERR_INVALID_ARG;
+  if (tokens_of(cfg) > 0 && (!logits || !idx || !w)) return EPL_ERR_INVALID_ARG;
+  if (!aligned(logits, o->logits == EPL_LOGITS_F32 ? 4 : 2) || !aligned(idx, 4) || !aligned(w, 4))
+    return EPL_ERR_ALIGN;
+  return EPL_OK;
+}
+
+epl::RouteArgs route_args(const epl_config* cfg, const epl_route_opts* o, const void* logits) {
+  epl::RouteArgs p{};
+  p.logits = logits;
+  p.T = tokens_of(cfg);
+  p.E = cfg->num_experts;
+  p.k = cfg->topk;
+  p.bf16 = o->logits == EPL_LOGITS_BF16;
+  p.sigmoid = o->score == EPL_SCORE_SIGMOID;
+  p.normalize = o->normalize != 0;
+  p.scale = o->scale;
+  return p;
+}
+
+bool known_activation(int a) { return a >= EPL_ACT_NONE && a <= EPL_ACT_RELU; }
+bool feature_count(int n) { return n >= 8 && n <= EPL_MAX_HIDDEN && n % 8 == 0; }
+
+// The checks the products share: config, layout offsets, row capacity.
+epl_status check_products(const epl_config* cfg, const epl_layout_buffers* L, int64_t rows) {
+  const epl_status st = check_config(cfg);
+  if (st != EPL_OK) return st;
+  if (!L || !L->expert_off) return EPL_ERR_INVALID_ARG;
+  if (!aligned(L->expert_off, 4)) return EPL_ERR_ALIGN;
+  if (rows < tokens_of(cfg) * cfg->topk) return EPL_ERR_CAPACITY;
+  return EPL_OK;
+}
+
+// stride: 0 (packed) or at least one matrix, in whole 16-byte pieces.
+bool stride_ok(int64_t stride, int64_t matrix, int esize) {
+  return stride == 0 || (stride >= matrix && stride * esize % 16 == 0 && stride <= INT64_MAX / (2 * EPL_MAX_EXPERTS));
+}
+bool pitch_ok(int pitch, int features, int esize) {
+  return pitch == 0 || (pitch >= features && pitch <= EPL_MAX_HIDDEN && pitch * esize % 16 == 0);
+}
+
+// Packed-row buffers must be there if there can be rows; matrices always.
+struct Ptr {
+  const void* p;
+  bool need;
+};
+epl_status check_ptrs(std::initializer_list<Ptr> ptrs, uintptr_t a) {
+  for (const Ptr& x : ptrs)
+    if (x.need && !x.p) return EPL_ERR_INVALID_ARG;
+  for (const Ptr& x : ptrs)
+    if (!aligned(x.p, a)) return EPL_ERR_ALIGN;
+  return EPL_OK;
+}
+
+epl_status check_gated(const epl_config* cfg, const epl_gated* g, const epl_layout_buffers* L, int64_t rows) {
+  const epl_status st = check_products(cfg, L, rows);
+  if (st != EPL_OK) return st;
+  if (!g || !feature_count(g->inner) || !known_activation(g->activation)) return EPL_ERR_INVALID_ARG;
+  if (!stride_ok(g->expert_stride, (int64_t)g->inner * cfg->hidden, is_fp8(cfg) ? 1 : 2)) return EPL_ERR_INVALID_ARG;
+  return EPL_OK;
+}
+
+epl_status check_linear(const epl_config* cfg, const epl_linear* l, const epl_layout_buffers* L, int64_t rows) {
+  const epl_status st = check_products(cfg, L, rows);
+  if (st != EPL_OK) return st;
+  if (!l || !feature_count(l->in_features) || !feature_count(l->out_features) || !known_activation(l->activation))
+    return EPL_ERR_INVALID_ARG;
+  if (l->payload != EPL_PAYLOAD_BF16 && l->payload != EPL_PAYLOAD_FP8_E4M3) return EPL_ERR_UNSUPPORTED;
+  const int esize = l->payload == EPL_PAYLOAD_BF16 ? 2 : 1;
+  if (!pitch_ok(l->in_pitch, l->in_features, esize) || !pitch_ok(l->out_pitch, l->out_features, 2) ||
+      !pitch_ok(l->residual_pitch, l->out_features, 2) ||
+      !stride_ok(l->expert_stride, (int64_t)l->in_features * l->out_features, esize))
+    return EPL_ERR_INVALID_ARG;
+  if (esize == 1 && l->in_features % 128 != 0) return EPL_ERR_UNSUPPORTED;
+  return EPL_OK;
+}
+
+int cap_of(const epl_config* cfg) { return (int)(tokens_of(cfg) * cfg->topk); }
+
+}  // namespace
+
+EPL_EXPORT epl_status epl_route(const epl_config* cfg, const epl_route_opts* opts, const void* logits,
+                                const float* bias, int32_t* topk_idx, float* topk_w, void* stream) {
+  const epl_status st = check_route(cfg, opts, logits, topk_idx, topk_w);
+  if (st != EPL_OK) return st;
+  if (!aligned(bias, 4)) return EPL_ERR_ALIGN;
+  epl::RouteArgs p = route_args(cfg, opts, logits);
+  p.bias = bias;
+  p.idx = topk_idx;
+  p.w = topk_w;
+  return from_hip(epl::launch_route(p, static_cast<hipStream_t>(stream)));
+}
+
+EPL_EXPORT epl_status epl_route_backward(const epl_config* cfg, const epl_route_opts* opts, const void* logits,
+                                         const int32_t* topk_idx, const float* dtopk_w, void* dlogits, void* stream) {
+  const epl_status st = check_route(cfg, opts, logits, topk_idx, dtopk_w);
+  if (st != EPL_OK) return st;
+  if (tokens_of(cfg) > 0 && (!dlogits || dlogits == logits)) return EPL_ERR_INVALID_ARG;
+  if (!aligned(dlogits, opts->logits == EPL_LOGITS_F32 ? 4 : 2)) return EPL_ERR_ALIGN;
+  epl::RouteArgs p = route_args(cfg, opts, logits);
+  p.idx = const_cast<int32_t*>(topk_idx);
+  p.dw = dtopk_w;
+  p.dlogits = dlogits;
+  return from_hip(epl::launch_route_backward(p, static_cast<hipStream_t>(stream)));
+}
+
+EPL_EXPORT epl_status epl_experts_gated(const epl_config* cfg, const epl_gated* gated, const void* recv,
+                                        const float* recv_scale, int64_t rows, const epl_layout_buffers* L,
+                                        const void* w_gate, const void* w_up, const float* gate_scale,
+                                        const float* up_scale, void* h, void* pre, void* stream) {
+  epl_status st = check_gated(cfg, gated, L, rows);
+  if (st != EPL_OK) return st;
+  const bool fp8 = is_fp8(cfg), any = cap_of(cfg) > 0;
+  if (fp8 && cfg->hidden % 128 != 0) return EPL_ERR_UNSUPPORTED;
+  if ((st = check_ptrs({{recv, any}, {w_gate, any}, {w_up, any}, {h, any}, {pre, false}}, 16)) != EPL_OK) return st;
+  if (fp8 && (st = check_ptrs({{recv_scale, any}, {gate_scale, any}, {up_scale, any}}, 4)) != EPL_OK) return st;
+  const int esize = fp8 ? 1 : 2;
+  epl::ForwardArgs p{};
+  p.a = static_cast<const char*>(recv);
+  p.a_scale = recv_scale;
+  p.w = static_cast<const char*>(w_gate);
+  p.w2 = static_cast<const char*>(w_up);
+  p.w_scale = gate_scale;
+  p.w2_scale = up_scale;
+  p.out = static_cast<char*>(h);
+  p.pre = static_cast<char*>(pre);
+  p.expert_off = L->expert_off;
+  p.a_ld = (int64_t)pitch_of(cfg) * esize;
+  p.out_ld = (int64_t)gated->inner * 2;
+  p.expert_stride = gated->expert_stride ? gated->expert_stride : (int64_t)gated->inner * cfg->hidden;
+  p.E = cfg->num_experts;
+  p.cap = cap_of(cfg);
+  p.N = gated->inner;
+  p.K = cfg->hidden;
+  p.act = gated->activation;
+  return from_hip(epl::launch_forward(p, fp8, true, static_cast<hipStream_t>(stream)));
+}
+
+EPL_EXPORT epl_status epl_experts_gated_backward(const epl_config* cfg, const epl_gated* gated, const void* dh,
+                                                 const void* pre, const void* recv, int64_t rows,
+                                                 const epl_layout_buffers* L, const void* w_gate, const void* w_up,
+                                                 void* dpre, void* drecv, void* dw_gate, void* dw_up, void* stream) {
+  epl_status st = check_gated(cfg, gated, L, rows);
+  if (st != EPL_OK) return st;
+  if (is_fp8(cfg)) return EPL_ERR_UNSUPPORTED;
+  const bool any = cap_of(cfg) > 0;
+  if ((st = check_ptrs({{dh, any}, {pre, any}, {recv, any}, {w_gate, any}, {w_up, any}, {dpre, any}, {drecv, any},
+                        {dw_gate, true}, {dw_up, true}}, 16)) != EPL_OK)
+    return st;
+  if (any && drecv == recv) return EPL_ERR_INVALID_ARG;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  const int E = cfg->num_experts, I = gated->inner, cap = cap_of(cfg);
+  hipError_t e = epl::launch_gated_pre_grad(dh, pre, dpre, L->expert_off, E, cap, I, gated->activation, s);
+  if (e != hipSuccess) return from_hip(e);
+  epl::RowGradArgs r{};
+  r.d = static_cast<const char*>(dpre);
+  r.w = static_cast<const char*>(w_gate);
+  r.w2 = static_cast<const char*>(w_up);
+  r.dx = static_cast<char*>(drecv);
+  r.expert_off = L->expert_off;
+  r.dx_ld = (int64_t)pitch_of(cfg) * 2;
+  r.expert_stride = gated->expert_stride ? gated->expert_stride : (int64_t)I * cfg->hidden;
+  r.E = E;
+  r.cap = cap;
+  r.N = I;
+  r.K = cfg->hidden;
+  r.parts = 2;
+  if ((e = epl::launch_row_grad(r, s)) != hipSuccess) return from_hip(e);
+  epl::WeightGradArgs w{};
+  w.d = static_cast<const char*>(dpre);
+  w.x = static_cast<const char*>(recv);
+  w.dw = static_cast<char*>(dw_gate);
+  w.dw2 = static_cast<char*>(dw_up);
+  w.expert_off = L->expert_off;
+  w.x_ld = (int64_t)pitch_of(cfg) * 2;
+  w.E = E;
+  w.cap = cap;
+  w.N = I;
+  w.K = cfg->hidden;
+  w.parts = 2;
+  return from_hip(epl::launch_weight_grad(w, s));
+}
+
+EPL_EXPORT epl_status epl_experts_linear(const epl_config* cfg, const epl_linear* lin, const void* a,
+                                         const float* a_scale, int64_t rows, const epl_layout_buffers* L,
+                                         const void* w, const float* w_scale, const void* bias, const void* residual,
+                                         void* out, void* pre, void* stream) {
+  epl_status st = check_linear(cfg, lin, L, rows);
+  if (st != EPL_OK) return st;
+  const bool fp8 = lin->payload == EPL_PAYLOAD_FP8_E4M3, any = cap_of(cfg) > 0;
+  if ((st = check_ptrs({{a, any}, {w, any}, {bias, false}, {residual, false}, {out, any}, {pre, false}}, 16)) != EPL_OK)
+    return st;
+  if (fp8 && (st = check_ptrs({{a_scale, any}, {w_scale, any}}, 4)) != EPL_OK) return st;
+  const int K = lin->in_features, N = lin->out_features;
+  epl::ForwardArgs p{};
+  p.a = static_cast<const char*>(a);
+  p.a_scale = a_scale;
+  p.w = static_cast<const char*>(w);
+  p.w_scale = w_scale;
+  p.bias = static_cast<const char*>(bias);
+  p.residual = static_cast<const char*>(residual);
+  p.out = static_cast<char*>(out);
+  p.pre = static_cast<char*>(pre);
+  p.expert_off = L->expert_off;
+  p.a_ld = (int64_t)(lin->in_pitch ? lin->in_pitch : K) * (fp8 ? 1 : 2);
+  p.out_ld = (int64_t)(lin->out_pitch ? lin->out_pitch : N) * 2;
+  p.res_ld = (int64_t)(lin->residual_pitch ? lin->residual_pitch : N) * 2;
+  p.expert_stride = lin->expert_stride ? lin->expert_stride : (int64_t)N * K;
+  p.E = cfg->num_experts;
+  p.cap = cap_of(cfg);
+  p.N = N;
+  p.K = K;
+  p.act = lin->activation;
+  return from_hip(epl::launch_forward(p, fp8, false, static_cast<hipStream_t>(stream)));
+}
+
+EPL_EXPORT epl_status epl_experts_linear_backward(const epl_config* cfg, const epl_linear* lin, const void* dy,
+                                                  const void* pre, const void* a, int64_t rows,
+                                                  const epl_layout_buffers* L, const void* w, void* dpre, void* da,
+                                                  void* dw, void* dbias, void* stream) {
+  epl_status st = check_linear(cfg, lin, L, rows);
+  if (st != EPL_OK) return st;
+  if (lin->payload != EPL_PAYLOAD_BF16) return EPL_ERR_UNSUPPORTED;
+  const bool any = cap_of(cfg) > 0, act = lin->activation != EPL_ACT_NONE;
+  if ((st = check_ptrs({{dy, any}, {act ? pre : nullptr, act && any}, {a, any}, {w, any},
+                        {act ? dpre : nullptr, act && any}, {da, any}, {dw, true}, {dbias, false}}, 16)) != EPL_OK)
+    return st;
+  if (any && da == a) return EPL_ERR_INVALID_ARG;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  const int E = cfg->num_experts, K = lin->in_features, N = lin->out_features, cap = cap_of(cfg);
+  hipError_t e = hipSuccess;
+  // dbias before dpre: dpre may overwrite its inputs.
+  if (dbias && (e = epl::launch_bias_grad(dy, pre, dbias, L->expert_off, E, cap, N, lin->activation, s)) != hipSuccess)
+    return from_hip(e);
+  if (act && (e = epl::launch_pre_grad(dy, pre, dpre, L->expert_off, E, cap, N, lin->activation, s)) != hipSuccess)
+    return from_hip(e);
+  epl::RowGradArgs r{};
+  r.d = static_cast<const char*>(act ? dpre : dy);
+  r.w = static_cast<const char*>(w);
+  r.dx = static_cast<char*>(da);
+  r.expert_off = L->expert_off;
+  r.dx_ld = (int64_t)(lin->in_pitch ? lin->in_pitch : K) * 2;
+  r.expert_stride = lin->expert_stride ? lin->expert_stride : (int64_t)N * K;
+  r.E = E;
+  r.cap = cap;
+  r.N = N;
+  r.K = K;
+  r.parts = 1;
+  if ((e = epl::launch_row_grad(r, s)) != hipSuccess) return from_hip(e);
+  epl::WeightGradArgs g{};
+  g.d = r.d;
+  g.x = static_cast<const char*>(a);
+  g.dw = static_cast<char*>(dw);
+  g.expert_off = L->expert_off;
+  g.x_ld = r.dx_ld;
+  g.E = E;
+  g.cap = cap;
+  g.N = N;
+  g.K = K;
+  g.parts = 1;
+  return from_hip(epl::launch_weight_grad(g, s));
+}
+
+EPL_EXPORT epl_status epl_combine_backward(const epl_config* cfg, const void* dout, const void* y,
+                                           const float* topk_w, const epl_layout_buffers* L, void* dy, int64_t rows,
+                                           float* dtopk_w, void* stream) {
+  epl_status st = check_config(cfg);
+  if (st != EPL_OK) return st;
+  if (!L || !L->pair_row) return EPL_ERR_INVALID_ARG;
+  if (!aligned(L->pair_row, 4)) return EPL_ERR_ALIGN;
+  const bool any = tokens_of(cfg) > 0;
+  if ((st = check_ptrs({{dout, any}, {y, any}, {dy, any}}, 16)) != EPL_OK) return st;
+  if ((st = check_ptrs({{topk_w, any}, {dtopk_w, any}}, 4)) != EPL_OK) return st;
+  if (rows < cap_of(cfg)) return EPL_ERR_CAPACITY;
+  return from_hip(epl::launch_combine_grad(dout, y, topk_w, L->pair_row, dy, dtopk_w, tokens_of(cfg), cfg->topk,
+                                           cfg->hidden, pitch_of(cfg), cap_of(cfg), static_cast<hipStream_t>(stream)));
 }
 
 EPL_EXPORT epl_status epl_debug_f32_to_e4m3(const float* in, uint8_t* out, int64_t n, void* stream) {

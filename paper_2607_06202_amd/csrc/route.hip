@@ -1,0 +1,334 @@
+// The router: scores of a token's experts, its top-k choices with their gate weights, and the way back.
+//
+// One wave per token; lane l holds experts l, l + 64, ... The choices are taken one by one: a wave maximum over
+// order-preserving integer keys (a key of 0 is an expert that cannot be chosen), then the lowest expert index
+// among the lanes that hold the maximum.
+//
+// With a selection bias the order is that of score + bias, which fp32 arithmetic can get wrong where two experts
+// nearly tie. So the fp32 keys choose only where every gap between one choice and the next best exceeds what the
+// rounding can make of it; the rare other tokens are chosen again from fp64 scores.
+#include "epl_internal.h"
+#include "experts.h"
+
+namespace epl {
+
+constexpr int kRouteWaves = 4;
+
+__device__ __forceinline__ uint32_t order_key(float v) {
+  const uint32_t u = __float_as_uint(v + 0.0f);  // -0 counts as 0
+  return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ uint64_t order_key(double v) {
+  const uint64_t u = (uint64_t)__double_as_longlong(v + 0.0);
+  return u ^ ((uint64_t)((int64_t)u >> 63) | 0x8000000000000000ull);
+}
+__device__ __forceinline__ float key_value(uint32_t k) {
+  return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
+}
+
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ uint32_t dpp_max(uint32_t v) {
+  const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, ROW_MASK, 0xf, false);
+  return v > o ? v : o;
+}
+// Maximum over the wave, uniform. Row shifts by 1, 2, 4, 8, then the broadcasts of lane 15 and lane 31.
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+  v = dpp_max<0x111, 0xf>(v);
+  v = dpp_max<0x112, 0xf>(v);
+  v = dpp_max<0x114, 0xf>(v);
+  v = dpp_max<0x118, 0xf>(v);
+  v = dpp_max<0x142, 0xa>(v);
+  v = dpp_max<0x143, 0xc>(v);
+  return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+__device__ __forceinline__ uint64_t wave_max(uint64_t v) {
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) {
+    const uint64_t o = __shfl_xor((unsigned long long)v, off, kWave);
+    v = v > o ? v : o;
+  }
+  return v;
+}
+template <class F>
+__device__ __forceinline__ F wave_total(F v) {
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, kWave);
+  return v;
+}
+
+template <bool BF16>
+__device__ __forceinline__ float load_logit(const void* logits, int64_t i) {
+  if constexpr (BF16)
+    return __uint_as_float((uint32_t)((const uint16_t*)logits)[i] << 16);
+  else
+    return ((const float*)logits)[i];
+}
+__device__ __forceinline__ bool can_choose(float l) { return l > -INFINITY; }  // false for NaN
+
+// exp(l - m) for l <= m, 1 where they are equal (also where both are infinite).
+__device__ __forceinline__ float exp_below(float l, float m) { return l == m ? 1.0f : expf(l - m); }
+__device__ __forceinline__ double exp_below(double l, double m) { return l == m ? 1.0 : exp(l - m); }
+template <class F>
+__device__ __forceinline__ F sigmoid(F l) {
+  if constexpr (sizeof(F) == 8)
+    return 1.0 / (1.0 + exp(-l));
+  else
+    return 1.0f / (1.0f + expf(-l));
+}
+
+// Takes the k largest keys in order; lane j ends up with choice j (or -1). next: the largest key left.
+template <int SLOTS, class K>
+__device__ __forceinline__ int take_top(K (&key)[SLOTS], int k, int lane, K* picked, K* next) {
+  int mine = -1;
+  K mine_key = 0;
+  K best = 0;
+  for (int j = 0; j <= k; ++j) {
+    K b = 0;
+    int bs = 0;
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s) {
+      if (key[s] > b) {  // strictly: the lowest slot among equals
+        b = key[s];
+        bs = s;
+      }
+    }
+    best = wave_max(b);
+    if (j == k || best == 0) break;
+    // Lowest expert among the holders: lowest slot first, then lowest lane.
+    const bool holds = b == best;
+    uint64_t who = __ballot(holds);
+    if (who & (who - 1)) {
+#pragma unroll
+      for (int s = 0; s < SLOTS; ++s) {
+        const uint64_t at = __ballot(holds && bs == s);
+        if (at) {
+          who = at;
+          break;
+        }
+      }
+    }
+    const int owner = __builtin_ctzll(who);
+    const int slot = __builtin_amdgcn_readlane(bs, owner);
+    if (lane == j) {
+      mine = slot * kWave + owner;
+      mine_key = best;
+    }
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s)
+      if (lane == owner && s == slot) key[s] = 0;
+  }
+  *picked = mine_key;
+  *next = best;
+  return mine;
+}
+
+// fp64 scores and keys, for a token whose fp32 keys cannot be told apart.
+template <int SLOTS>
+__device__ __forceinline__ int take_top_wide(const float (&l)[SLOTS], const float* bias, float m, int E,
+                                                       int k, bool sig, int lane) {
+  double z[SLOTS], sum = 0.0;
+#pragma unroll
+  for (int s = 0; s < SLOTS; ++s) {
+    z[s] = sig ? sigmoid((double)l[s]) : (can_choose(l[s]) ? exp_below((double)l[s], (double)m) : 0.0);
+    sum += z[s];
+  }
+  sum = wave_total(sum);
+  uint64_t key[SLOTS], a, b;
+#pragma unroll
+  for (int s = 0; s < SLOTS; ++s) {
+    const int e = s * kWave + lane;
+    key[s] = 0;
+    if (e < E && can_choose(l[s])) {
+      const double v = (sig ? z[s] : z[s] / sum) + (double)bias[e];
+      if (v > -INFINITY) key[s] = order_key(v);
+    }
+  }
+  return take_top<SLOTS, uint64_t>(key, k, lane, &a, &b);
+}
+
+// Weight of each chosen logit among the choices, p_j / sum of the chosen p, from scores scaled so that the largest
+// stays in range: exp(l - m) for the softmax (its own sum cancels), exp(l - m) / (1 + exp(l)) for sigmoids that
+// are all below one half, m the largest chosen logit. Zero where 64-bit sigmoids vanish.
+__device__ __forceinline__ float share(float l, bool valid, bool sig) {
+  constexpr float kVanish = -709.7827f;  // 1 / (1 + exp(-l)) is 0 in fp64 below
+  const float m = key_value(wave_max(valid ? order_key(l) : 0u));
+  float s = 0.0f;
+  if (valid) {
+    if (!sig)
+      s = exp_below(l, m);
+    else if (m >= 0.0f)
+      s = sigmoid(l);
+    else
+      s = m < kVanish ? 0.0f : exp_below(l, m) / (1.0f + expf(l));
+  }
+  const float total = wave_total(s);
+  return total > 0.0f ? s / total : 0.0f;
+}
+
+template <int SLOTS, bool BF16>
+__global__ void __launch_bounds__(kRouteWaves* kWave) route_kernel(RouteArgs p) {
+  const int lane = threadIdx.x % kWave;
+  const int E = p.E, k = p.k;
+  for (int64_t g = (int64_t)blockIdx.x * kRouteWaves + threadIdx.x / kWave; g < p.T;
+       g += (int64_t)gridDim.x * kRouteWaves) {
+    float l[SLOTS];
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s) {
+      const int e = s * kWave + lane;
+      l[s] = e < E ? load_logit<BF16>(p.logits, g * E + e) : -INFINITY;
+    }
+    // The largest logit, and for the softmax scores the sum.
+    uint32_t top = 0;
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s) top = can_choose(l[s]) ? std::max(top, order_key(l[s])) : top;
+    const bool need_sum = !p.sigmoid && (!p.normalize || p.bias);
+    float m = 0.0f, sum = 1.0f;
+    if (need_sum) {
+      m = key_value(wave_max(top));
+      sum = 0.0f;
+#pragma unroll
+      for (int s = 0; s < SLOTS; ++s) sum += can_choose(l[s]) ? exp_below(l[s], m) : 0.0f;
+      sum = wave_total(sum);
+    }
+    uint32_t key[SLOTS], picked, next;
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s) {
+      key[s] = 0;
+      if (!can_choose(l[s])) continue;
+      if (p.bias) {
+        const float v = (p.sigmoid ? sigmoid(l[s]) : exp_below(l[s], m) / sum) + p.bias[s * kWave + lane];
+        if (v > -INFINITY) key[s] = order_key(v);
+      } else {
+        key[s] = order_key(l[s]);
+      }
+    }
+    int e = take_top<SLOTS, uint32_t>(key, k, lane, &picked, &next);
+    if (p.bias) {
+      // Error of an fp32 key: the exponential and its argument 1e-7, the sum of up to 1024 terms (16 per lane,
+      // then a tree of 6) and the division 1.4e-6, all relative to a score of at most 1, and half a unit of the
+      // final sum. Two keys further apart than twice that are in the right order.
+      uint32_t after = (uint32_t)__shfl_down((int)picked, 1, kWave);
+      if (lane == k - 1) after = next;
+      const float a = key_value(picked), b = key_value(after);
+      const bool near = lane < k && picked && after && !(a - b > 4e-6f + 2.4e-7f * (fabsf(a) + fabsf(b)));
+      if (__ballot(near)) e = take_top_wide<SLOTS>(l, p.bias, m, E, k, p.sigmoid, lane);
+    }
+    // Lane j: the score and weight of choice j.
+    const bool valid = lane < k && e >= 0;
+    const float le = valid ? load_logit<BF16>(p.logits, g * E + e) : -INFINITY;
+    float sc = 0.0f;
+    if (p.normalize)
+      sc = share(le, valid, p.sigmoid);
+    else if (valid)
+      sc = p.sigmoid ? sigmoid(le) : exp_below(le, m) / sum;
+    if (lane < k) {
+      p.idx[g * k + lane] = e;
+      p.w[g * k + lane] = sc * p.scale;
+    }
+  }
+}
+
+// Gradient of the logits. With p the scores, d_j = scale dw_j for choice j of expert e_j:
+//   softmax               dl = p (dp - sum p dp), dp_e the sum of d_j over the choices of e
+//   sigmoid               dl = dp p (1 - p)
+//   renormalised softmax  dl_e = sum of w_j (d_j - sum_i w_i d_i) over the choices of e, w as in the forward pass:
+//                         the row's own sum drops out
+//   renormalised sigmoid  the same terms times (1 - p)
+// Choices outside [0, E) count for nothing, and neither does a chosen expert that is masked.
+template <int SLOTS, bool BF16>
+__global__ void __launch_bounds__(kRouteWaves* kWave) route_backward_kernel(RouteArgs p) {
+  const int lane = threadIdx.x % kWave;
+  const int E = p.E, k = p.k;
+  for (int64_t g = (int64_t)blockIdx.x * kRouteWaves + threadIdx.x / kWave; g < p.T;
+       g += (int64_t)gridDim.x * kRouteWaves) {
+    const int e = lane < k ? p.idx[g * k + lane] : -1;
+    const bool in = e >= 0 && e < E;
+    const float le = in ? load_logit<BF16>(p.logits, g * E + e) : -INFINITY;
+    const bool valid = in && can_choose(le);
+    float dw = valid ? p.dw[g * k + lane] * p.scale : 0.0f;
+    const bool need_row = !p.sigmoid && !p.normalize;
+    float l[SLOTS], m = 0.0f, sum = 1.0f;
+    if (need_row) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int s = 0; s < SLOTS; ++s) {
+        const int ee = s * kWave + lane;
+        l[s] = ee < E ? load_logit<BF16>(p.logits, g * E + ee) : -INFINITY;
+        top = can_choose(l[s]) ? std::max(top, order_key(l[s])) : top;
+      }
+      m = key_value(wave_max(top));
+      sum = 0.0f;
+#pragma unroll
+      for (int s = 0; s < SLOTS; ++s) sum += can_choose(l[s]) ? exp_below(l[s], m) : 0.0f;
+      sum = wave_total(sum);
+    }
+    // What each choice adds to its expert's logit.
+    float sc;
+    if (p.normalize) {
+      sc = share(le, valid, p.sigmoid);
+      dw -= wave_total(dw * sc);
+    } else {
+      sc = !valid ? 0.0f : p.sigmoid ? sigmoid(le) : exp_below(le, m) / sum;
+    }
+    float add = valid ? dw * sc : 0.0f;
+    if (p.sigmoid && valid) add *= sigmoid(-le);
+    const float dot = need_row ? wave_total(add) : 0.0f;
+    float d[SLOTS];
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s)
+      d[s] = need_row && can_choose(l[s]) ? -(exp_below(l[s], m) / sum) * dot : 0.0f;
+    for (int j = 0; j < k; ++j) {
+      const int ej = __builtin_amdgcn_readlane(valid ? e : -1, j);
+      const float aj = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(add), j));
+#pragma unroll
+      for (int s = 0; s < SLOTS; ++s)
+        if (ej == s * kWave + lane) d[s] += aj;
+    }
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s) {
+      const int ee = s * kWave + lane;
+      if (ee >= E) continue;
+      if constexpr (BF16)
+        ((uint16_t*)p.dlogits)[g * E + ee] = (uint16_t)f32x2_to_bf16x2(d[s], 0.0f);
+      else
+        ((float*)p.dlogits)[g * E + ee] = d[s];
+    }
+  }
+}
+
+template <int SLOTS>
+static void launch_slots(const RouteArgs& p, bool back, dim3 grid, hipStream_t s) {
+  const dim3 block(kRouteWaves * kWave);
+  if (back) {
+    if (p.bf16)
+      hipLaunchKernelGGL((route_backward_kernel<SLOTS, true>), grid, block, 0, s, p);
+    else
+      hipLaunchKernelGGL((route_backward_kernel<SLOTS, false>), grid, block, 0, s, p);
+  } else {
+    if (p.bf16)
+      hipLaunchKernelGGL((route_kernel<SLOTS, true>), grid, block, 0, s, p);
+    else
+      hipLaunchKernelGGL((route_kernel<SLOTS, false>), grid, block, 0, s, p);
+  }
+}
+
+static hipError_t launch(const RouteArgs& p, bool back, hipStream_t s) {
+  if (p.T == 0) return hipSuccess;
+  const dim3 grid((unsigned)std::min<int64_t>((p.T + kRouteWaves - 1) / kRouteWaves, 1 << 20));
+  if (p.E <= 64)
+    launch_slots<1>(p, back, grid, s);
+  else if (p.E <= 128)
+    launch_slots<2>(p, back, grid, s);
+  else if (p.E <= 256)
+    launch_slots<4>(p, back, grid, s);
+  else if (p.E <= 512)
+    launch_slots<8>(p, back, grid, s);
+  else
+    launch_slots<16>(p, back, grid, s);
+  return hipGetLastError();
+}
+
+hipError_t launch_route(const RouteArgs& p, hipStream_t s) { return launch(p, false, s); }
+hipError_t launch_route_backward(const RouteArgs& p, hipStream_t s) { return launch(p, true, s); }
+
+}  // namespace epl

@@ -1,4 +1,5 @@
-"""Python binding of libepl (MoE dispatch / combine on one MI355X): argument marshalling only.
+"""Python binding of libepl (the MoE layer on one MI355X: router, dispatch, the experts' products, combine):
+argument marshalling only.
 
 Every step runs in the HIP kernels behind the C ABI declared in ``include/epl.h``. This module
 allocates output tensors with torch on the tensors' device (the receive buffer, on request, as one
@@ -95,6 +96,26 @@ DAF_TOKEN_FLAG_FUSION = 1  # EPL_DAF_TOKEN_FLAG_FUSION
 DAF_DATA_CHECKSUM = 2      # EPL_DAF_DATA_CHECKSUM
 
 
+SCORE = {"softmax": 0, "sigmoid": 1}                          # epl_score
+LOGITS = {torch.float32: 0, torch.bfloat16: 1}                # epl_logits
+ACTIVATION = {"none": 0, "silu": 1, "gelu": 2, "relu": 3}     # epl_activation
+
+
+class RouteOpts(ctypes.Structure):
+    _fields_ = [("logits", ctypes.c_int32), ("score", ctypes.c_int32), ("normalize", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
+
+
+class Gated(ctypes.Structure):
+    _fields_ = [("inner", ctypes.c_int32), ("activation", ctypes.c_int32), ("expert_stride", ctypes.c_int64)]
+
+
+class Linear(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("in_features", "out_features", "in_pitch", "out_pitch",
+                                              "residual_pitch", "activation", "payload")]
+    _fields_ += [("expert_stride", ctypes.c_int64)]
+
+
 class LayoutBuffers(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("send_cnt", "rank_cnt", "expert_off", "rank_off", "seg_off",
                                                "tok_nranks", "pair_row", "pair_rslot", "recv_src", "recv_j",
@@ -164,6 +185,17 @@ def lib() -> ctypes.CDLL:
         L.epl_hop_schedule.argtypes = [CP, P, P, I32, P, I32, I32, P, P, P, P]
         L.epl_dispatch_scheduled.restype = ctypes.c_int
         L.epl_dispatch_scheduled.argtypes = [CP, P, LP, P, P, I64, I32, I32, P]
+        RP, GP, NP = ctypes.POINTER(RouteOpts), ctypes.POINTER(Gated), ctypes.POINTER(Linear)
+        for name, args in [
+                ("epl_route", [CP, RP, P, P, P, P, P]),
+                ("epl_route_backward", [CP, RP, P, P, P, P, P]),
+                ("epl_experts_gated", [CP, GP, P, P, I64, LP, P, P, P, P, P, P, P]),
+                ("epl_experts_gated_backward", [CP, GP, P, P, P, I64, LP, P, P, P, P, P, P, P]),
+                ("epl_experts_linear", [CP, NP, P, P, I64, LP, P, P, P, P, P, P, P]),
+                ("epl_experts_linear_backward", [CP, NP, P, P, P, I64, LP, P, P, P, P, P, P]),
+                ("epl_combine_backward", [CP, P, P, P, LP, P, I64, P, P])]:
+            getattr(L, name).restype = ctypes.c_int
+            getattr(L, name).argtypes = args
         _lib = L
     return _lib
 
@@ -746,6 +778,314 @@ def combine(cfg: Config, y: torch.Tensor, topk_w: torch.Tensor, L: Layout, out: 
         _check(lib().epl_combine(ctypes.byref(cfg), y.data_ptr(), topk_w.data_ptr(), ctypes.byref(bufs),
                                  out.data_ptr(), _stream(dev)), "epl_combine")
     return out
+
+
+def _one_of(table: dict, value, name: str) -> int:
+    if value not in table:
+        raise ValueError("%s must be one of %s, got %r" % (name, ", ".join(map(str, table)), value))
+    return table[value]
+
+
+def _route_args(cfg: Config, logits: torch.Tensor, score: str, normalize: bool, scale: float):
+    """Checks shared by route and route_backward -> RouteOpts."""
+    _dev(logits, "logits")
+    if _rows_of(logits, "logits", cfg.num_experts) != cfg.T:
+        raise ValueError("logits has %d rows, expected T = %d" % (logits.shape[0], cfg.T))
+    return RouteOpts(_one_of(LOGITS, logits.dtype, "logits' type"), _one_of(SCORE, score, "score"), int(bool(normalize)),
+                     scale)
+
+
+def _per_choice(cfg: Config, t: torch.Tensor, name: str, dtype) -> None:
+    _dev(t, name, dtype)
+    if _rows_of(t, name, cfg.topk) < cfg.T:
+        raise ValueError("%s has %d rows, needs T = %d" % (name, t.shape[0], cfg.T))
+
+
+def route(cfg: Config, logits: torch.Tensor, bias: torch.Tensor | None = None, score: str = "softmax",
+          normalize: bool = True, scale: float = 1.0, topk_idx: torch.Tensor | None = None,
+          topk_w: torch.Tensor | None = None):
+    """epl_route: logits [T, E] fp32 or bf16 (-inf masks an expert), bias [E] fp32 added to the scores for the
+    choice alone -> (topk_idx [T, k] int32, -1 where no expert is left; topk_w [T, k] fp32), as layout and
+    combine take them."""
+    opts = _route_args(cfg, logits, score, normalize, scale)
+    dev = logits.device
+    if bias is not None:
+        _dev(bias, "bias", torch.float32)
+        if bias.numel() != cfg.num_experts:
+            raise ValueError("bias must hold E values")
+    if topk_idx is None:
+        topk_idx = torch.empty(cfg.T, cfg.topk, dtype=torch.int32, device=dev)
+    if topk_w is None:
+        topk_w = torch.empty(cfg.T, cfg.topk, dtype=torch.float32, device=dev)
+    _per_choice(cfg, topk_idx, "topk_idx", torch.int32)
+    _per_choice(cfg, topk_w, "topk_w", torch.float32)
+    _same_device(dev, bias=bias, topk_idx=topk_idx, topk_w=topk_w)
+    with _on(dev):
+        _check(lib().epl_route(ctypes.byref(cfg), ctypes.byref(opts), logits.data_ptr(),
+                               None if bias is None else bias.data_ptr(), topk_idx.data_ptr(), topk_w.data_ptr(),
+                               _stream(dev)), "epl_route")
+    return topk_idx, topk_w
+
+
+def route_backward(cfg: Config, logits: torch.Tensor, topk_idx: torch.Tensor, dtopk_w: torch.Tensor,
+                   score: str = "softmax", normalize: bool = True, scale: float = 1.0,
+                   dlogits: torch.Tensor | None = None) -> torch.Tensor:
+    """epl_route_backward: the gradient of route's weights with respect to logits, given its choices -> dlogits
+    [T, E] in the type of logits. score, normalize and scale as in the forward call."""
+    opts = _route_args(cfg, logits, score, normalize, scale)
+    dev = logits.device
+    _per_choice(cfg, topk_idx, "topk_idx", torch.int32)
+    _per_choice(cfg, dtopk_w, "dtopk_w", torch.float32)
+    if dlogits is None:
+        dlogits = torch.empty_like(logits)
+    _dev(dlogits, "dlogits", logits.dtype)
+    if _rows_of(dlogits, "dlogits", cfg.num_experts) < cfg.T:
+        raise ValueError("dlogits has %d rows, needs T = %d" % (dlogits.shape[0], cfg.T))
+    _same_device(dev, topk_idx=topk_idx, dtopk_w=dtopk_w, dlogits=dlogits)
+    with _on(dev):
+        _check(lib().epl_route_backward(ctypes.byref(cfg), ctypes.byref(opts), logits.data_ptr(),
+                                        topk_idx.data_ptr(), dtopk_w.data_ptr(), dlogits.data_ptr(), _stream(dev)),
+               "epl_route_backward")
+    return dlogits
+
+
+def _packed(t, name: str, dtype, width: int, cfg: Config, pitch: int | None = None) -> int:
+    """A buffer of packed rows: 2-D [>= T*k, width] on the GPU with dense columns and one stride between rows
+    (pitch, if given) -> elements from one row to the next."""
+    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+        raise ValueError("%s must be a GPU tensor" % name)
+    if t.dtype != dtype:
+        raise ValueError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    rows = _rows_of(t, name, width)
+    if rows < recv_rows_cap(cfg):
+        raise ValueError("%s has %d rows, needs T*k = %d" % (name, rows, recv_rows_cap(cfg)))
+    at = t.stride(0) if rows > 1 else (pitch or width)
+    if (width > 1 and t.stride(1) != 1) or at < width or (pitch is not None and at != pitch):
+        raise ValueError("%s rows must be %s elements apart and dense, got strides %s" % (
+            name, "at least %d" % width if pitch is None else pitch, t.stride()))
+    return at
+
+
+def _matrices(t, name: str, dtype, cfg: Config, shape=None) -> int:
+    """The experts' matrices [E, out, in]: each one dense, any stride between experts -> that stride."""
+    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+        raise ValueError("%s must be a GPU tensor" % name)
+    if t.dtype != dtype:
+        raise ValueError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    if t.dim() != 3 or t.shape[0] != cfg.num_experts or (shape is not None and tuple(t.shape[1:]) != tuple(shape)):
+        raise ValueError("%s must be [%d, %s], got %s" % (
+            name, cfg.num_experts, "out, in" if shape is None else "%d, %d" % tuple(shape), tuple(t.shape)))
+    if t.stride(2) != 1 or t.stride(1) != t.shape[2]:
+        raise ValueError("%s: each expert's matrix must be contiguous, got strides %s" % (name, t.stride()))
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+def _scales(t, name: str, rows: int, cols: int) -> int:
+    p = _dev(t, name, torch.float32)
+    if _rows_of(t, name, cols) < rows:
+        raise ValueError("%s has %d rows, needs %d" % (name, t.shape[0], rows))
+    return p
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _rows_out(t, cfg: Config, width: int, dev, pitch: int = 0) -> torch.Tensor:
+    """t, or a new [T*k, width] bf16 buffer of packed rows pitch (0: width) elements apart."""
+    if t is not None:
+        return t
+    return torch.empty(max(recv_rows_cap(cfg), 1), pitch or width, dtype=torch.bfloat16, device=dev)[:, :width]
+
+
+def experts_gated(cfg: Config, recv: torch.Tensor, L: Layout, w_gate: torch.Tensor, w_up: torch.Tensor,
+                  activation: str = "silu", recv_scale: torch.Tensor | None = None,
+                  gate_scale: torch.Tensor | None = None, up_scale: torch.Tensor | None = None,
+                  h: torch.Tensor | None = None, pre: torch.Tensor | None = None, keep_pre: bool = False):
+    """epl_experts_gated: h = act(recv w_gate^T) * (recv w_up^T) on every expert's packed rows. recv as dispatch
+    wrote it (for an fp8 cfg with recv_scale, and E4M3 bytes w_gate, w_up with a scale per output feature,
+    gate_scale and up_scale [E, I]); w_gate, w_up [E, I, H], halves of one [E, 2I, H] tensor included ->
+    (h [T*k, I] bf16, pre [T*k, 2I] or None). Pass pre, or keep_pre, for the backward pass."""
+    dev = recv.device
+    fp8 = cfg.payload == PAYLOAD_FP8_E4M3
+    dt = torch.uint8 if fp8 else torch.bfloat16
+    _packed(recv, "recv", dt, cfg.hidden, cfg, cfg.pitch)
+    stride = _matrices(w_gate, "w_gate", dt, cfg)
+    inner = w_gate.shape[1]
+    if w_gate.shape[2] != cfg.hidden or _matrices(w_up, "w_up", dt, cfg, (inner, cfg.hidden)) != stride:
+        raise ValueError("w_gate and w_up must be [E, I, %d] with one stride between experts" % cfg.hidden)
+    sp = [None, None, None]
+    if fp8:
+        sp = [_scales(recv_scale, "recv_scale", recv_rows_cap(cfg), cfg.hidden // 128),
+              _scales(gate_scale, "gate_scale", cfg.num_experts, inner),
+              _scales(up_scale, "up_scale", cfg.num_experts, inner)]
+        _same_device(dev, recv_scale=recv_scale, gate_scale=gate_scale, up_scale=up_scale)
+    h = _rows_out(h, cfg, inner, dev)
+    _packed(h, "h", torch.bfloat16, inner, cfg, inner)
+    if pre is not None or keep_pre:
+        pre = _rows_out(pre, cfg, 2 * inner, dev)
+        _packed(pre, "pre", torch.bfloat16, 2 * inner, cfg, 2 * inner)
+    _check_layout(cfg, L, dev)
+    _same_device(dev, w_gate=w_gate, w_up=w_up, h=h, pre=pre)
+    g = Gated(inner, _one_of(ACTIVATION, activation, "activation"), stride)
+    bufs = L.buffers()
+    with _on(dev):
+        _check(lib().epl_experts_gated(ctypes.byref(cfg), ctypes.byref(g), recv.data_ptr(), sp[0], recv.shape[0],
+                                       ctypes.byref(bufs), w_gate.data_ptr(), w_up.data_ptr(), sp[1], sp[2],
+                                       h.data_ptr(), _ptr(pre), _stream(dev)), "epl_experts_gated")
+    return h, pre
+
+
+def experts_gated_backward(cfg: Config, dh: torch.Tensor, pre: torch.Tensor, recv: torch.Tensor, L: Layout,
+                           w_gate: torch.Tensor, w_up: torch.Tensor, activation: str = "silu",
+                           dpre: torch.Tensor | None = None, drecv: torch.Tensor | None = None,
+                           dw_gate: torch.Tensor | None = None, dw_up: torch.Tensor | None = None):
+    """epl_experts_gated_backward: from dh [T*k, I] and the kept pre -> (drecv [T*k, H] at cfg's pitch, dw_gate,
+    dw_up [E, I, H]), all bf16. dpre [T*k, 2I] is scratch for the gradient of pre; it may be pre itself."""
+    dev = recv.device
+    bf = torch.bfloat16
+    if cfg.payload != PAYLOAD_BF16:
+        raise EplError(5, "epl_experts_gated_backward (bf16 only)")
+    H = cfg.hidden
+    _packed(recv, "recv", bf, H, cfg, cfg.pitch)
+    stride = _matrices(w_gate, "w_gate", bf, cfg)
+    inner = w_gate.shape[1]
+    if w_gate.shape[2] != H or _matrices(w_up, "w_up", bf, cfg, (inner, H)) != stride:
+        raise ValueError("w_gate and w_up must be [E, I, %d] with one stride between experts" % H)
+    _packed(dh, "dh", bf, inner, cfg, inner)
+    _packed(pre, "pre", bf, 2 * inner, cfg, 2 * inner)
+    dpre = _rows_out(dpre, cfg, 2 * inner, dev)
+    _packed(dpre, "dpre", bf, 2 * inner, cfg, 2 * inner)
+    drecv = _rows_out(drecv, cfg, H, dev, cfg.pitch)
+    _packed(drecv, "drecv", bf, H, cfg, cfg.pitch)
+    dw_gate = torch.empty(w_gate.shape, dtype=bf, device=dev) if dw_gate is None else dw_gate
+    dw_up = torch.empty(w_gate.shape, dtype=bf, device=dev) if dw_up is None else dw_up
+    for n, t in (("dw_gate", dw_gate), ("dw_up", dw_up)):
+        if _matrices(t, n, bf, cfg, (inner, H)) != inner * H:
+            raise ValueError("%s must be contiguous" % n)
+    _check_layout(cfg, L, dev)
+    _same_device(dev, dh=dh, pre=pre, w_gate=w_gate, w_up=w_up, dpre=dpre, drecv=drecv, dw_gate=dw_gate, dw_up=dw_up)
+    g = Gated(inner, _one_of(ACTIVATION, activation, "activation"), stride)
+    bufs = L.buffers()
+    rows = min(t.shape[0] for t in (recv, dh, pre, dpre, drecv))
+    with _on(dev):
+        _check(lib().epl_experts_gated_backward(ctypes.byref(cfg), ctypes.byref(g), dh.data_ptr(), pre.data_ptr(),
+                                                recv.data_ptr(), rows, ctypes.byref(bufs), w_gate.data_ptr(),
+                                                w_up.data_ptr(), dpre.data_ptr(), drecv.data_ptr(), dw_gate.data_ptr(),
+                                                dw_up.data_ptr(), _stream(dev)), "epl_experts_gated_backward")
+    return drecv, dw_gate, dw_up
+
+
+def _biases(t, name: str, cfg: Config, width: int):
+    if t is None:
+        return None
+    p = _dev(t, name, torch.bfloat16)
+    if tuple(t.shape) != (cfg.num_experts, width):
+        raise ValueError("%s must be [%d, %d], got %s" % (name, cfg.num_experts, width, tuple(t.shape)))
+    return p
+
+
+def experts_linear(cfg: Config, a: torch.Tensor, L: Layout, w: torch.Tensor, bias: torch.Tensor | None = None,
+                   residual: torch.Tensor | None = None, activation: str = "none", a_scale: torch.Tensor | None = None,
+                   w_scale: torch.Tensor | None = None, out: torch.Tensor | None = None,
+                   pre: torch.Tensor | None = None, keep_pre: bool = False):
+    """epl_experts_linear: out = act(a w^T + bias) + residual on every expert's packed rows. a [T*k, K] (rows any
+    pitch apart) and w [E, N, K] bf16, or both E4M3 bytes with a_scale [T*k, K/128] and w_scale [E, N]; bias
+    [E, N], residual [T*k, N] -> (out [T*k, N], pre [T*k, N] or None). A new out of cfg.hidden columns has cfg's
+    pitch, as combine reads it; pass pre, or keep_pre, to keep the activation's argument for the backward pass."""
+    dev = a.device
+    dt = a.dtype if a.dtype in (torch.uint8, torch.bfloat16) else torch.bfloat16
+    stride = _matrices(w, "w", dt, cfg)
+    N, K = w.shape[1], w.shape[2]
+    lda = _packed(a, "a", dt, K, cfg)
+    sp = [None, None]
+    if dt == torch.uint8:
+        sp = [_scales(a_scale, "a_scale", recv_rows_cap(cfg), K // 128), _scales(w_scale, "w_scale", cfg.num_experts, N)]
+        _same_device(dev, a_scale=a_scale, w_scale=w_scale)
+    bp = _biases(bias, "bias", cfg, N)
+    out = _rows_out(out, cfg, N, dev, cfg.pitch if N == cfg.hidden else 0)
+    ldo = _packed(out, "out", torch.bfloat16, N, cfg)
+    ldr = 0 if residual is None else _packed(residual, "residual", torch.bfloat16, N, cfg)
+    if pre is not None or keep_pre:
+        pre = _rows_out(pre, cfg, N, dev)
+        _packed(pre, "pre", torch.bfloat16, N, cfg, N)
+    _check_layout(cfg, L, dev)
+    _same_device(dev, w=w, bias=bias, residual=residual, out=out, pre=pre)
+    lin = Linear(K, N, lda, ldo, ldr, _one_of(ACTIVATION, activation, "activation"),
+                 PAYLOAD_FP8_E4M3 if dt == torch.uint8 else PAYLOAD_BF16, stride)
+    bufs = L.buffers()
+    rows = min(a.shape[0], out.shape[0])
+    with _on(dev):
+        _check(lib().epl_experts_linear(ctypes.byref(cfg), ctypes.byref(lin), a.data_ptr(), sp[0], rows,
+                                        ctypes.byref(bufs), w.data_ptr(), sp[1], bp, _ptr(residual), out.data_ptr(),
+                                        _ptr(pre), _stream(dev)), "epl_experts_linear")
+    return out, pre
+
+
+def experts_linear_backward(cfg: Config, dy: torch.Tensor, a: torch.Tensor, L: Layout, w: torch.Tensor,
+                            pre: torch.Tensor | None = None, activation: str = "none", need_dbias: bool = False,
+                            dpre: torch.Tensor | None = None, da: torch.Tensor | None = None,
+                            dw: torch.Tensor | None = None, dbias: torch.Tensor | None = None):
+    """epl_experts_linear_backward: from dy [T*k, N] (contiguous; the residual's gradient is dy itself) and, with an
+    activation, the kept pre -> (da [T*k, K] at a's pitch, dw [E, N, K], dbias [E, N] or None), all bf16. dpre
+    [T*k, N] is scratch for the gradient of pre; it may be pre or dy."""
+    dev = a.device
+    bf = torch.bfloat16
+    stride = _matrices(w, "w", bf, cfg)
+    N, K = w.shape[1], w.shape[2]
+    lda = _packed(a, "a", bf, K, cfg)
+    _packed(dy, "dy", bf, N, cfg, N)
+    act = _one_of(ACTIVATION, activation, "activation")
+    if act:
+        _packed(pre, "pre", bf, N, cfg, N)
+        dpre = _rows_out(dpre, cfg, N, dev)
+        _packed(dpre, "dpre", bf, N, cfg, N)
+    else:
+        pre = dpre = None
+    da = _rows_out(da, cfg, K, dev, lda)
+    _packed(da, "da", bf, K, cfg, lda)
+    dw = torch.empty(w.shape, dtype=bf, device=dev) if dw is None else dw
+    if _matrices(dw, "dw", bf, cfg, (N, K)) != N * K:
+        raise ValueError("dw must be contiguous")
+    if need_dbias and dbias is None:
+        dbias = torch.empty(cfg.num_experts, N, dtype=bf, device=dev)
+    bp = _biases(dbias, "dbias", cfg, N)
+    _check_layout(cfg, L, dev)
+    _same_device(dev, dy=dy, pre=pre, dpre=dpre, w=w, da=da, dw=dw, dbias=dbias)
+    lin = Linear(K, N, lda, 0, 0, act, PAYLOAD_BF16, stride)
+    bufs = L.buffers()
+    rows = min(t.shape[0] for t in (a, dy, da, pre, dpre) if t is not None)
+    with _on(dev):
+        _check(lib().epl_experts_linear_backward(ctypes.byref(cfg), ctypes.byref(lin), dy.data_ptr(), _ptr(pre),
+                                                 a.data_ptr(), rows, ctypes.byref(bufs), w.data_ptr(), _ptr(dpre),
+                                                 da.data_ptr(), dw.data_ptr(), bp, _stream(dev)),
+               "epl_experts_linear_backward")
+    return da, dw, dbias
+
+
+def combine_backward(cfg: Config, dout: torch.Tensor, y: torch.Tensor, topk_w: torch.Tensor, L: Layout,
+                     dy: torch.Tensor | None = None, dtopk_w: torch.Tensor | None = None):
+    """epl_combine_backward: dout [T, H] bf16, y and topk_w as combine read them -> (dy [T*k, H] bf16 at cfg's pitch,
+    dtopk_w [T, k] fp32). Dispatch's own gradient is combine(cfg, drecv, ones, L)."""
+    dev = y.device
+    _dev(dout, "dout", torch.bfloat16)
+    if _rows_of(dout, "dout", cfg.hidden) < cfg.T:
+        raise ValueError("dout has %d rows, needs T = %d" % (dout.shape[0], cfg.T))
+    _packed(y, "y", torch.bfloat16, cfg.hidden, cfg, cfg.pitch)
+    _per_choice(cfg, topk_w, "topk_w", torch.float32)
+    _check_layout(cfg, L, dev)
+    dy = _rows_out(dy, cfg, cfg.hidden, dev, cfg.pitch)
+    _packed(dy, "dy", torch.bfloat16, cfg.hidden, cfg, cfg.pitch)
+    if dtopk_w is None:
+        dtopk_w = torch.empty(max(cfg.T, 1), cfg.topk, dtype=torch.float32, device=dev)
+    _per_choice(cfg, dtopk_w, "dtopk_w", torch.float32)
+    _same_device(dev, dout=dout, topk_w=topk_w, dy=dy, dtopk_w=dtopk_w)
+    bufs = L.buffers()
+    with _on(dev):
+        _check(lib().epl_combine_backward(ctypes.byref(cfg), dout.data_ptr(), y.data_ptr(), topk_w.data_ptr(),
+                                          ctypes.byref(bufs), dy.data_ptr(), dy.shape[0], dtopk_w.data_ptr(),
+                                          _stream(dev)), "epl_combine_backward")
+    return dy, dtopk_w
 
 
 class PreparedLayer:

@@ -1,0 +1,272 @@
+"""The experts' products (epl_experts_gated, epl_experts_linear and their gradients) against 64-bit references, at
+the sizes where a tile, a step of the reduction or a segment ends: experts without rows, with one row, with more
+than a tile; rows behind the last one that hold NaN and must stay untouched; pitches, gaps between the experts'
+matrices, features that are no multiple of a tile; every activation; the fp8 payload."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2607_06202_amd import epl
+from tests.gpu_util import device
+from tests.products_util import (BF16_HALF_STEP, FEW, SLOPE, Packed, act, act_grad, assert_within, dequantise_rows,
+                                 dequantise_weights, quantise_rows, quantise_weights, rounded, routing_of_counts,
+                                 sum_error, weights)
+
+pytestmark = pytest.mark.gpu
+
+# Rows of each expert. The tile edges at 16, 32, 128 and 256 rows, empty and single-row experts.
+COUNTS = {
+    "one_token": [0, 0, 1, 0, 1, 0, 0, 1],
+    "few": [3, 0, 1, 2, 0, 5, 16, 17],
+    "edges": [127, 128, 129, 0, 1, 64, 255, 31],
+    "one_expert": [0, 0, 0, 700, 0, 0, 0, 0],
+    "none": [0, 0, 0, 0, 0, 0, 0, 0],
+    "large": [513, 256, 300, 1, 0, 257, 640, 90],
+}
+
+
+def packed(counts, H, k=2, seed=0, **kw):
+    rng = np.random.default_rng(seed)
+    idx = routing_of_counts(COUNTS[counts], 8, k, rng)
+    idx = np.concatenate([idx, np.full((3, k), -1, np.int32)])  # padded tokens
+    return Packed(idx, 8, H, device(), **kw)
+
+
+def gated_reference(pk, x, wg, wu, name):
+    """h, pre and their bounds, in 64 bits, rows 0..P-1."""
+    K = x.shape[1]
+    I = wg.shape[1]
+    h = torch.zeros(pk.P, I, dtype=torch.float64)
+    hb = torch.zeros_like(h)
+    pre = torch.zeros(pk.P, 2 * I, dtype=torch.float64)
+    pb = torch.zeros_like(pre)
+    for e, a, b in pk.experts():
+        if a == b:
+            continue
+        xe = x[a:b]
+        g, u = xe @ wg[e].T, xe @ wu[e].T
+        dg = sum_error(K + 2, xe.abs() @ wg[e].abs().T) + FEW * g.abs()
+        du = sum_error(K + 2, xe.abs() @ wu[e].abs().T) + FEW * u.abs()
+        v = act(name, g)
+        h[a:b] = v * u
+        err = SLOPE * dg * (u.abs() + du) + (v.abs() + FEW) * du + FEW * (v * u).abs()
+        hb[a:b] = rounded(v * u, err)
+        pre[a:b] = torch.cat([g, u], 1)
+        pb[a:b] = torch.cat([rounded(g, dg), rounded(u, du)], 1)
+    return h, hb, pre, pb
+
+
+CASES = [  # counts, H, I, pitch, activation, gap between matrices, halves of one tensor
+    ("few", 8, 8, 0, "silu", 0, False),
+    ("few", 200, 72, 256, "gelu", 0, True),
+    ("one_token", 512, 264, 0, "silu", 0, False),
+    ("edges", 136, 136, 192, "silu", 64, False),
+    ("edges", 64, 128, 0, "relu", 0, True),
+    ("one_expert", 328, 104, 0, "none", 0, False),
+    ("none", 64, 64, 0, "silu", 0, False),
+    ("large", 192, 296, 256, "silu", 0, True),
+    ("large", 1032, 40, 0, "gelu", 8, False),
+]
+
+
+def gated_inputs(counts, H, I, pitch, gap, halves, seed):
+    g = torch.Generator().manual_seed(seed)
+    pk = packed(counts, H, row_pitch=pitch)
+    x = pk.buffer(g, H, pitch)
+    if halves:
+        both = weights(g, 8, 2 * I, H, pk.dev)
+        wg, wu = both[:, :I], both[:, I:]
+    else:
+        stride = I * H + gap if gap else 0
+        wg, wu = weights(g, 8, I, H, pk.dev, stride), weights(g, 8, I, H, pk.dev, stride)
+    return pk, x, wg, wu, g
+
+
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "-".join(map(str, c)))
+def test_gated_forward(case):
+    counts, H, I, pitch, name, gap, halves = case
+    pk, x, wg, wu, _ = gated_inputs(counts, H, I, pitch, gap, halves, 1)
+    h, pre = pk.out(I), pk.out(2 * I)
+    epl.experts_gated(pk.cfg, x, pk.L, wg, wu, name, h=h, pre=pre)
+    alone, none = epl.experts_gated(pk.cfg, x, pk.L, wg, wu, name)
+    torch.cuda.synchronize()
+    assert none is None and torch.equal(alone[: pk.P], h[: pk.P])
+    want, bound, wpre, pbound = gated_reference(pk, x[: pk.P].cpu().double(), wg.cpu().double(), wu.cpu().double(), name)
+    assert_within(h[: pk.P], want, bound, "h")
+    assert_within(pre[: pk.P], wpre, pbound, "pre")
+    pk.assert_untouched(h, "h")
+    pk.assert_untouched(pre, "pre")
+
+
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "-".join(map(str, c)))
+def test_gated_backward(case):
+    counts, H, I, pitch, name, gap, halves = case
+    pk, x, wg, wu, g = gated_inputs(counts, H, I, pitch, gap, halves, 2)
+    pre, dh = pk.buffer(g, 2 * I), pk.buffer(g, I)
+    dx = pk.out(H, pitch)
+    dpre = pk.out(2 * I)
+    _, dwg, dwu = epl.experts_gated_backward(pk.cfg, dh, pre, x, pk.L, wg, wu, name, dpre=dpre, drecv=dx)
+    torch.cuda.synchronize()
+    kept = pre.clone()
+    dx2, dwg2, dwu2 = epl.experts_gated_backward(pk.cfg, dh, kept, x, pk.L, wg, wu, name, dpre=kept)  # in place
+    torch.cuda.synchronize()
+    assert torch.equal(dx2[: pk.P], dx[: pk.P]) and torch.equal(dwg, dwg2) and torch.equal(dwu, dwu2)
+    pk.assert_untouched(dx, "drecv")
+    pk.assert_untouched(dpre, "dpre")
+    xd, wgd, wud = x.cpu().double(), wg.cpu().double(), wu.cpu().double()
+    dhd, pd = dh.cpu().double(), pre.cpu().double()
+    for e, a, b in pk.experts():
+        if a == b:
+            assert not dwg[e].any() and not dwu[e].any()
+            continue
+        gg, u, d = pd[a:b, :I], pd[a:b, I:], dhd[a:b]
+        dg, du = d * u * act_grad(name, gg), d * act(name, gg)
+        # dpre: its factors' roundings and act's and act''s own (relative to values below SLOPE and |g|), then bf16
+        eg = rounded(dg, FEW * (d * u).abs() * SLOPE)
+        eu = rounded(du, FEW * (d * gg).abs())
+        assert_within(dpre[a:b, :I], dg, eg, "dpre gate")
+        assert_within(dpre[a:b, I:], du, eu, "dpre up")
+        want = dg @ wgd[e] + du @ wud[e]
+        terms = (dg.abs() + eg) @ wgd[e].abs() + (du.abs() + eu) @ wud[e].abs()
+        err = eg @ wgd[e].abs() + eu @ wud[e].abs() + sum_error(2 * I + 2, terms)
+        assert_within(dx[a:b], want, rounded(want, err), "drecv")
+        for got, dd, ee, what in ((dwg, dg, eg, "dw_gate"), (dwu, du, eu, "dw_up")):
+            want = dd.T @ xd[a:b]
+            err = ee.T @ xd[a:b].abs() + sum_error(b - a + 2, (dd.abs() + ee).T @ xd[a:b].abs())
+            assert_within(got[e], want, rounded(want, err), what)
+
+
+FP8_CASES = [("few", 128, 8, 0, "silu"), ("edges", 384, 136, 448, "silu"), ("large", 256, 72, 0, "gelu"),
+             ("one_token", 1024, 200, 0, "silu"), ("none", 128, 64, 0, "silu")]
+
+
+@pytest.mark.parametrize("case", FP8_CASES, ids=lambda c: "-".join(map(str, c)))
+def test_gated_forward_fp8(case):
+    """E4M3 products are exact in fp32 up to the sums: 448 * 448 needs 8 bits of significand. Each 128-element block
+    is summed (128 additions), scaled (one rounding) and added (one), then the output scale multiplies."""
+    counts, H, I, pitch, name = case
+    g = torch.Generator().manual_seed(3)
+    pk = packed(counts, H, payload="fp8", row_pitch=pitch)
+    x = torch.randn(pk.rows, H, generator=g)
+    x[: pk.P, :128] *= 100.0  # blocks of very different scales
+    if pk.P:
+        x[0] = 0.0            # an all-zero row: scale 0
+    q, s = quantise_rows(x)
+    q[pk.P:] = 0x7F           # NaN behind the last row
+    s[pk.P:] = float("nan")
+    buf = torch.full((pk.rows, pitch or H), 0x7F, dtype=torch.uint8)
+    buf[:, :H] = q
+    qg, sg = quantise_weights(torch.randn(8, I, H, generator=g) * H ** -0.5)
+    qu, su = quantise_weights(torch.randn(8, I, H, generator=g) * H ** -0.5)
+    d = pk.dev
+    h, pre = pk.out(I), pk.out(2 * I)
+    epl.experts_gated(pk.cfg, buf.to(d)[:, :H], pk.L, qg.to(d), qu.to(d), name, s.to(d), sg.to(d), su.to(d), h, pre)
+    torch.cuda.synchronize()
+    want, bound, wpre, pbound = gated_reference(pk, dequantise_rows(q[: pk.P], s[: pk.P]), dequantise_weights(qg, sg),
+                                                dequantise_weights(qu, su), name)
+    assert_within(h[: pk.P], want, bound, "h")
+    assert_within(pre[: pk.P], wpre, pbound, "pre")
+    pk.assert_untouched(h, "h")
+    pk.assert_untouched(pre, "pre")
+
+
+LINEAR_CASES = [  # counts, K, N, in pitch, out pitch, activation, bias, residual (own pitch), gap
+    ("few", 8, 8, 0, 0, "none", False, False, 0),
+    ("few", 72, 200, 80, 256, "silu", True, True, 0),
+    ("one_token", 264, 512, 0, 0, "none", True, False, 0),
+    ("edges", 136, 136, 0, 192, "gelu", True, True, 24),
+    ("edges", 128, 64, 0, 0, "none", False, True, 0),
+    ("one_expert", 104, 328, 0, 0, "relu", True, False, 0),
+    ("none", 64, 64, 0, 0, "gelu", True, True, 0),
+    ("large", 296, 192, 304, 256, "none", True, True, 0),
+    ("large", 40, 1032, 0, 0, "silu", False, False, 0),
+]
+
+
+@pytest.mark.parametrize("case", LINEAR_CASES, ids=lambda c: "-".join(map(str, c)))
+def test_linear_forward(case):
+    counts, K, N, ip, op, name, has_bias, has_res, gap = case
+    g = torch.Generator().manual_seed(4)
+    pk = packed(counts, max(N, 8))
+    a = pk.buffer(g, K, ip)
+    w = weights(g, 8, N, K, pk.dev, N * K + gap if gap else 0)
+    bias = torch.randn(8, N, generator=g).bfloat16().to(pk.dev) if has_bias else None
+    res = pk.buffer(g, N, N + 16) if has_res else None
+    out, pre = pk.out(N, op), pk.out(N)
+    epl.experts_linear(pk.cfg, a, pk.L, w, bias, res, name, out=out, pre=pre)
+    alone, none = epl.experts_linear(pk.cfg, a, pk.L, w, bias, res, name)
+    torch.cuda.synchronize()
+    assert none is None and torch.equal(alone[: pk.P], out[: pk.P])
+    pk.assert_untouched(out, "out")
+    pk.assert_untouched(pre, "pre")
+    ad, wd = a.cpu().double(), w.cpu().double()
+    for e, r0, r1 in pk.experts():
+        v = ad[r0:r1] @ wd[e].T
+        err = sum_error(K + 2, ad[r0:r1].abs() @ wd[e].abs().T)
+        if has_bias:
+            v = v + bias[e].cpu().double()
+            err = err + FEW * (v.abs() + bias[e].cpu().double().abs())
+        assert_within(pre[r0:r1], v, rounded(v, err), "pre")
+        y = act(name, v)
+        err = SLOPE * err + FEW * y.abs()
+        if has_res:
+            r = res[r0:r1].cpu().double()
+            y = y + r
+            err = err + FEW * (y.abs() + r.abs())
+        assert_within(out[r0:r1], y, rounded(y, err), "out")
+
+
+@pytest.mark.parametrize("case", LINEAR_CASES, ids=lambda c: "-".join(map(str, c)))
+def test_linear_backward(case):
+    counts, K, N, ip, _, name, has_bias, _, gap = case
+    g = torch.Generator().manual_seed(5)
+    pk = packed(counts, max(N, 8))
+    a, dy = pk.buffer(g, K, ip), pk.buffer(g, N)
+    pre = pk.buffer(g, N) if name != "none" else None
+    w = weights(g, 8, N, K, pk.dev, N * K + gap if gap else 0)
+    da = pk.out(K, ip)
+    _, dw, db = epl.experts_linear_backward(pk.cfg, dy, a, pk.L, w, pre, name, need_dbias=has_bias, da=da)
+    torch.cuda.synchronize()
+    assert (db is not None) == has_bias
+    pk.assert_untouched(da, "da")
+    ad, wd, dyd = a.cpu().double(), w.cpu().double(), dy.cpu().double()
+    for e, r0, r1 in pk.experts():
+        if r0 == r1:
+            assert not dw[e].any() and (db is None or not db[e].any())
+            continue
+        d = dyd[r0:r1]
+        er = torch.zeros_like(d)
+        sums = FEW * d.abs() * SLOPE
+        if name != "none":
+            d = d * act_grad(name, pre[r0:r1].cpu().double())
+            er = rounded(d, sums)
+        want = d @ wd[e]
+        err = er @ wd[e].abs() + sum_error(N + 2, (d.abs() + er) @ wd[e].abs())
+        assert_within(da[r0:r1], want, rounded(want, err), "da")
+        want = d.T @ ad[r0:r1]
+        err = er.T @ ad[r0:r1].abs() + sum_error(r1 - r0 + 2, (d.abs() + er).T @ ad[r0:r1].abs())
+        assert_within(dw[e], want, rounded(want, err), "dw")
+        if has_bias:
+            want = d.sum(0)
+            err = sums.sum(0) + sum_error(r1 - r0 + 2, d.abs().sum(0))
+            assert_within(db[e], want, rounded(want, err), "dbias")
+
+
+def test_linear_forward_fp8():
+    counts, K, N = "edges", 256, 200
+    g = torch.Generator().manual_seed(6)
+    pk = packed(counts, K, payload="fp8")
+    q, s = quantise_rows(torch.randn(pk.rows, K, generator=g))
+    qw, sw = quantise_weights(torch.randn(8, N, K, generator=g))
+    bias = torch.randn(8, N, generator=g).bfloat16()
+    d = pk.dev
+    out = pk.out(N)
+    epl.experts_linear(pk.cfg, q.to(d), pk.L, qw.to(d), bias.to(d), None, "relu", s.to(d), sw.to(d), out=out)
+    torch.cuda.synchronize()
+    x, w = dequantise_rows(q, s), dequantise_weights(qw, sw)
+    for e, r0, r1 in pk.experts():
+        v = x[r0:r1] @ w[e].T + bias[e].double()
+        err = sum_error(K + 4, x[r0:r1].abs() @ w[e].abs().T) + FEW * (v.abs() + bias[e].double().abs())
+        y = v.clamp_min(0)
+        assert_within(out[r0:r1], y, rounded(y, err), "out")
+    pk.assert_untouched(out, "out")
