@@ -19,7 +19,7 @@ CSRC = os.path.join(PKG, "csrc")
 BUILD_DIR = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libepl.so")
 SOURCES = ["api.hip", "layout.hip", "small.hip", "dispatch.hip", "decomposed.hip", "combine.hip", "locate.hip", "schedule.hip",
-           "route.hip", "experts.hip", "combine_grad.hip"]
+           "route.hip", "experts.hip", "experts_few.hip", "combine_grad.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

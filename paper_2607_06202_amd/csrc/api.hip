@@ -676,12 +676,8 @@ EPL_EXPORT epl_status epl_experts_linear_backward(const epl_config* cfg, const e
   if (any && da == a) return EPL_ERR_INVALID_ARG;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const int E = cfg->num_experts, K = lin->in_features, N = lin->out_features, cap = cap_of(cfg);
-  hipError_t e = hipSuccess;
-  // dbias before dpre: dpre may overwrite its inputs.
-  if (dbias && (e = epl::launch_bias_grad(dy, pre, dbias, L->expert_off, E, cap, N, lin->activation, s)) != hipSuccess)
-    return from_hip(e);
-  if (act && (e = epl::launch_pre_grad(dy, pre, dpre, L->expert_off, E, cap, N, lin->activation, s)) != hipSuccess)
-    return from_hip(e);
+  hipError_t e = epl::launch_pre_grad(dy, pre, dpre, dbias, L->expert_off, E, cap, N, lin->activation, s);
+  if (e != hipSuccess) return from_hip(e);
   epl::RowGradArgs r{};
   r.d = static_cast<const char*>(act ? dpre : dy);
   r.w = static_cast<const char*>(w);

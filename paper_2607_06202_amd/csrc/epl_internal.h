@@ -18,6 +18,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 // Buffer resource descriptor word 3 for raw (untyped) buffer accesses on CDNA3/CDNA4.
 constexpr int kBufferRsrcWord3 = 0x00020000;
 // Cache-policy operand of the raw buffer builtins: bit 0 = sc0, bit 1 = nt, bit 4 = sc1.
+constexpr int kCachePolicyNt = 2;
 constexpr int kCachePolicySc1 = 16;
 constexpr int kCachePolicySc1Nt = 18;
 

@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 namespace epl {
 
 // Row strides (…_ld) are in bytes, expert_stride in elements. cap: packed rows, the bound on expert_off.
@@ -39,15 +41,26 @@ struct WeightGradArgs {
   int E, cap, N, K, parts;
 };
 
+// The kernels' choice by the rows that there can be (cap = T*k) over E experts.
+//
+// few_rows: the split reduction of experts_few.hip against 128 x 256 tiles, us. 128 experts, 2048 to 2 x 768, top-8:
+// 8 rows 16.0 / 32.3, 16 rows 29.3 / 33.8, 32 rows 43.5 / 36.8, 64 rows 71 / 76, 128 rows 108 / 105; 768 to 2048,
+// 8 rows 14.5 / 15.4, 32 rows 27 / 21. E4M3, 64 experts, 7168 to 2 x 2048: 8 rows 56 / 92, 32 rows 173 / 229, 128 rows
+// 353 / 459, 512 rows 434 / 494.
+inline bool few_rows(int64_t cap, int E, bool fp8) { return cap <= (fp8 ? std::max(16, 8 * E) : 16); }
+// many_rows: 256 x 256 tiles against 128 x 256, us, 32 experts, 7168 to 2 x 2048: 256 rows each 607 / 658 (the smaller
+// tile first), 512 rows 1001 / 1023, 1024 rows 1844 / 1774, 2048 rows 3565 / 3421; 2048 to 7168: 980 / 1001 at 1024,
+// 1851 / 1833 at 2048.
+inline bool many_rows(int64_t cap, int E) { return cap / E >= 1024; }
+hipError_t launch_forward_few(const ForwardArgs& p, bool fp8, bool gated, hipStream_t stream);
 hipError_t launch_forward(const ForwardArgs& p, bool fp8, bool gated, hipStream_t stream);
 hipError_t launch_row_grad(const RowGradArgs& p, hipStream_t stream);
 hipError_t launch_weight_grad(const WeightGradArgs& p, hipStream_t stream);
 hipError_t launch_gated_pre_grad(const void* dh, const void* pre, void* dpre, const int32_t* expert_off, int E,
                                  int cap, int I, int act, hipStream_t stream);
-hipError_t launch_pre_grad(const void* dy, const void* pre, void* dpre, const int32_t* expert_off, int E, int cap,
-                           int N, int act, hipStream_t stream);
-hipError_t launch_bias_grad(const void* dy, const void* pre, void* dbias, const int32_t* expert_off, int E, int cap,
-                            int N, int act, hipStream_t stream);
+// dpre (with an activation) and, unless dbias is null, dbias.
+hipError_t launch_pre_grad(const void* dy, const void* pre, void* dpre, void* dbias, const int32_t* expert_off, int E,
+                           int cap, int N, int act, hipStream_t stream);
 
 struct RouteArgs {
   const void* logits;  // [T][E] fp32 or bf16

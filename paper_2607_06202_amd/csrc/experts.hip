@@ -7,308 +7,373 @@ namespace epl {
 
 constexpr int kCus = 256;  // compute units of an MI355X
 
-// The steps of one tile: stage s+1 is loaded while stage s is multiplied; one barrier per step.
-template <class S, class P, class A, class B>
-__device__ __forceinline__ void run_steps(const P& prod, A& a, B& b, int steps, uint32_t lds, int wave,
-                                          f32x4 (&acc)[S::MF][S::NF]) {
-  uint32_t cur = lds, nxt = lds + S::kStage;
-  a.load(cur, wave);
-  b.load(cur + A::kBytes, wave);
-  for (int s = 0; s < steps; ++s) {
-    wait_tiles();
-    if (s + 1 < steps) {
-      a.load(nxt, wave);
-      b.load(nxt + A::kBytes, wave);
-    }
-    prod.step(cur, acc, nullptr);
-    const uint32_t t = cur;
-    cur = nxt;
-    nxt = t;
+// The lane's place in a tile's results: rows row + 16 f, and eight columns from col + 32 g of each pair of column
+// fragments.
+template <class S, bool SPLIT = false>
+struct LanePlace {
+  int row, col;
+  __device__ __forceinline__ LanePlace(int wave, int lane)
+      : row((wave / S::WN) * S::MF * 16 + (lane & 15)),
+        col((wave % S::WN) * S::NF * 16 / (SPLIT ? 2 : 1) + (lane >> 4) * 8) {}
+};
+
+// Stores of a tile's results, bounded by the descriptor: every lane issues every store, so that the number of them is
+// known (run_tiles counts on it), and those past the last row or column are dropped.
+struct TileOut {
+  __amdgpu_buffer_rsrc_t rs;
+  int ld, cols;
+  __device__ __forceinline__ TileOut(char* base, int64_t row0, int64_t ld_, int col0, int rows, int cols_)
+      : ld((int)ld_), cols(cols_) {
+    const uint64_t at = (uint64_t)(base + row0 * ld_ + (int64_t)col0 * 2);
+    const uint64_t uni = (uint64_t)(uint32_t)uniform((int)(uint32_t)at) | (uint64_t)(uint32_t)uniform((int)(at >> 32)) << 32;
+    rs = __builtin_amdgcn_make_buffer_rsrc((void*)uni, 0, uniform((rows - 1) * (int)ld_ + cols_ * 2), kBufferRsrcWord3);
   }
-}
+  // Streamed: results that stayed in L2 would push out the operands (8% of a gated tile of 16 steps).
+  __device__ __forceinline__ void put(int r, int c, u32x4 v) const {
+    __builtin_amdgcn_raw_buffer_store_b128(v, rs, c < cols ? r * ld + c * 2 : kOutOfRange, 0, kCachePolicyNt);
+  }
+  __device__ __forceinline__ void store(int r, int c, const float (&v)[8]) const { put(r, c, pack8(v)); }
+  // Columns c.. and c + 32.. of row r from every lane, as whole 128-byte lines: lanes rho and rho + 8 of a row of 16
+  // exchange halves, so that one store takes rows 0..7 of the fragment and the other rows 8..15.
+  __device__ __forceinline__ void store2(int r, int c, const float (&v0)[8], const float (&v1)[8]) const {
+    const bool low = (r & 8) == 0;
+    const u32x4 p0 = pack8(v0), p1 = pack8(v1);
+    u32x4 mine, other;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      mine[i] = low ? p0[i] : p1[i];
+      other[i] = (uint32_t)__builtin_amdgcn_mov_dpp((int)(low ? p1[i] : p0[i]), 0x128, 0xf, 0xf, false);  // row_ror:8
+    }
+    const int cc = low ? c : c + 32;
+    put(r & ~8, cc, low ? mine : other);
+    put(r | 8, cc, low ? other : mine);
+  }
+};
 
 template <class S>
-__device__ __forceinline__ void clear(f32x4 (&acc)[S::MF][S::NF]) {
+__device__ __forceinline__ void store_tile(const TileOut& out, int row, int col, f32x4 (&acc)[S::MF][S::NF]) {
 #pragma unroll
-  for (int m = 0; m < S::MF; ++m)
+  for (int g = 0; g < S::NF / 4; ++g)
 #pragma unroll
-    for (int n = 0; n < S::NF; ++n) acc[m][n] = f32x4{0, 0, 0, 0};
-}
-
-__device__ __forceinline__ u32x4 pack8(const float (&v)[8]) {
-  return u32x4{f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]), f32x2_to_bf16x2(v[4], v[5]),
-               f32x2_to_bf16x2(v[6], v[7])};
-}
-__device__ __forceinline__ void unpack8(u32x4 w, float (&v)[8]) {
+    for (int f = 0; f < S::MF; ++f) {
+      float v[2][8];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[2 * i] = bf16lo_to_f32(w[i]);
-    v[2 * i + 1] = bf16hi_to_f32(w[i]);
-  }
+      for (int i = 0; i < 16; ++i) v[i / 8][i % 8] = acc[f][g * 4 + i / 4][i % 4];
+      out.store2(row + f * 16, col + g * 64, v[0], v[1]);
+    }
 }
 
 // ---------------------------------------------------------------- forward
 // GATED: B tile = BN/2 gate rows and BN/2 up rows; BN/2 output columns.
 template <class S, bool FP8, bool GATED>
-__global__ void __launch_bounds__(S::kThreads) forward_kernel(ForwardArgs p) {
-  __shared__ __attribute__((aligned(1024))) char tiles[2 * S::kStage];
-  __shared__ int mt[EPL_MAX_EXPERTS + 1];
-  constexpr int kCols = GATED ? S::BN / 2 : S::BN;  // output columns of a tile
-  const int wave = uniform(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-  const int rho = lane & 15, q = lane >> 4;
-  const int esize = FP8 ? 1 : 2;
-  count_row_tiles<S::BM>(p.expert_off, p.E, p.cap, mt);
-  Products<S, false, false, FP8, GATED> prod;
-  prod.init(wave, lane);
-  Operand<false, S::BM, S::kWaves, false> a;
-  Operand<false, S::BN, S::kWaves, true, GATED> b;
-  const int nt = (p.N + kCols - 1) / kCols;
-  const int64_t total = (int64_t)mt[p.E] * nt;
-  const int steps = (p.K * esize + kStepBytes - 1) / kStepBytes;
-  const uint32_t lds = lds_addr(tiles);
-  const int slot = xcd_slot(blockIdx.x, gridDim.x);
-  for (int64_t t = slot; t < total; t += gridDim.x) {
-    const int e = uniform(quaternary_find(mt, p.E, t / nt));
-    int beg, end, m, n;
-    expert_rows(p.expert_off, e, p.cap, beg, end);
-    beg = uniform(beg);
-    end = uniform(end);
-    const int m0 = uniform(mt[e]);
-    band_tile(t - (int64_t)m0 * nt, uniform(mt[e + 1]) - m0, nt, 8, m, n);
-    const int row0 = beg + m * S::BM, rows = end - row0;
-    const int col0 = n * kCols, cols = p.N - col0;
-    if (m < 0 || rows <= 0) continue;
-    const int64_t ldb = (int64_t)p.K * esize;
-    const int64_t boff = e * p.expert_stride * esize + col0 * ldb;
-    a.lanes(rows, p.a_ld, wave, lane);
+struct ForwardJob {
+  static constexpr int kCols = GATED ? S::BN / 2 : S::BN;  // output columns of a tile
+  static constexpr int kPairs = kCols / S::WN / 32;        // pairs of column fragments of a wave
+  static constexpr int kEsize = FP8 ? 1 : 2;
+  struct Tile {
+    int64_t t;
+    int e, row0, rows, col0, steps;
+  };
+  const ForwardArgs& p;
+  const RowTable& tab;
+  int wave, lane, nt, steps;
+  int64_t total;
+  LanePlace<S, GATED> at;
+  __device__ __forceinline__ ForwardJob(const ForwardArgs& p_, const RowTable& tab_, int wave_, int lane_)
+      : p(p_), tab(tab_), wave(wave_), lane(lane_), at(wave_, lane_) {
+    nt = (p.N + kCols - 1) / kCols;
+    steps = S::steps(p.K * kEsize, FP8);
+    total = (int64_t)uniform(tab.mt[p.E]) * nt;
+  }
+  __device__ __forceinline__ bool place(Tile& t) const {
+    if (t.t >= total) return false;
+    int m, n;
+    t.e = uniform(quaternary_find(tab.mt, p.E, t.t / nt));
+    const int m0 = uniform(tab.mt[t.e]), beg = uniform(tab.off[t.e]), end = uniform(tab.off[t.e + 1]);
+    band_tile(t.t - (int64_t)m0 * nt, uniform(tab.mt[t.e + 1]) - m0, nt, 8, m, n);
+    t.row0 = beg + m * S::BM;
+    t.rows = std::min(end - t.row0, S::BM);
+    t.col0 = n * kCols;
+    t.steps = steps;
+    return true;
+  }
+  __device__ __forceinline__ bool first(Tile& t) const {
+    t.t = xcd_slot(blockIdx.x, gridDim.x);
+    return place(t);
+  }
+  __device__ __forceinline__ bool next(Tile& t) const {
+    t.t += gridDim.x;
+    return place(t);
+  }
+  template <class A, class B>
+  __device__ __forceinline__ void begin(const Tile& t, A& a, B& b) const {
+    const int64_t ldb = (int64_t)p.K * kEsize;
+    const int64_t boff = t.e * p.expert_stride * kEsize + t.col0 * ldb;
+    const int cols = std::min(p.N - t.col0, kCols);
+    a.lanes(t.rows, p.a_ld, wave, lane);
     b.lanes(cols, ldb, wave, lane);
-    a.start_rows(p.a + row0 * p.a_ld, nullptr, std::min(rows, S::BM), p.a_ld, p.K * esize);
-    b.start_rows(p.w + boff, p.w2 + boff, std::min(cols, kCols), ldb, p.K * esize);
-    f32x4 acc[S::MF][S::NF];
-    clear<S>(acc);
-    const int wm0 = (wave / S::WN) * S::MF * 16, wn0 = (wave % S::WN) * S::NF * 16 / (GATED ? 2 : 1);
-    wait_tiles();  // the previous tile's reads are done
-    if constexpr (!FP8) {
-      run_steps<S>(prod, a, b, steps, lds, wave, acc);
-    } else {
-      // Row scales one step ahead; touched right after the wait for the step's tiles, where they have arrived.
-      float sc[S::MF], sn[S::MF];
-      const float* sp[S::MF];
+    a.start_rows(p.a + t.row0 * p.a_ld, nullptr, t.rows, p.a_ld, p.K * kEsize);
+    b.start_rows(p.w + boff, p.w2 + boff, cols, ldb, p.K * kEsize);
+  }
+  template <class A, class B>
+  __device__ __forceinline__ void turn(const Tile&, int, A&, B&) const {}
+  // One scale per lane for 64 rows; a tile has at most 256, and waves beyond its rows load some again.
+  __device__ __forceinline__ void load_scales(const Tile& t, int step, uint32_t lds) const {
+    constexpr int kSpans = S::BM / kWave;
+    const int span = wave % kSpans * kWave, nb = p.K / 128;
+    const u32x4 rs = make_rsrc((uint64_t)(p.a_scale + (int64_t)t.row0 * nb + step), step < nb ? ((int64_t)(t.rows - 1) * nb + 1) * 4 : 0);
+    load_words_to_lds(rs, lds + span * 4, (span + lane) * nb * 4);
+  }
+  template <int N>
+  __device__ __forceinline__ void wait(bool stored) const {
+    constexpr int kEach = kPairs * S::MF;
+    if (!stored)
+      wait_tiles<N>();
+    else if (!p.pre)
+      wait_tiles<std::min(63, N + kEach)>();
+    else
+      wait_tiles<std::min(63, N + kEach * (GATED ? 3 : 2))>();
+  }
+  __device__ __forceinline__ void finish(const Tile& t, f32x4 (&acc)[S::MF][S::NF]) const {
+    const int cols = std::min(p.N - t.col0, kCols);
+    const TileOut out(p.out, t.row0, p.out_ld, t.col0, t.rows, cols);
+    const int64_t pre_ld = (int64_t)p.N * (GATED ? 4 : 2);
+    const TileOut pre(p.pre, t.row0, pre_ld, t.col0, t.rows, cols);
+    const TileOut pre2(p.pre, t.row0, pre_ld, t.col0 + p.N, t.rows, cols);
+    constexpr int kTake = kPairs % 2 ? 1 : 2;  // groups of 32 columns stored together
 #pragma unroll
-      for (int f = 0; f < S::MF; ++f) {
-        sp[f] = p.a_scale + (int64_t)std::min(row0 + wm0 + f * 16 + rho, end - 1) * (p.K / 128);
-        sn[f] = sp[f][0];
-      }
-      uint32_t cur = lds, nxt = lds + S::kStage;
-      a.load(cur, wave);
-      b.load(cur + S::BM * kStepBytes, wave);
-      for (int s = 0; s < steps; ++s) {
-        wait_tiles();
+    for (int g0 = 0; g0 < kPairs; g0 += kTake) {
+      const int c0 = at.col + g0 * 32;
+      float s1[kTake][8], s2[kTake][8], bias[kTake][8];
 #pragma unroll
-        for (int f = 0; f < S::MF; ++f) {
-          asm volatile("" : "+v"(sn[f]));
-          sc[f] = sn[f];
+      for (int k = 0; k < kTake; ++k) {
+        // In range for the lanes past the last column.
+        const int64_t cc = (int64_t)t.e * p.N + t.col0 + std::min(c0 + k * 32, cols - 8);
+        if constexpr (FP8) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            s1[k][i] = p.w_scale[cc + i];
+            if constexpr (GATED) s2[k][i] = p.w2_scale[cc + i];
+          }
         }
-        if (s + 1 < steps) {
-#pragma unroll
-          for (int f = 0; f < S::MF; ++f) sn[f] = sp[f][s + 1];
-          a.load(nxt, wave);
-          b.load(nxt + S::BM * kStepBytes, wave);
+        if constexpr (!GATED) {
+          if (p.bias) unpack8(*(const u32x4*)(p.bias + cc * 2), bias[k]);
         }
-        prod.step(cur, acc, sc);
-        const uint32_t u = cur;
-        cur = nxt;
-        nxt = u;
-      }
-    }
-    // Lane: rows m0 + rho of each row fragment, eight consecutive columns of each pair of column fragments.
-    constexpr int kPairs = (GATED ? S::NF / 2 : S::NF) / 2;
-#pragma unroll
-    for (int g = 0; g < kPairs; ++g) {
-      const int c = col0 + wn0 + g * 32 + q * 8;
-      if (c >= p.N) continue;
-      float s1[8], s2[8], bias[8];
-      if constexpr (FP8) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          s1[i] = p.w_scale[(int64_t)e * p.N + c + i];
-          if constexpr (GATED) s2[i] = p.w2_scale[(int64_t)e * p.N + c + i];
-        }
-      }
-      if constexpr (!GATED) {
-        if (p.bias) unpack8(*(const u32x4*)(p.bias + ((int64_t)e * p.N + c) * 2), bias);
       }
 #pragma unroll
       for (int f = 0; f < S::MF; ++f) {
-        const int64_t row = row0 + wm0 + f * 16 + rho;
-        if (row >= end) continue;
-        float v[8], u[8];
+        const int r = at.row + f * 16;
+        float v[kTake][8], u[kTake][8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          v[i] = acc[f][g * 2 + i / 4][i % 4];
-          if constexpr (FP8) v[i] *= s1[i];
+        for (int j = 0; j < kTake * 8; ++j) {
+          const int k = j / 8, i = j % 8, at_n = (g0 + k) * 2 + i / 4;
+          v[k][i] = acc[f][at_n][i % 4];
+          if constexpr (FP8) v[k][i] *= s1[k][i];
           if constexpr (GATED) {
-            u[i] = acc[f][S::NF / 2 + g * 2 + i / 4][i % 4];
-            if constexpr (FP8) u[i] *= s2[i];
+            u[k][i] = acc[f][S::NF / 2 + at_n][i % 4];
+            if constexpr (FP8) u[k][i] *= s2[k][i];
           } else if (p.bias) {
-            v[i] += bias[i];
+            v[k][i] += bias[k][i];
           }
         }
         if (p.pre) {
-          if constexpr (GATED) {
-            *(u32x4*)(p.pre + (row * 2 * p.N + c) * 2) = pack8(v);
-            *(u32x4*)(p.pre + (row * 2 * p.N + p.N + c) * 2) = pack8(u);
-          } else {
-            *(u32x4*)(p.pre + (row * p.N + c) * 2) = pack8(v);
-          }
+          store<kTake>(pre, r, c0, v);
+          if constexpr (GATED) store<kTake>(pre2, r, c0, u);
         }
+        with_activation(p.act, [&](auto act) EPL_INLINE {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          v[i] = activate(p.act, v[i]);
-          if constexpr (GATED) v[i] *= u[i];
-        }
+          for (int j = 0; j < kTake * 8; ++j) {
+            v[j / 8][j % 8] = activate<act>(v[j / 8][j % 8]);
+            if constexpr (GATED) v[j / 8][j % 8] *= u[j / 8][j % 8];
+          }
+        });
         if constexpr (!GATED) {
           if (p.residual) {
-            float r[8];
-            unpack8(*(const u32x4*)(p.residual + row * p.res_ld + c * 2), r);
+            const char* res = p.residual + (t.row0 + std::min(r, t.rows - 1)) * p.res_ld;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += r[i];
+            for (int k = 0; k < kTake; ++k) {
+              float d[8];
+              unpack8(*(const u32x4*)(res + (t.col0 + std::min(c0 + k * 32, cols - 8)) * 2ll), d);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) v[k][i] += d[i];
+            }
           }
         }
-        *(u32x4*)(p.out + row * p.out_ld + c * 2) = pack8(v);
+        store<kTake>(out, r, c0, v);
       }
     }
   }
+  template <int TAKE>
+  static __device__ __forceinline__ void store(const TileOut& o, int r, int c, const float (&v)[TAKE][8]) {
+    if constexpr (TAKE == 2)
+      o.store2(r, c, v[0], v[1]);
+    else
+      o.store(r, c, v[0]);
+  }
+};
+
+template <class S, bool FP8, bool GATED>
+__global__ void __launch_bounds__(S::kThreads) forward_kernel(ForwardArgs p) {
+  __shared__ __attribute__((aligned(1024))) char tiles[S::STAGES * S::stage(FP8)];
+  __shared__ RowTable tab;
+  const int wave = uniform(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+  fill_row_table<S::BM>(p.expert_off, p.E, p.cap, tab);
+  ForwardJob<S, FP8, GATED> job(p, tab, wave, lane);
+  run_tiles<S, false, false, FP8, GATED>(job, lds_addr(tiles), wave, lane);
 }
 
 // ---------------------------------------------------------------- gradient of the rows
 // dx[r] = sum over parts and n of d[r][part * N + n] w_part[e][n]: the reduction runs over the weights' rows.
 template <class S>
-__global__ void __launch_bounds__(S::kThreads) row_grad_kernel(RowGradArgs p) {
-  __shared__ __attribute__((aligned(1024))) char tiles[2 * S::kStage];
-  __shared__ int mt[EPL_MAX_EXPERTS + 1];
-  const int wave = uniform(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-  const int rho = lane & 15, q = lane >> 4;
-  count_row_tiles<S::BM>(p.expert_off, p.E, p.cap, mt);
-  Products<S, false, true, false> prod;
-  prod.init(wave, lane);
-  Operand<false, S::BM, S::kWaves, false> a;
-  Operand<true, S::BN, S::kWaves, true> b;
-  const int nt = (p.K + S::BN - 1) / S::BN;
-  const int64_t total = (int64_t)mt[p.E] * nt;
-  const int part_steps = (p.N + kTileK - 1) / kTileK;
-  const int steps = part_steps * p.parts;
-  const uint32_t lds = lds_addr(tiles);
-  const int64_t lda = (int64_t)p.N * p.parts * 2, ldb = (int64_t)p.K * 2;
-  for (int64_t t = xcd_slot(blockIdx.x, gridDim.x); t < total; t += gridDim.x) {
-    const int e = uniform(quaternary_find(mt, p.E, t / nt));
-    int beg, end, m, n;
-    expert_rows(p.expert_off, e, p.cap, beg, end);
-    beg = uniform(beg);
-    end = uniform(end);
-    const int m0 = uniform(mt[e]);
-    band_tile(t - (int64_t)m0 * nt, uniform(mt[e + 1]) - m0, nt, 8, m, n);
-    const int row0 = beg + m * S::BM, rows = end - row0;
-    const int col0 = n * S::BN, cols = std::min(p.K - col0, S::BN);
-    if (m < 0 || rows <= 0) continue;
-    a.lanes(rows, lda, wave, lane);
-    b.lanes(cols, ldb, wave, lane);
-    const int64_t boff = (e * p.expert_stride + col0) * 2;
-    f32x4 acc[S::MF][S::NF];
-    clear<S>(acc);
-    uint32_t cur = lds, nxt = lds + S::kStage;
-    int at = 0;  // steps loaded
-    auto load = [&](uint32_t stage) {
-      if (at == 0 || at == part_steps) {
-        const int part = at == 0 ? 0 : 1;
-        a.start_rows(p.d + row0 * lda + (int64_t)part * p.N * 2, nullptr, std::min(rows, S::BM), lda, p.N * 2);
-        b.start_cols((part ? p.w2 : p.w) + boff, p.N, cols, ldb);
-      }
-      a.load(stage, wave);
-      b.load(stage + S::BM * kStepBytes, wave);
-      ++at;
-    };
-    wait_tiles();
-    load(cur);
-    for (int s = 0; s < steps; ++s) {
-      wait_tiles();
-      if (s + 1 < steps) load(nxt);
-      prod.step(cur, acc, nullptr);
-      const uint32_t u = cur;
-      cur = nxt;
-      nxt = u;
-    }
-    const int wm0 = (wave / S::WN) * S::MF * 16, wn0 = (wave % S::WN) * S::NF * 16;
-#pragma unroll
-    for (int g = 0; g < S::NF / 2; ++g) {
-      const int c = col0 + wn0 + g * 32 + q * 8;
-      if (c >= p.K) continue;
-#pragma unroll
-      for (int f = 0; f < S::MF; ++f) {
-        const int64_t row = row0 + wm0 + f * 16 + rho;
-        if (row >= end) continue;
-        float v[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = acc[f][g * 2 + i / 4][i % 4];
-        *(u32x4*)(p.dx + row * p.dx_ld + c * 2) = pack8(v);
-      }
-    }
+struct RowGradJob {
+  struct Tile {
+    int64_t t;
+    int e, row0, rows, col0, steps;
+  };
+  const RowGradArgs& p;
+  const RowTable& tab;
+  int wave, lane, nt, part_steps;
+  int64_t total;
+  LanePlace<S> at;
+  __device__ __forceinline__ RowGradJob(const RowGradArgs& p_, const RowTable& tab_, int wave_, int lane_)
+      : p(p_), tab(tab_), wave(wave_), lane(lane_), at(wave_, lane_) {
+    nt = (p.K + S::BN - 1) / S::BN;
+    part_steps = (p.N * 2 + S::STEP - 1) / S::STEP;
+    total = (int64_t)uniform(tab.mt[p.E]) * nt;
   }
+  __device__ __forceinline__ bool place(Tile& t) const {
+    if (t.t >= total) return false;
+    int m, n;
+    t.e = uniform(quaternary_find(tab.mt, p.E, t.t / nt));
+    const int m0 = uniform(tab.mt[t.e]), beg = uniform(tab.off[t.e]), end = uniform(tab.off[t.e + 1]);
+    band_tile(t.t - (int64_t)m0 * nt, uniform(tab.mt[t.e + 1]) - m0, nt, 8, m, n);
+    t.row0 = beg + m * S::BM;
+    t.rows = std::min(end - t.row0, S::BM);
+    t.col0 = n * S::BN;
+    t.steps = S::steps(part_steps * p.parts * S::STEP, false);
+    return true;
+  }
+  __device__ __forceinline__ bool first(Tile& t) const {
+    t.t = xcd_slot(blockIdx.x, gridDim.x);
+    return place(t);
+  }
+  __device__ __forceinline__ bool next(Tile& t) const {
+    t.t += gridDim.x;
+    return place(t);
+  }
+  template <class A, class B>
+  __device__ __forceinline__ void begin(const Tile& t, A& a, B& b) const {
+    a.lanes(t.rows, (int64_t)p.N * p.parts * 2, wave, lane);
+    b.lanes(std::min(p.K - t.col0, S::BN), (int64_t)p.K * 2, wave, lane);
+    start(t, 0, p.w, a, b);
+  }
+  template <class A, class B>
+  __device__ __forceinline__ void start(const Tile& t, int part, const char* w, A& a, B& b) const {
+    const int64_t lda = (int64_t)p.N * p.parts * 2, ldb = (int64_t)p.K * 2;
+    a.start_rows(p.d + t.row0 * lda + (int64_t)part * p.N * 2, nullptr, t.rows, lda, p.N * 2);
+    b.start_cols(w + (t.e * p.expert_stride + t.col0) * 2, p.N, std::min(p.K - t.col0, S::BN), ldb);
+  }
+  // The second part's first step. (An only part's padded step may have that number too.)
+  template <class A, class B>
+  __device__ __forceinline__ void turn(const Tile& t, int step, A& a, B& b) const {
+    if (p.parts == 2 && step == part_steps) start(t, 1, p.w2, a, b);
+  }
+  template <int N>
+  __device__ __forceinline__ void wait(bool stored) const {
+    if (stored)
+      wait_tiles<std::min(63, N + S::NF / 2 * S::MF)>();
+    else
+      wait_tiles<N>();
+  }
+  __device__ __forceinline__ void finish(const Tile& t, f32x4 (&acc)[S::MF][S::NF]) const {
+    const TileOut out(p.dx, t.row0, p.dx_ld, t.col0, t.rows, std::min(p.K - t.col0, S::BN));
+    store_tile<S>(out, at.row, at.col, acc);
+  }
+};
+
+template <class S>
+__global__ void __launch_bounds__(S::kThreads) row_grad_kernel(RowGradArgs p) {
+  __shared__ __attribute__((aligned(1024))) char tiles[S::STAGES * S::stage(false)];
+  __shared__ RowTable tab;
+  const int wave = uniform(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+  fill_row_table<S::BM>(p.expert_off, p.E, p.cap, tab);
+  RowGradJob<S> job(p, tab, wave, lane);
+  run_tiles<S, false, true, false, false>(job, lds_addr(tiles), wave, lane);
 }
 
 // ---------------------------------------------------------------- gradient of the weights
-// dw_part[e][n][k] = sum over the expert's rows r of d[r][part * N + n] x[r][k]: the reduction runs over the rows,
-// which an expert without any leaves at zero.
+// dw_part[e][n][k] = sum over the expert's rows r of d[r][part * N + n] x[r][k]: the reduction runs over the rows. An
+// expert without rows takes one step of zeros.
+template <class S>
+struct WeightGradJob {
+  struct Tile {
+    int64_t t;
+    int e, part, m0, col0, beg, rows, steps;
+  };
+  const WeightGradArgs& p;
+  const RowTable& tab;
+  int wave, lane, mt, nt;
+  LanePlace<S> at;
+  __device__ __forceinline__ WeightGradJob(const WeightGradArgs& p_, const RowTable& tab_, int wave_, int lane_)
+      : p(p_), tab(tab_), wave(wave_), lane(lane_), at(wave_, lane_) {
+    mt = (p.N + S::BM - 1) / S::BM;
+    nt = (p.K + S::BN - 1) / S::BN;
+  }
+  __device__ __forceinline__ bool place(Tile& t) const {
+    const int64_t per = (int64_t)mt * p.parts * nt;
+    if (t.t >= per * p.E) return false;
+    int m, n;
+    t.e = (int)(t.t / per);
+    t.beg = uniform(tab.off[t.e]);
+    t.rows = uniform(tab.off[t.e + 1]) - t.beg;
+    band_tile(t.t - t.e * per, mt * p.parts, nt, 8, m, n);
+    t.part = m >= mt;
+    t.m0 = (t.part ? m - mt : m) * S::BM;
+    t.col0 = n * S::BN;
+    t.steps = S::steps(t.rows * 2, false);
+    return true;
+  }
+  __device__ __forceinline__ bool first(Tile& t) const {
+    t.t = xcd_slot(blockIdx.x, gridDim.x);
+    return place(t);
+  }
+  __device__ __forceinline__ bool next(Tile& t) const {
+    t.t += gridDim.x;
+    return place(t);
+  }
+  template <class A, class B>
+  __device__ __forceinline__ void turn(const Tile&, int, A&, B&) const {}
+  template <class A, class B>
+  __device__ __forceinline__ void begin(const Tile& t, A& a, B& b) const {
+    const int64_t lda = (int64_t)p.N * p.parts * 2;
+    const int m = std::min(p.N - t.m0, S::BM), cols = std::min(p.K - t.col0, S::BN);
+    a.lanes(m, lda, wave, lane);
+    b.lanes(cols, p.x_ld, wave, lane);
+    a.start_cols(p.d + t.beg * lda + ((int64_t)t.part * p.N + t.m0) * 2, t.rows, m, lda);
+    b.start_cols(p.x + t.beg * p.x_ld + t.col0 * 2ll, t.rows, cols, p.x_ld);
+  }
+  template <int N>
+  __device__ __forceinline__ void wait(bool stored) const {
+    if (stored)
+      wait_tiles<std::min(63, N + S::NF / 2 * S::MF)>();
+    else
+      wait_tiles<N>();
+  }
+  __device__ __forceinline__ void finish(const Tile& t, f32x4 (&acc)[S::MF][S::NF]) const {
+    char* dw = (t.part ? p.dw2 : p.dw) + (int64_t)t.e * p.N * p.K * 2;
+    const TileOut out(dw, t.m0, (int64_t)p.K * 2, t.col0, std::min(p.N - t.m0, S::BM), std::min(p.K - t.col0, S::BN));
+    store_tile<S>(out, at.row, at.col, acc);
+  }
+};
+
 template <class S>
 __global__ void __launch_bounds__(S::kThreads) weight_grad_kernel(WeightGradArgs p) {
-  __shared__ __attribute__((aligned(1024))) char tiles[2 * S::kStage];
+  __shared__ __attribute__((aligned(1024))) char tiles[S::STAGES * S::stage(false)];
+  __shared__ RowTable tab;
   const int wave = uniform(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-  const int rho = lane & 15, q = lane >> 4;
-  Products<S, true, true, false> prod;
-  prod.init(wave, lane);
-  Operand<true, S::BM, S::kWaves, false> a;
-  Operand<true, S::BN, S::kWaves, true> b;
-  const int mt = (p.N + S::BM - 1) / S::BM * p.parts, nt = (p.K + S::BN - 1) / S::BN;
-  const int64_t per = (int64_t)mt * nt;
-  const int64_t total = per * p.E;
-  const uint32_t lds = lds_addr(tiles);
-  const int64_t lda = (int64_t)p.N * p.parts * 2;
-  for (int64_t t = xcd_slot(blockIdx.x, gridDim.x); t < total; t += gridDim.x) {
-    const int e = uniform((int)(t / per));
-    int beg, end, mi, n;
-    expert_rows(p.expert_off, e, p.cap, beg, end);
-    beg = uniform(beg);
-    end = uniform(end);
-    band_tile(t - e * per, mt, nt, 8, mi, n);
-    const int part = mi / (mt / p.parts), m0 = (mi % (mt / p.parts)) * S::BM;
-    const int mrows = std::min(p.N - m0, S::BM);
-    const int col0 = n * S::BN, cols = std::min(p.K - col0, S::BN);
-    a.lanes(mrows, lda, wave, lane);
-    b.lanes(cols, p.x_ld, wave, lane);
-    a.start_cols(p.d + beg * lda + ((int64_t)part * p.N + m0) * 2, end - beg, mrows, lda);
-    b.start_cols(p.x + beg * p.x_ld + col0 * 2, end - beg, cols, p.x_ld);
-    f32x4 acc[S::MF][S::NF];
-    clear<S>(acc);
-    const int steps = (end - beg + kTileK - 1) / kTileK;
-    wait_tiles();
-    if (steps > 0) run_steps<S>(prod, a, b, steps, lds, wave, acc);
-    char* dw = (part ? p.dw2 : p.dw) + (int64_t)e * p.N * p.K * 2;
-    const int wm0 = (wave / S::WN) * S::MF * 16, wn0 = (wave % S::WN) * S::NF * 16;
-#pragma unroll
-    for (int g = 0; g < S::NF / 2; ++g) {
-      const int c = col0 + wn0 + g * 32 + q * 8;
-      if (c >= p.K) continue;
-#pragma unroll
-      for (int f = 0; f < S::MF; ++f) {
-        const int r = m0 + wm0 + f * 16 + rho;
-        if (r >= p.N) continue;
-        float v[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = acc[f][g * 2 + i / 4][i % 4];
-        *(u32x4*)(dw + ((int64_t)r * p.K + c) * 2) = pack8(v);
-      }
-    }
-  }
+  fill_row_table<0>(p.expert_off, p.E, p.cap, tab);
+  WeightGradJob<S> job(p, tab, wave, lane);
+  run_tiles<S, true, true, false, false>(job, lds_addr(tiles), wave, lane);
 }
 
 // ---------------------------------------------------------------- gradients through the activation
@@ -325,12 +390,14 @@ __global__ void __launch_bounds__(256) gated_pre_grad_kernel(const char* dh, con
     unpack8(((const u32x4*)dh)[i], d);
     unpack8(((const u32x4*)pre)[r * 2 * nv + c], g);
     unpack8(((const u32x4*)pre)[r * 2 * nv + nv + c], u);
+    with_activation(act, [&](auto act_) EPL_INLINE {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float a = activate(act, g[j]), ag = activate_grad(act, g[j]);
-      g[j] = d[j] * u[j] * ag;
-      u[j] = d[j] * a;
-    }
+      for (int j = 0; j < 8; ++j) {
+        const float a = activate<act_>(g[j]), ag = activate_grad<act_>(g[j]);
+        g[j] = d[j] * u[j] * ag;
+        u[j] = d[j] * a;
+      }
+    });
     ((u32x4*)dpre)[r * 2 * nv + c] = pack8(g);
     ((u32x4*)dpre)[r * 2 * nv + nv + c] = pack8(u);
   }
@@ -344,48 +411,69 @@ __global__ void __launch_bounds__(256) pre_grad_kernel(const char* dy, const cha
     float d[8], v[8];
     unpack8(((const u32x4*)dy)[i], d);
     unpack8(((const u32x4*)pre)[i], v);
+    with_activation(act, [&](auto act_) EPL_INLINE {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) d[j] *= activate_grad(act, v[j]);
+      for (int j = 0; j < 8; ++j) d[j] *= activate_grad<act_>(v[j]);
+    });
     ((u32x4*)dpre)[i] = pack8(d);
   }
 }
 
-// dbias[e][n] = sum over the expert's rows of dy act'(pre), unrounded terms summed in fp32 in a fixed order:
-// 8 row lanes of a workgroup take every eighth row of 256 columns, then are added in order.
-__global__ void __launch_bounds__(256) bias_grad_kernel(const char* dy, const char* pre, char* dbias,
-                                                        const int32_t* expert_off, int cap, int N, int act) {
-  __shared__ float part[8][32][8 + 1];
-  const int e = blockIdx.y, cv = threadIdx.x % 32, rl = threadIdx.x / 32;
-  const int c = blockIdx.x * 32 + cv;  // 8-column vector
-  int beg, end;
-  expert_rows(expert_off, e, cap, beg, end);
+// The same with dbias[e][n] = the sum of the unrounded dpre over the expert's rows, in one pass over dy and pre (without
+// an activation there is no dpre to write). A workgroup takes 64 columns of one expert: 8 lanes of 8 columns, 32 row
+// lanes that take every 32nd row, two at a time; fp32 sums, added over the row lanes in order.
+__global__ void __launch_bounds__(256) pre_bias_grad_kernel(const char* dy, const char* pre, char* dpre, char* dbias,
+                                                            const int32_t* expert_off, int cap, int N, int act) {
+  constexpr int kLanes = 32;
+  __shared__ float part[kLanes][8][8 + 1];
+  const int cv = threadIdx.x % 8, rl = threadIdx.x / 8;
+  const int ntiles = (N + 63) / 64;
+  const int e = blockIdx.x / ntiles, c = (blockIdx.x - e * ntiles) * 64 + cv * 8;
+  const int beg = std::min(std::max(expert_off[e], 0), cap);
+  const int end = std::min(std::max(expert_off[e + 1], beg), cap);
   float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-  if (c * 8 < N) {
-    for (int64_t r = beg + rl; r < end; r += 8) {
-      float d[8], v[8];
-      unpack8(*(const u32x4*)(dy + (r * N + c * 8) * 2), d);
-      if (act != EPL_ACT_NONE) {
-        unpack8(*(const u32x4*)(pre + (r * N + c * 8) * 2), v);
+  if (c < N) {
+    for (int64_t r0 = beg + rl; r0 < end; r0 += 2 * kLanes) {
+      u32x4 dw[2], vw[2];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) d[j] *= activate_grad(act, v[j]);
+      for (int k = 0; k < 2; ++k) {
+        const int64_t at = (std::min<int64_t>(r0 + k * kLanes, end - 1) * N + c) * 2;
+        dw[k] = *(const u32x4*)(dy + at);
+        if (act != EPL_ACT_NONE) vw[k] = *(const u32x4*)(pre + at);
       }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) s[j] += d[j];
+      for (int k = 0; k < 2; ++k) {
+        const int64_t r = r0 + k * kLanes;
+        if (r >= end) continue;
+        float d[8], v[8];
+        unpack8(dw[k], d);
+        if (act != EPL_ACT_NONE) {
+          unpack8(vw[k], v);
+          with_activation(act, [&](auto act_) EPL_INLINE {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) d[j] *= activate_grad<act_>(v[j]);
+          });
+          *(u32x4*)(dpre + (r * N + c) * 2) = pack8(d);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[j] += d[j];
+      }
     }
   }
 #pragma unroll
   for (int j = 0; j < 8; ++j) part[rl][cv][j] = s[j];
   __syncthreads();
-  if (rl == 0 && c * 8 < N) {
-    for (int k = 1; k < 8; ++k)
+  if (rl == 0 && c < N) {
+    for (int k = 1; k < kLanes; ++k)
 #pragma unroll
       for (int j = 0; j < 8; ++j) s[j] += part[k][cv][j];
-    *(u32x4*)(dbias + ((int64_t)e * N + c * 8) * 2) = pack8(s);
+    *(u32x4*)(dbias + ((int64_t)e * N + c) * 2) = pack8(s);
   }
 }
 
 // ---------------------------------------------------------------- launches
-using Mid = Shape<128, 128, 2, 2>;
+using Big = Shape<256, 256, 2, 4, 128, 2>;
+using Mid = Shape<128, 256, 2, 4, 128, 3>;
 
 static unsigned persistent_grid(int64_t tiles, int per_cu) {
   return (unsigned)std::min<int64_t>(tiles, (int64_t)kCus * per_cu);
@@ -398,14 +486,17 @@ template <class S, bool FP8, bool GATED>
 static hipError_t forward_as(const ForwardArgs& p, hipStream_t stream) {
   const int cols = GATED ? S::BN / 2 : S::BN;
   const int64_t tiles = row_tiles(p.cap, p.E, S::BM) * ((p.N + cols - 1) / cols);
-  hipLaunchKernelGGL((forward_kernel<S, FP8, GATED>), dim3(persistent_grid(tiles, 2)), dim3(S::kThreads), 0, stream,
+  hipLaunchKernelGGL((forward_kernel<S, FP8, GATED>), dim3(persistent_grid(tiles, 1)), dim3(S::kThreads), 0, stream,
                      p);
   return hipGetLastError();
 }
 
 hipError_t launch_forward(const ForwardArgs& p, bool fp8, bool gated, hipStream_t stream) {
   if (p.cap == 0) return hipSuccess;
+  if (few_rows(p.cap, p.E, fp8)) return launch_forward_few(p, fp8, gated, stream);
   if (fp8) return gated ? forward_as<Mid, true, true>(p, stream) : forward_as<Mid, true, false>(p, stream);
+  if (many_rows(p.cap, p.E))
+    return gated ? forward_as<Big, false, true>(p, stream) : forward_as<Big, false, false>(p, stream);
   return gated ? forward_as<Mid, false, true>(p, stream) : forward_as<Mid, false, false>(p, stream);
 }
 
@@ -413,7 +504,7 @@ hipError_t launch_row_grad(const RowGradArgs& p, hipStream_t stream) {
   if (p.cap == 0) return hipSuccess;
   using S = Mid;
   const int64_t tiles = row_tiles(p.cap, p.E, S::BM) * ((p.K + S::BN - 1) / S::BN);
-  hipLaunchKernelGGL((row_grad_kernel<S>), dim3(persistent_grid(tiles, 2)), dim3(S::kThreads), 0, stream, p);
+  hipLaunchKernelGGL((row_grad_kernel<S>), dim3(persistent_grid(tiles, 1)), dim3(S::kThreads), 0, stream, p);
   return hipGetLastError();
 }
 
@@ -421,7 +512,7 @@ hipError_t launch_weight_grad(const WeightGradArgs& p, hipStream_t stream) {
   using S = Mid;
   const int64_t tiles =
       (int64_t)p.E * p.parts * ((p.N + S::BM - 1) / S::BM) * ((p.K + S::BN - 1) / S::BN);
-  hipLaunchKernelGGL((weight_grad_kernel<S>), dim3(persistent_grid(tiles, 2)), dim3(S::kThreads), 0, stream, p);
+  hipLaunchKernelGGL((weight_grad_kernel<S>), dim3(persistent_grid(tiles, 1)), dim3(S::kThreads), 0, stream, p);
   return hipGetLastError();
 }
 
@@ -437,18 +528,14 @@ hipError_t launch_gated_pre_grad(const void* dh, const void* pre, void* dpre, co
   return hipGetLastError();
 }
 
-hipError_t launch_pre_grad(const void* dy, const void* pre, void* dpre, const int32_t* expert_off, int E, int cap,
-                           int N, int act, hipStream_t stream) {
-  if (cap == 0) return hipSuccess;
-  hipLaunchKernelGGL(pre_grad_kernel, dim3(elementwise_grid((int64_t)cap * (N / 8))), dim3(256), 0, stream,
-                     (const char*)dy, (const char*)pre, (char*)dpre, expert_off, E, cap, N, act);
-  return hipGetLastError();
-}
-
-hipError_t launch_bias_grad(const void* dy, const void* pre, void* dbias, const int32_t* expert_off, int E, int cap,
-                            int N, int act, hipStream_t stream) {
-  hipLaunchKernelGGL(bias_grad_kernel, dim3((unsigned)((N + 255) / 256), (unsigned)E), dim3(256), 0, stream,
-                     (const char*)dy, (const char*)pre, (char*)dbias, expert_off, cap, N, act);
+hipError_t launch_pre_grad(const void* dy, const void* pre, void* dpre, void* dbias, const int32_t* expert_off, int E,
+                           int cap, int N, int act, hipStream_t stream) {
+  if (dbias)
+    hipLaunchKernelGGL(pre_bias_grad_kernel, dim3((unsigned)((N + 63) / 64 * E)), dim3(256), 0, stream, (const char*)dy,
+                       (const char*)pre, (char*)dpre, (char*)dbias, expert_off, cap, N, act);
+  else if (act != EPL_ACT_NONE && cap > 0)
+    hipLaunchKernelGGL(pre_grad_kernel, dim3(elementwise_grid((int64_t)cap * (N / 8))), dim3(256), 0, stream,
+                       (const char*)dy, (const char*)pre, (char*)dpre, expert_off, E, cap, N, act);
   return hipGetLastError();
 }
 

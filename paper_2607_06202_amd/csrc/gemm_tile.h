@@ -1,10 +1,9 @@
 // Matrix-instruction tile shared by the experts' products (device only).
 //
 // A workgroup computes a BM x BN tile of D = A * B^T with 64-wide waves in a WM x WN arrangement. Both
-// operands pass through LDS in steps of 128 bytes of the reduction (64 bf16 or 128 E4M3 elements), and each may
-// be stored either way round in memory:
-//   * reduction-contiguous ("rows"): LDS holds [rows][128 bytes]; a lane reads 16 bytes of its row;
-//   * reduction-major ("columns"):   LDS holds [64 reduction rows][columns]; a lane reads two 4x16 blocks that
+// operands pass through LDS in steps of 64 or 128 bytes of the reduction (32 or 64 bf16, 128 E4M3 elements), and each may be stored either way round in memory:
+//   * reduction-contiguous ("rows"): LDS holds [rows][step bytes]; a lane reads 16 bytes of its row;
+//   * reduction-major ("columns"):   LDS holds [reduction rows][columns]; a lane reads two 4x16 blocks that
 //     the transposing LDS read turns to its own column (ds_read_b64_tr_b16).
 // Either way a lane ends up with the same eight reduction elements of one row, so the two mix freely: forward
 // (rows x rows), input gradient (rows x columns) and weight gradient (columns x columns) are one loop.
@@ -19,6 +18,8 @@
 // give eight: one 16-byte bf16 store per lane.
 #pragma once
 
+#include <type_traits>
+
 #include "epl_internal.h"
 
 namespace epl {
@@ -29,8 +30,9 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
-constexpr int kStepBytes = 128;       // reduction bytes of a row per step
-constexpr int kTileK = 64;            // bf16 reduction elements per step
+// Lambdas over register arrays: out of line they would put the arrays in memory.
+#define EPL_INLINE __attribute__((always_inline))
+
 constexpr int kOutOfRange = INT_MIN;  // as an unsigned offset, past every descriptor below 2 GiB
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
@@ -47,7 +49,7 @@ __device__ __forceinline__ u32x4 make_rsrc(uint64_t base, int64_t bytes) {
 }
 
 // 64 lanes x 16 bytes from the descriptor to consecutive LDS bytes at lds. Outside the compiler's view of
-// outstanding loads: wait_tiles() is what waits for it. (The builtin makes the compiler wait for every such load
+// outstanding loads: wait_tiles is what waits for it. (The builtin makes the compiler wait for every such load
 // before any LDS read, which would end the overlap of a step's loads with the previous step's products.)
 __device__ __forceinline__ void load_to_lds(u32x4 rsrc, uint32_t lds, int voff) {
   asm volatile(
@@ -58,18 +60,27 @@ __device__ __forceinline__ void load_to_lds(u32x4 rsrc, uint32_t lds, int voff) 
       : "memory");
 }
 
-// All of this wave's loads have landed and its LDS reads are done; then every wave of the workgroup is here.
-__device__ __forceinline__ void wait_tiles() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// 64 lanes x 4 bytes, the same way.
+__device__ __forceinline__ void load_words_to_lds(u32x4 rsrc, uint32_t lds, int voff) {
+  asm volatile(
+      "s_mov_b32 m0, %0\n\t"
+      "s_nop 0\n\t"
+      "buffer_load_dword %1, %2, 0 offen lds" ::"s"(uniform((int)lds)),
+      "v"(voff), "s"(rsrc)
+      : "memory");
+}
 
 // One operand's stream of steps. Wave-uniform except the lane's offsets.
 //   COLS: reduction-major in memory (reduction rows ld bytes apart, columns contiguous);
-//   ROWS: rows (columns) of the tile; NW waves share its loads; B: the B operand's swizzle key.
+//   ROWS: rows (columns) of the tile; NW waves share its loads; STEP: reduction bytes of a row per step; B: the B
+//   operand's swizzle key.
 // A second base serves a tile whose second half of rows comes from another matrix (gate and up projections).
-template <bool COLS, int ROWS, int NW, bool B, bool SPLIT = false>
+template <bool COLS, int ROWS, int NW, int STEP, bool B, bool SPLIT = false>
 struct Operand {
-  static constexpr int kLoads = ROWS * kStepBytes / 1024 / NW;  // per wave and step
-  static_assert(kLoads >= 1 && kLoads * NW * 1024 == ROWS * kStepBytes, "tile not a whole number of loads");
-  static constexpr int kBytes = ROWS * kStepBytes;
+  static constexpr int kBytes = ROWS * STEP;
+  static constexpr int kLoads = kBytes / 1024 / NW;  // per wave and step
+  static_assert(kLoads >= 1 && kLoads * NW * 1024 == kBytes, "tile not a whole number of loads");
+  static constexpr int kRowsPerLoad = 1024 / STEP, kSlots = STEP / 16;
 
   uint64_t base, base2;
   int64_t bytes;
@@ -78,34 +89,39 @@ struct Operand {
   int voff[kLoads];
   int piece[2];  // rows: byte offset of the lane's piece, for even and odd loads
 
-  // rows: `n` valid rows ld bytes apart, kbytes reduction bytes. columns: `n` valid columns (of 2 bytes),
-  // reduction rows ld bytes apart.
+  // The slot of a row's piece c is c ^ key(row), so that the rows that lanes read together meet different banks.
+  static __device__ __forceinline__ int key(int row) {
+    if constexpr (STEP == 64)
+      return B ? ((row >> 1) & 1) | ((row >> 2) & 2) : (row >> 1) & 3;
+    else
+      return B ? (row & 3) | ((row >> 1) & 4) : row & 7;
+  }
+  // rows: `n` valid rows ld bytes apart. columns: `n` valid columns (of 2 bytes), reduction rows ld bytes apart.
   __device__ __forceinline__ void lanes(int n, int64_t ld, int wave, int lane) {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int ii = wave * kLoads + i;
       if constexpr (!COLS) {
-        const int r8 = lane >> 3;
-        const int key = B ? (r8 & 3) | ((ii & 1) << 2) : r8;
-        int row = ii * 8 + r8;
-        const int pc = ((lane & 7) ^ key) * 16;
+        int row = ii * kRowsPerLoad + lane / kSlots;
+        const int pc = ((lane % kSlots) ^ key(row)) * 16;
         piece[i & 1] = pc;
         if constexpr (SPLIT) row = row >= ROWS / 2 ? row - ROWS / 2 : row;
-        voff[i] = row < n ? (int)(row * ld) + pc : kOutOfRange;
+        voff[i] = row < n ? row * (int)ld + pc : kOutOfRange;
       } else {
         constexpr int kPer = ROWS / 8;  // 16-byte pieces per reduction row
         const int p = ii * 64 + lane;
         const int kr = p / kPer, slot = p % kPer;
         const int c = slot ^ ((kr & 3) * (B ? 4 : 2));
-        voff[i] = c * 8 < n ? (int)(kr * ld) + c * 16 : kOutOfRange;
+        voff[i] = c * 8 < n ? kr * (int)ld + c * 16 : kOutOfRange;
       }
     }
   }
+  // n rows of kbytes reduction bytes
   __device__ __forceinline__ void start_rows(const void* p, const void* p2, int n, int64_t ld, int kbytes) {
     base = (uint64_t)p;
     base2 = (uint64_t)p2;
     bytes = n <= 0 ? 0 : (n - 1) * ld + kbytes;
-    step = kStepBytes;
+    step = STEP;
     left = kbytes;
   }
   // k reduction rows, n columns
@@ -113,164 +129,370 @@ struct Operand {
     base = (uint64_t)p;
     base2 = 0;
     bytes = k <= 0 ? 0 : (k - 1) * ld + n * 2;
-    step = kTileK * ld;
+    step = STEP / 2 * ld;
     left = 0;
   }
-  // Issue the loads of the next step into the tile at lds and move on.
+  // Load I of the next step into the tile at lds; the last one moves on to the step after.
+  template <int I>
   __device__ __forceinline__ void load(uint32_t lds, int wave) {
-    const u32x4 r = make_rsrc(base, bytes);
-    u32x4 r2 = r;
-    if constexpr (SPLIT) r2 = make_rsrc(base2, bytes);
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      int v = voff[i];
-      if constexpr (!COLS) v = piece[i & 1] < left ? v : kOutOfRange;
-      const bool second = SPLIT && wave * kLoads + i >= ROWS / 16;
-      load_to_lds(second ? r2 : r, lds + (wave * kLoads + i) * 1024, v);
+    int v = voff[I];
+    if constexpr (!COLS) v = piece[I & 1] < left ? v : kOutOfRange;
+    const bool second = SPLIT && wave * kLoads + I >= kBytes / 2048;
+    load_to_lds(make_rsrc(second ? base2 : base, bytes), lds + (wave * kLoads + I) * 1024, v);
+    if constexpr (I == kLoads - 1) {
+      base += step;
+      if constexpr (SPLIT) base2 += step;
+      bytes -= step;
+      left -= STEP;
     }
-    base += step;
-    if constexpr (SPLIT) base2 += step;
-    bytes -= step;
-    left -= kStepBytes;
   }
 };
 
-// Eight reduction elements (bf16) of fragment rows from LDS. `rho` = lane % 16, `q` = lane / 16.
-// rows: address of the lane's row at piece q ^ (rho & 7); the second half of the step is 64 bytes away by XOR.
+// Sixteen bytes of a lane's row, and eight elements of a lane's column (two transposing reads, the second four
+// reduction rows on), from LDS. Addresses come in registers that the compiler cannot see through plus constants, so
+// that the constants become the instructions' offsets.
+template <int OFFSET>
 __device__ __forceinline__ i32x4 read_rows(uint32_t addr) {
-  return *(const __attribute__((address_space(3))) i32x4*)(uintptr_t)addr;
+  return *(const __attribute__((address_space(3))) i32x4*)(uintptr_t)(addr + OFFSET);
 }
-__device__ __forceinline__ i32x4 read_cols(uint32_t addr, int row_bytes) {
-  const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(uintptr_t)addr);
-  const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-      (__attribute__((address_space(3))) s16x4*)(uintptr_t)(addr + 4 * row_bytes));
+template <int OFFSET, int ROW_BYTES>
+__device__ __forceinline__ i32x4 read_cols(uint32_t addr) {
   typedef int i32x2 __attribute__((ext_vector_type(2)));
-  const i32x2 a = __builtin_bit_cast(i32x2, lo), b = __builtin_bit_cast(i32x2, hi);
+  using Ptr = __attribute__((address_space(3))) s16x4*;
+  const i32x2 a = __builtin_bit_cast(i32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)(uintptr_t)(addr + OFFSET)));
+  const i32x2 b = __builtin_bit_cast(
+      i32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)(uintptr_t)(addr + OFFSET + 4 * ROW_BYTES)));
   return i32x4{a[0], a[1], b[0], b[1]};
 }
 
-// BM x BN tile by WM x WN waves. MF x NF fragments of 16 x 16 per wave.
-template <int BM_, int BN_, int WM_, int WN_>
+// BM x BN tile by WM x WN waves. MF x NF fragments of 16 x 16 per wave. STEP: reduction bytes of a row per step (64 or
+// 128; 128 for fp8); STAGES: steps that LDS holds.
+template <int BM_, int BN_, int WM_, int WN_, int STEP_, int STAGES_>
 struct Shape {
-  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STEP = STEP_, STAGES = STAGES_;
   static constexpr int kWaves = WM * WN, kThreads = kWaves * kWave;
   static constexpr int MF = BM / WM / 16, NF = BN / WN / 16;
-  static constexpr int kStage = (BM + BN) * kStepBytes;
+  // A tile, B tile and (fp8) the scales of A's rows.
+  static constexpr int stage(bool fp8) { return (BM + BN) * STEP + (fp8 ? 1024 : 0); }
   static_assert(NF % 2 == 0, "fragments of B come in pairs");
+  // Steps of a tile with n bytes of reduction: at least what LDS holds, and even where a step is one set of groups.
+  __host__ __device__ static constexpr int steps(int n, bool fp8) {
+    const int s = std::max((n + STEP - 1) / STEP, STAGES);
+    return fp8 || STEP == 64 ? (s + 1) & ~1 : s;
+  }
 };
 
-// Fragment addresses of one wave inside a stage (A tile first, then B), and the products of one step.
+// Compile-time loop: f(integral_constant<int, I>) for I = 0 .. N-1, so that offsets are constants.
+template <int I, int N, class F>
+__device__ __forceinline__ void static_for(F&& f) {
+  if constexpr (I < N) {
+    f(std::integral_constant<int, I>{});
+    static_for<I + 1, N>(f);
+  }
+}
+
+// Fragments of one wave inside a stage (A tile first, then B).
 //   SPLIT: the B tile's first half of rows are gate rows and its second half up rows; a wave takes the same
 //   columns of both: fragments 0..NF/2-1 are gate, the rest up.
-template <class S, bool ACOLS, bool BCOLS, bool FP8, bool SPLIT = false>
-struct Products {
-  uint32_t a[ACOLS ? 4 : 1];
-  uint32_t b[BCOLS ? (S::NF >= 4 ? 2 : 1) : 1];
+template <class S, bool ACOLS, bool BCOLS, bool SPLIT>
+struct Fragments {
+  static constexpr int kStep = S::STEP, kPieces = kStep / 64;  // 16-byte pieces of a lane's row
+  static constexpr int kA = ACOLS ? 4 : kPieces, kB = BCOLS ? S::NF / 2 : kPieces;
+  uint32_t a[kA], b[kB];    // offsets in a stage
+  uint32_t ra[kA], rb[kB];  // addresses in the stage being read
+  static_assert(!BCOLS || (S::BN >= 128 && !SPLIT), "column swizzle of B");
+  static_assert(!ACOLS || (S::MF >= 4 && S::BM >= 64), "column swizzle of A");
+
   __device__ __forceinline__ void init(int wave, int lane) {
     const int rho = lane & 15, q = lane >> 4;
-    const int wm = wave / S::WN, wn = wave % S::WN;
-    const int m0 = wm * S::MF * 16;
-    if constexpr (!ACOLS) {
-      a[0] = (m0 + rho) * kStepBytes + ((q ^ (rho & 7)) * 16);
-    } else {
-      const int kr = q * 8 + (rho >> 2);
+    const int m0 = (wave / S::WN) * S::MF * 16;
+    const int n0 = (wave % S::WN) * S::NF * 16 / (SPLIT ? 2 : 1);
+    const int kr = q * 8 + (rho >> 2);
+    const uint32_t bt = S::BM * kStep;
+    const int key = kStep == 128 ? rho & 7 : (rho >> 1) & 3;  // the key of the rows this lane reads, in both operands
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < kA; ++i) {
+      if constexpr (!ACOLS)
+        a[i] = (m0 + rho) * kStep + (((q + 4 * i) ^ key) * 16);
+      else
         a[i] = kr * S::BM * 2 + (((m0 / 8 + i * 2 + ((rho & 3) >> 1)) ^ ((rho >> 2) * 2)) * 16) + (rho & 1) * 8;
     }
-    const int n0 = wn * S::NF * 16 / (SPLIT ? 2 : 1);
-    const uint32_t bt = S::BM * kStepBytes;
-    if constexpr (!BCOLS) {
-      b[0] = bt + (n0 + (rho >> 2) * 8 + (rho & 3)) * kStepBytes + ((q ^ (rho & 7)) * 16);
-    } else {
-      const int kr = q * 8 + (rho >> 2);
 #pragma unroll
-      for (int i = 0; i < (S::NF >= 4 ? 2 : 1); ++i)
+    for (int i = 0; i < kB; ++i) {
+      if constexpr (!BCOLS)
+        b[i] = bt + (n0 + (rho >> 2) * 8 + (rho & 3)) * kStep + (((q + 4 * i) ^ key) * 16);
+      else
         b[i] = bt + kr * S::BN * 2 + (((n0 / 8 + i * 4 + (rho & 3)) ^ ((rho >> 2) * 4)) * 16);
     }
   }
-  __device__ __forceinline__ i32x4 a_frag(uint32_t stage, int mf, int kk) const {
-    if constexpr (!ACOLS)
-      return read_rows(stage + (a[0] ^ (kk * 64)) + mf * 16 * kStepBytes);
-    else  // four fragments are 128 bytes; further ones repeat the pattern
-      return read_cols(stage + a[mf & 3] + (mf >> 2) * 128 + kk * 32 * S::BM * 2, S::BM * 2);
-  }
-  __device__ __forceinline__ i32x4 b_frag(uint32_t stage, int nf, int kk) const {
-    const int half = SPLIT ? nf / (S::NF / 2) : 0;
-    const int f = SPLIT ? nf % (S::NF / 2) : nf;
-    if constexpr (!BCOLS)
-      return read_rows(stage + (b[0] ^ (kk * 64)) + ((f >> 1) * 32 + (f & 1) * 4 + half * (S::BN / 2)) * kStepBytes);
-    else
-      return read_cols(stage + b[(f >> 1) & 1] + (f >> 2) * 128 + (f & 1) * 8 + kk * 32 * S::BN * 2, S::BN * 2);
-  }
-  __device__ __forceinline__ void step(uint32_t stage, f32x4 (&acc)[S::MF][S::NF], const float* row_scale) const {
-    if constexpr (!FP8) {
+  __device__ __forceinline__ void stage(uint32_t lds) {
 #pragma unroll
-      for (int kk = 0; kk < 2; ++kk) {
-        i32x4 fb[S::NF];
-#pragma unroll
-        for (int n = 0; n < S::NF; ++n) fb[n] = b_frag(stage, n, kk);
-#pragma unroll
-        for (int m = 0; m < S::MF; ++m) {
-          const bf16x8 fa = __builtin_bit_cast(bf16x8, a_frag(stage, m, kk));
-#pragma unroll
-          for (int n = 0; n < S::NF; ++n)
-            acc[m][n] =
-                __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fb[n]), fa, acc[m][n], 0, 0, 0);
-        }
-      }
-    } else {
-      // The step is one 128-element block of the row's scale: the block's product starts at zero and joins the
-      // sum scaled, in 32 bits. The instruction's own block scales stay at one (exponent 127).
-      i32x8 fb[S::NF];
-#pragma unroll
-      for (int n = 0; n < S::NF; ++n) {
-        const i32x4 lo = b_frag(stage, n, 0), hi = b_frag(stage, n, 1);
-        fb[n] = i32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-      }
-#pragma unroll
-      for (int m = 0; m < S::MF; ++m) {
-        const i32x4 lo = a_frag(stage, m, 0), hi = a_frag(stage, m, 1);
-        const i32x8 fa = i32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-#pragma unroll
-        for (int n = 0; n < S::NF; ++n) {
-          const f32x4 p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[n], fa, f32x4{0, 0, 0, 0}, 0, 0, 0,
-                                                                           0x7f7f7f7f, 0, 0x7f7f7f7f);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) acc[m][n][i] = fmaf(row_scale[m], p[i], acc[m][n][i]);
-        }
-      }
+    for (int i = 0; i < kA; ++i) {
+      ra[i] = lds + a[i];
+      asm volatile("" : "+v"(ra[i]));
     }
+#pragma unroll
+    for (int i = 0; i < kB; ++i) {
+      rb[i] = lds + b[i];
+      asm volatile("" : "+v"(rb[i]));
+    }
+  }
+  // Piece H (the step's H-th 64 bytes) of row fragment M / column fragment N.
+  template <int M, int H>
+  __device__ __forceinline__ i32x4 read_a() const {
+    if constexpr (!ACOLS)
+      return read_rows<M * 16 * kStep>(ra[H]);
+    else
+      return read_cols<(M >> 2) * 128 + H * 32 * S::BM * 2, S::BM * 2>(ra[M & 3]);
+  }
+  template <int N, int H>
+  __device__ __forceinline__ i32x4 read_b() const {
+    constexpr int half = SPLIT ? N / (S::NF / 2) : 0, f = SPLIT ? N % (S::NF / 2) : N;
+    if constexpr (!BCOLS)
+      return read_rows<((f >> 1) * 32 + (f & 1) * 4 + half * (S::BN / 2)) * kStep>(rb[H]);
+    else
+      return read_cols<(f & 1) * 8 + H * 32 * S::BN * 2, S::BN * 2>(rb[f >> 1]);
   }
 };
 
-// ---------------------------------------------------------------- tiles over the experts' rows
-// Rows [beg, end) of expert e in the packed buffer. The offsets are clipped to the buffer, so that whatever they
-// hold, no access leaves it.
-__device__ __forceinline__ void expert_rows(const int32_t* expert_off, int e, int cap, int& beg, int& end) {
-  beg = std::min(std::max(expert_off[e], 0), cap);
-  end = std::min(std::max(expert_off[e + 1], beg), cap);
+// The wave's loads but the last N have landed and its LDS reads are done; then every wave of the workgroup is here.
+template <int N>
+__device__ __forceinline__ void wait_tiles() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-// mt[e] = row tiles of the experts before e, in LDS; returns after a barrier.
+// Makes the compiler wait for a loaded value here, if it still has to.
+template <class T>
+__device__ __forceinline__ void arrived(T& v) {
+  asm volatile("" : "+v"(v));
+}
+
+// ---------------------------------------------------------------- a workgroup's tiles
+// `Job` provides
+//   Tile, first(t), next(t)       the workgroup's tiles in order (false: no more); t.steps from Shape::steps (a step past the
+//                                 operands' ends multiplies zeros);
+//   begin(t, a, b)                sets the operands up for step 0 of tile t;
+//   turn(t, step, a, b)           the same for a later step at which a source changes;
+//   load_scales(t, step, lds)     fp8: one load per wave that brings the step's row scales to lds;
+//   finish(t, acc)                the end of a tile: a known number of buffer stores per wave, whatever is masked;
+//   wait<N>(stored)               wait_tiles<N>, or with the number of stores added.
+//
+// A step is a group of NF products for each row fragment and (bf16) 64 bytes of the reduction. The row fragment of a
+// group is read kAhead groups before it, into a ring of four, across the end of the step too: the barrier between
+// steps comes when the last kAhead groups' operands are in registers, so the matrix unit has their work while the
+// waves meet and the first reads of the next stage return. At that point every wave has read this stage, and the
+// loads of the step that takes its place are issued: they have STAGES - 1 steps to land. Each read and load stands
+// behind a product: a wave issues in order, and eight waves that all read at once fill the queue of LDS and hold up
+// what stands behind their reads. Scheduling barriers keep that order: left to itself the compiler reads each fragment
+// right before its products and waits out the latency of LDS every time. The steps in the middle of a tile run without a
+// branch, and the last STAGES steps, which load nothing, are written out: a taken branch refetches instructions, which
+// costs as much as several products.
+//
+// The next tile's first steps are loaded before this one's results are worked out and stored. Loads and stores leave
+// one in-order counter, so the first steps of a tile wait for all but the stores behind their loads.
+template <class S, bool ACOLS, bool BCOLS, bool FP8, bool SPLIT, class Job>
+__device__ __forceinline__ void run_tiles(Job& job, uint32_t lds, int wave, int lane) {
+  constexpr int kStage = S::stage(FP8);
+  using A = Operand<ACOLS, S::BM, S::kWaves, S::STEP, false>;
+  using B = Operand<BCOLS, S::BN, S::kWaves, S::STEP, true, SPLIT>;
+  using Frag = std::conditional_t<FP8, i32x8, i32x4>;
+  constexpr int kHalves = FP8 ? 1 : S::STEP / 64;
+  constexpr int kGroups = kHalves * S::MF, kRing = 4, kAhead = 3, kTail = kGroups - kAhead;
+  constexpr int kLoads = A::kLoads + B::kLoads + (FP8 ? 1 : 0);
+  constexpr int kLater = S::STAGES - 2;  // steps loading behind the one that a step waits for
+  static_assert(kGroups % kRing == 0, "ring of row fragments");
+  static_assert(!FP8 || (!ACOLS && !BCOLS && S::STEP == 128), "fp8 operands are rows of 128-element blocks");
+  static_assert(kHalves == 2 || S::STAGES % 2 == 0 || S::STAGES == 3, "written-out steps alternate");
+  Fragments<S, ACOLS, BCOLS, SPLIT> fr;
+  fr.init(wave, lane);
+  const uint32_t scale_at = A::kBytes + B::kBytes + ((wave / S::WN) * S::MF * 16 + (lane & 15)) * 4;
+  A a;
+  B b;
+  Frag fa[kRing], fb[2][S::NF];  // fb: by half, or by the parity of the step where it has one
+  float sc[2][S::MF];
+  f32x4 acc[S::MF][S::NF];
+  int at = 0;  // steps of the tile being loaded
+  typename Job::Tile tile;
+  const auto load = [&](uint32_t stage, auto i) EPL_INLINE {
+    if constexpr (i < A::kLoads)
+      a.template load<i>(stage, wave);
+    else if constexpr (i < A::kLoads + B::kLoads)
+      b.template load<i - A::kLoads>(stage + A::kBytes, wave);
+    else if constexpr (FP8)
+      job.load_scales(tile, at - 1, stage + A::kBytes + B::kBytes);
+  };
+  // Of the stage that fr points to: column fragment n of half h into fb[to]; the row fragment of group g.
+  const auto read_b = [&](auto to, auto n, auto h) EPL_INLINE {
+    if constexpr (FP8) {
+      const i32x4 lo = fr.template read_b<n, 0>(), hi = fr.template read_b<n, 1>();
+      fb[to][n] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    } else {
+      fb[to][n] = fr.template read_b<n, h>();
+    }
+  };
+  const auto read_a = [&](auto g) EPL_INLINE {
+    if constexpr (FP8) {
+      const i32x4 lo = fr.template read_a<g, 0>(), hi = fr.template read_a<g, 1>();
+      fa[g % kRing] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    } else {
+      fa[g % kRing] = fr.template read_a<g % S::MF, g / S::MF>();
+    }
+  };
+  const auto read_scale = [&](auto to, auto f, uint32_t stage) EPL_INLINE {
+    sc[to][f] = *(const __attribute__((address_space(3))) float*)(uintptr_t)(stage + scale_at + f * 64);
+  };
+  using Zero = std::integral_constant<int, 0>;
+  using One = std::integral_constant<int, 1>;
+  // The first reads of a stage: its column fragments (and row scales).
+  const auto open_stage = [&](auto to, uint32_t stage) EPL_INLINE {
+    fr.stage(stage);
+    static_for<0, S::NF>([&](auto n) EPL_INLINE { read_b(to, n, Zero{}); });
+    if constexpr (FP8) static_for<0, S::MF>([&](auto f) EPL_INLINE { read_scale(to, f, stage); });
+  };
+  // Set up a tile's operands and issue the loads of its first STAGES steps.
+  const auto begin_tile = [&]() EPL_INLINE {
+    job.begin(tile, a, b);
+    at = 1;
+    static_for<0, S::STAGES>([&](auto i) EPL_INLINE {
+      static_for<0, kLoads>([&](auto j) EPL_INLINE { load(lds + i * kStage, j); });
+      job.turn(tile, at, a, b);
+      ++at;
+    });
+  };
+
+  uint32_t cur = lds;  // stage of the current step
+  int stored = 0;  // steps still to come whose loads are in front of the previous tile's stores
+  // One step. par: its parity. left: steps of the tile after it, or STAGES if this stage is loaded again.
+  const auto step = [&](auto par, auto left) EPL_INLINE {
+    const uint32_t here = cur;
+    cur = cur == lds + (S::STAGES - 1) * kStage ? lds : cur + kStage;
+    static_for<0, kGroups>([&](auto g) EPL_INLINE {
+      constexpr int m = g % S::MF, bi = kHalves == 2 ? g / S::MF : par;
+      if constexpr (g == kTail) {
+        // All reads of this stage have returned, also in the compiler's books: otherwise it would make the last
+        // groups' products wait for the reads that follow the barrier.
+        static_for<0, kAhead>([&](auto i) EPL_INLINE { arrived(fa[(g + i) % kRing]); });
+        if constexpr (kHalves == 2) static_for<0, S::NF>([&](auto n) EPL_INLINE { arrived(fb[1][n]); });
+        if constexpr (left > 0) {
+          job.template wait<kLoads * std::min(kLater, left - 1)>(stored > 0);
+          fr.stage(cur);
+        }
+      }
+      static_for<0, S::NF>([&](auto n) EPL_INLINE {
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (!FP8) {
+          acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fb[bi][n]),
+                                                              __builtin_bit_cast(bf16x8, fa[g % kRing]), acc[m][n], 0,
+                                                              0, 0);
+        } else {
+          // One 128-element block of the row's scale: the block's product starts at zero and joins the sum
+          // scaled, in 32 bits; the instruction's own block scales stay at one (exponent 127).
+          const f32x4 p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+              fb[bi][n], fa[g % kRing], f32x4{0, 0, 0, 0}, 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[m][n][i] = fmaf(sc[bi][m], p[i], acc[m][n][i]);
+        }
+        // What follows this product in the instruction stream.
+        if constexpr (g < kTail) {
+          if constexpr (n == 0) read_a(std::integral_constant<int, g + kAhead>{});
+          // The second half's column fragments, spread over the first half's groups.
+          constexpr int kSpread = std::min(S::MF, kTail), per = (S::NF + kSpread - 1) / kSpread;
+          if constexpr (kHalves == 2 && g < kSpread && n == S::NF / 2)
+            static_for<g * per, std::min((g + 1) * per, S::NF)>([&](auto i) EPL_INLINE { read_b(One{}, i, One{}); });
+        } else if constexpr (left > 0) {
+          constexpr int slot = (g - kTail) * S::NF + n, kSlots = kAhead * S::NF;
+          constexpr int to = kHalves == 2 ? 0 : 1 - par;
+          if constexpr (slot < S::NF) read_b(std::integral_constant<int, to>{}, n, Zero{});
+          // A ring entry is free once its own group is done.
+          if constexpr (g == kTail + 1 && n < 2) read_a(n);
+          if constexpr (g == kTail + 2 && n == 0) read_a(std::integral_constant<int, 2>{});
+          if constexpr (FP8 && slot == S::NF)
+            static_for<0, S::MF>([&](auto f) EPL_INLINE { read_scale(std::integral_constant<int, to>{}, f, cur); });
+          if constexpr (left == S::STAGES) {
+            constexpr int per = (kLoads + kSlots - 1) / kSlots, begin = kSlots - (kLoads + per - 1) / per;
+            if constexpr (slot >= begin)
+              static_for<(slot - begin) * per, std::min((slot - begin + 1) * per, kLoads)>(
+                  [&](auto i) EPL_INLINE { load(here, i); });
+          }
+        }
+      });
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    stored -= stored > 0;
+    if constexpr (left == S::STAGES) {
+      job.turn(tile, at, a, b);
+      ++at;
+    }
+  };
+  using Middle = std::integral_constant<int, S::STAGES>;
+
+  if (!job.first(tile)) return;
+  begin_tile();
+  while (true) {
+#pragma unroll
+    for (int m = 0; m < S::MF; ++m)
+#pragma unroll
+      for (int n = 0; n < S::NF; ++n) acc[m][n] = f32x4{0, 0, 0, 0};
+    job.template wait<kLoads*(S::STAGES - 1)>(stored > 0);
+    cur = lds;
+    open_stage(Zero{}, cur);
+    static_for<0, kAhead>(read_a);
+    constexpr int kOdd = kHalves == 2 ? 0 : S::STAGES % 2;  // an odd number of written-out steps
+    if constexpr (kOdd) {
+      if (tile.steps > S::STAGES) step(Zero{}, Middle{});
+    }
+    for (int s = tile.steps - S::STAGES - kOdd; s > 0; s -= kHalves == 2 ? 1 : 2) {
+      step(std::integral_constant<int, kHalves == 2 ? 0 : kOdd>{}, Middle{});
+      if constexpr (kHalves == 1) step(std::integral_constant<int, 1 - kOdd>{}, Middle{});
+    }
+    static_for<0, S::STAGES>([&](auto i) EPL_INLINE {
+      step(std::integral_constant<int, kHalves == 2 ? 0 : (kOdd + i) % 2>{},
+           std::integral_constant<int, S::STAGES - 1 - i>{});
+    });
+    const typename Job::Tile done = tile;
+    const bool more = job.next(tile);
+    wait_tiles<0>();  // every wave has read the last stages
+    if (more) begin_tile();
+    job.finish(done, acc);
+    if (!more) return;
+    stored = S::STAGES - 1;
+  }
+}
+
+// ---------------------------------------------------------------- tiles over the experts' rows
+// The experts' row offsets, clipped, and the number of row tiles before each, in LDS.
+struct RowTable {
+  int off[EPL_MAX_EXPERTS + 1];  // expert e: rows [off[e], end(e))
+  int mt[EPL_MAX_EXPERTS + 1];
+};
+
+// Fills the table (BM rows a tile; 0: offsets alone); returns after a barrier. The clipped offsets are made
+// monotonic by a running maximum, so that expert e's rows are [off[e], off[e + 1]).
 template <int BM>
-__device__ __forceinline__ void count_row_tiles(const int32_t* expert_off, int E, int cap, int* mt) {
+__device__ __forceinline__ void fill_row_table(const int32_t* expert_off, int E, int cap, RowTable& tab) {
   if (threadIdx.x < kWave) {
     const int lane = threadIdx.x;
-    int carry = 0;
-    for (int e0 = 0; e0 < E; e0 += kWave) {
+    int carry = 0, top = 0;
+    for (int e0 = 0; e0 <= E; e0 += kWave) {
       const int e = e0 + lane;
-      int n = 0;
-      if (e < E) {
-        int beg, end;
-        expert_rows(expert_off, e, cap, beg, end);
-        n = (end - beg + BM - 1) / BM;
+      int o = e <= E ? std::min(std::max(expert_off[e], 0), cap) : 0;
+#pragma unroll
+      for (int d = 1; d < kWave; d <<= 1) {
+        const int v = __shfl_up(o, d, kWave);
+        if (lane >= d) o = std::max(o, v);
       }
-      const int inc = wave_inclusive_sum(n) + carry;
-      if (e < E) mt[e + 1] = inc;
-      carry = __shfl(inc, kWave - 1, kWave);
+      o = std::max(o, top);
+      if (e <= E) tab.off[e] = o;
+      if constexpr (BM > 0) {
+        int before = __shfl_up(o, 1, kWave);  // the offset before this one
+        if (lane == 0) before = top;
+        const int n = e > 0 && e <= E ? (o - before + BM - 1) / BM : 0;  // row tiles of expert e - 1
+        const int inc = wave_inclusive_sum(n) + carry;
+        if (e <= E) tab.mt[e] = inc;
+        carry = __shfl(inc, kWave - 1, kWave);
+      }
+      top = __shfl(o, kWave - 1, kWave);
     }
-    if (lane == 0) mt[0] = 0;
   }
   __syncthreads();
 }
@@ -291,31 +513,45 @@ __device__ __forceinline__ void band_tile(int64_t j, int64_t mt, int nt, int ban
   n = (int)(bi * band + (r - (int64_t)m * w));
 }
 
-// ---------------------------------------------------------------- activations (fp32)
-__device__ __forceinline__ float activate(int act, float v) {
-  switch (act) {
-    case EPL_ACT_SILU:
-      return v / (1.0f + expf(-v));
-    case EPL_ACT_GELU:
-      return 0.5f * v * (1.0f + erff(v * 0.70710678118654752f));
-    case EPL_ACT_RELU:
-      return v < 0.0f ? 0.0f : v;
-    default:
-      return v;
+__device__ __forceinline__ u32x4 pack8(const float (&v)[8]) {
+  return u32x4{f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]), f32x2_to_bf16x2(v[4], v[5]),
+               f32x2_to_bf16x2(v[6], v[7])};
+}
+__device__ __forceinline__ void unpack8(u32x4 w, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = bf16lo_to_f32(w[i]);
+    v[2 * i + 1] = bf16hi_to_f32(w[i]);
   }
 }
-__device__ __forceinline__ float activate_grad(int act, float v) {
+
+// ---------------------------------------------------------------- activations (fp32)
+template <int ACT>
+__device__ __forceinline__ float activate(float v) {
+  if constexpr (ACT == EPL_ACT_SILU) return v / (1.0f + expf(-v));
+  if constexpr (ACT == EPL_ACT_GELU) return 0.5f * v * (1.0f + erff(v * 0.70710678118654752f));
+  if constexpr (ACT == EPL_ACT_RELU) return v < 0.0f ? 0.0f : v;
+  return v;
+}
+template <int ACT>
+__device__ __forceinline__ float activate_grad(float v) {
+  if constexpr (ACT == EPL_ACT_SILU) {
+    const float s = 1.0f / (1.0f + expf(-v));
+    return s * (1.0f + v * (1.0f - s));
+  }
+  if constexpr (ACT == EPL_ACT_GELU)
+    return 0.5f * (1.0f + erff(v * 0.70710678118654752f)) + v * 0.39894228040143268f * expf(-0.5f * v * v);
+  if constexpr (ACT == EPL_ACT_RELU) return v > 0.0f ? 1.0f : 0.0f;
+  return 1.0f;
+}
+// f(integral_constant<int, activation>) of the activation `act`: one branch for all that f does.
+template <class F>
+__device__ __forceinline__ void with_activation(int act, F&& f) {
   switch (act) {
-    case EPL_ACT_SILU: {
-      const float s = 1.0f / (1.0f + expf(-v));
-      return s * (1.0f + v * (1.0f - s));
-    }
-    case EPL_ACT_GELU:
-      return 0.5f * (1.0f + erff(v * 0.70710678118654752f)) + v * 0.39894228040143268f * expf(-0.5f * v * v);
-    case EPL_ACT_RELU:
-      return v > 0.0f ? 1.0f : 0.0f;
-    default:
-      return 1.0f;
+    case EPL_ACT_SILU: f(std::integral_constant<int, EPL_ACT_SILU>{}); break;
+    case EPL_ACT_GELU: f(std::integral_constant<int, EPL_ACT_GELU>{}); break;
+    case EPL_ACT_RELU: f(std::integral_constant<int, EPL_ACT_RELU>{}); break;
+    default: f(std::integral_constant<int, EPL_ACT_NONE>{});
   }
 }
 
