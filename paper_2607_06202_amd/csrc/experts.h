@@ -43,11 +43,13 @@ struct WeightGradArgs {
 
 // The kernels' choice by the rows that there can be (cap = T*k) over E experts.
 //
-// few_rows: the split reduction of experts_few.hip against 128 x 256 tiles, us. 128 experts, 2048 to 2 x 768, top-8:
-// 8 rows 16.0 / 32.3, 16 rows 29.3 / 33.8, 32 rows 43.5 / 36.8, 64 rows 71 / 76, 128 rows 108 / 105; 768 to 2048,
-// 8 rows 14.5 / 15.4, 32 rows 27 / 21. E4M3, 64 experts, 7168 to 2 x 2048: 8 rows 56 / 92, 32 rows 173 / 229, 128 rows
-// 353 / 459, 512 rows 434 / 494.
-inline bool few_rows(int64_t cap, int E, bool fp8) { return cap <= (fp8 ? std::max(16, 8 * E) : 16); }
+// few_rows: the split reduction of experts_few.hip against 128 x 256 tiles, us, 128 experts, top-8. 2048 to 2 x 768: 8
+// rows 16.0 / 32.3, 16 rows 29.3 / 33.8, 32 rows 43.5 / 36.8, 128 rows 108 / 105; 768 to 2048: 8 rows 14.5 / 15.4, 32 rows
+// 27 / 21.
+inline bool few_rows(int64_t cap) { return cap <= 16; }
+// short_rows (fp8): 64 x 256 tiles against 128 x 256, us, 64 experts, 7168 to 2 x 2048: 8 rows each 351 / 494, 128 rows 728
+// / 897, 256 rows 1170 / 1136.
+inline bool short_rows(int64_t cap, int E) { return cap / E < 256; }
 // many_rows: 256 x 256 tiles against 128 x 256, us, 32 experts, 7168 to 2 x 2048: 256 rows each 607 / 658 (the smaller
 // tile first), 512 rows 1001 / 1023, 1024 rows 1844 / 1774, 2048 rows 3565 / 3421; 2048 to 7168: 980 / 1001 at 1024,
 // 1851 / 1833 at 2048.

@@ -474,6 +474,7 @@ __global__ void __launch_bounds__(256) pre_bias_grad_kernel(const char* dy, cons
 // ---------------------------------------------------------------- launches
 using Big = Shape<256, 256, 2, 4, 128, 2>;
 using Mid = Shape<128, 256, 2, 4, 128, 3>;
+using Short = Shape<64, 256, 1, 4, 128, 3>;
 
 static unsigned persistent_grid(int64_t tiles, int per_cu) {
   return (unsigned)std::min<int64_t>(tiles, (int64_t)kCus * per_cu);
@@ -493,7 +494,9 @@ static hipError_t forward_as(const ForwardArgs& p, hipStream_t stream) {
 
 hipError_t launch_forward(const ForwardArgs& p, bool fp8, bool gated, hipStream_t stream) {
   if (p.cap == 0) return hipSuccess;
-  if (few_rows(p.cap, p.E, fp8)) return launch_forward_few(p, fp8, gated, stream);
+  if (few_rows(p.cap)) return launch_forward_few(p, fp8, gated, stream);
+  if (fp8 && short_rows(p.cap, p.E))
+    return gated ? forward_as<Short, true, true>(p, stream) : forward_as<Short, true, false>(p, stream);
   if (fp8) return gated ? forward_as<Mid, true, true>(p, stream) : forward_as<Mid, true, false>(p, stream);
   if (many_rows(p.cap, p.E))
     return gated ? forward_as<Big, false, true>(p, stream) : forward_as<Big, false, false>(p, stream);

@@ -1,7 +1,7 @@
-// The experts' forward product for a handful of rows: one token, or a few sequences decoding.
+// The experts' forward product for a handful of rows: one token, a few sequences decoding.
 //
-// Few rows leave few tiles, too few to keep the memory busy, and reading the weights once is all there is to do. So
-// a workgroup takes 16 * NF weight rows of one expert, its four waves each take every fourth 128-byte step of the
+// Reading the weights once is all there is to do, and a tile's start and end would cost as much as its middle. So a
+// workgroup takes 16 * NF weight rows of one expert, its four waves each take every fourth 128-byte step of the
 // reduction, and the four partial sums are joined through LDS in a fixed order. A wave's fragments come straight from
 // memory, kDepth steps ahead: 2 * (NF + 1) KiB a step in flight. Rows past 16 make another pass over the weights.
 //
@@ -36,7 +36,7 @@ __device__ __forceinline__ int nth_expert(const int32_t* expert_off, int E, int 
 }
 
 template <int NF, bool FP8, bool GATED>
-__global__ void __launch_bounds__(kFewWaves* kWave) few_rows_kernel(ForwardArgs p) {
+__global__ void __launch_bounds__(kFewWaves* kWave, 2) few_rows_kernel(ForwardArgs p) {
   constexpr int kCols = 16 * NF / (GATED ? 2 : 1), kEsize = FP8 ? 1 : 2;
   constexpr int kUnits = kCols / 32;  // groups of 32 output columns
   __shared__ f32x4 part[kFewWaves][NF][kWave];
@@ -105,14 +105,15 @@ __global__ void __launch_bounds__(kFewWaves* kWave) few_rows_kernel(ForwardArgs 
               acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b[d][n][h]),
                                                                __builtin_bit_cast(bf16x8, a[d][h]), acc[n], 0, 0, 0);
         } else {
-          const i32x8 fa = __builtin_shufflevector(__builtin_bit_cast(i32x4, a[d][0]), __builtin_bit_cast(i32x4, a[d][1]),
-                                                   0, 1, 2, 3, 4, 5, 6, 7);
+          // As in run_tiles: a block's product joins the sum scaled, the instruction's own scales are one.
+          const auto join = [](const u32x4(&h)[2]) EPL_INLINE {
+            return __builtin_shufflevector(__builtin_bit_cast(i32x4, h[0]), __builtin_bit_cast(i32x4, h[1]), 0, 1, 2, 3,
+                                           4, 5, 6, 7);
+          };
 #pragma unroll
           for (int n = 0; n < NF; ++n) {
-            const i32x8 fb = __builtin_shufflevector(__builtin_bit_cast(i32x4, b[d][n][0]),
-                                                     __builtin_bit_cast(i32x4, b[d][n][1]), 0, 1, 2, 3, 4, 5, 6, 7);
-            const f32x4 t = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb, fa, f32x4{0, 0, 0, 0}, 0, 0, 0,
-                                                                             0x7f7f7f7f, 0, 0x7f7f7f7f);
+            const f32x4 t = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+                join(b[d][n]), join(a[d]), f32x4{0, 0, 0, 0}, 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
 #pragma unroll
             for (int i = 0; i < 4; ++i) acc[n][i] = fmaf(sc[d], t[i], acc[n][i]);
           }
@@ -124,61 +125,59 @@ __global__ void __launch_bounds__(kFewWaves* kWave) few_rows_kernel(ForwardArgs 
 #pragma unroll
     for (int n = 0; n < NF; ++n) part[wave][n][lane] = acc[n];
     __syncthreads();
-    if (wave < kUnits) {
-      // Column group `wave`: eight consecutive columns of row rho.
-      const int c = col0 + wave * 32 + q * 8;
-      if (c < p.N && rho < rows) {
-        float v[8], u[8];
+    // Column group `wave`: eight consecutive columns of row rho.
+    const int c = col0 + wave * 32 + q * 8;
+    if (wave < kUnits && c < p.N && rho < rows) {
+      float v[8], u[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        v[i] = u[i] = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kFewWaves; ++w) {
+          v[i] += part[w][wave * 2 + i / 4][lane][i % 4];
+          if constexpr (GATED) u[i] += part[w][NF / 2 + wave * 2 + i / 4][lane][i % 4];
+        }
+      }
+      const int64_t cc = (int64_t)e * p.N + c, row = row0 + rho;
+      if constexpr (FP8) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          v[i] = u[i] = 0.0f;
-#pragma unroll
-          for (int w = 0; w < kFewWaves; ++w) {
-            v[i] += part[w][wave * 2 + i / 4][lane][i % 4];
-            if constexpr (GATED) u[i] += part[w][NF / 2 + wave * 2 + i / 4][lane][i % 4];
-          }
+          v[i] *= p.w_scale[cc + i];
+          if constexpr (GATED) u[i] *= p.w2_scale[cc + i];
         }
-        const int64_t cc = (int64_t)e * p.N + c, row = row0 + rho;
-        if constexpr (FP8) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            v[i] *= p.w_scale[cc + i];
-            if constexpr (GATED) u[i] *= p.w2_scale[cc + i];
-          }
-        }
-        if constexpr (!GATED) {
-          if (p.bias) {
-            float d[8];
-            unpack8(*(const u32x4*)(p.bias + cc * 2), d);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += d[i];
-          }
-        }
-        if (p.pre) {
-          if constexpr (GATED) {
-            *(u32x4*)(p.pre + (row * 2 * p.N + c) * 2) = pack8(v);
-            *(u32x4*)(p.pre + (row * 2 * p.N + p.N + c) * 2) = pack8(u);
-          } else {
-            *(u32x4*)(p.pre + (row * p.N + c) * 2) = pack8(v);
-          }
-        }
-        with_activation(p.act, [&](auto act) EPL_INLINE {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            v[i] = activate<act>(v[i]);
-            if constexpr (GATED) v[i] *= u[i];
-          }
-        });
-        if constexpr (!GATED) {
-          if (p.residual) {
-            float d[8];
-            unpack8(*(const u32x4*)(p.residual + row * p.res_ld + c * 2ll), d);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += d[i];
-          }
-        }
-        *(u32x4*)(p.out + row * p.out_ld + c * 2ll) = pack8(v);
       }
+      if constexpr (!GATED) {
+        if (p.bias) {
+          float d[8];
+          unpack8(*(const u32x4*)(p.bias + cc * 2), d);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[i] += d[i];
+        }
+      }
+      if (p.pre) {
+        if constexpr (GATED) {
+          *(u32x4*)(p.pre + (row * 2 * p.N + c) * 2) = pack8(v);
+          *(u32x4*)(p.pre + (row * 2 * p.N + p.N + c) * 2) = pack8(u);
+        } else {
+          *(u32x4*)(p.pre + (row * p.N + c) * 2) = pack8(v);
+        }
+      }
+      with_activation(p.act, [&](auto act) EPL_INLINE {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          v[i] = activate<act>(v[i]);
+          if constexpr (GATED) v[i] *= u[i];
+        }
+      });
+      if constexpr (!GATED) {
+        if (p.residual) {
+          float d[8];
+          unpack8(*(const u32x4*)(p.residual + row * p.res_ld + c * 2ll), d);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[i] += d[i];
+        }
+      }
+      *(u32x4*)(p.out + row * p.out_ld + c * 2ll) = pack8(v);
     }
   }
 }
@@ -187,7 +186,8 @@ template <int NF, bool FP8, bool GATED>
 static hipError_t launch_as(const ForwardArgs& p, hipStream_t stream) {
   constexpr int kCols = 16 * NF / (GATED ? 2 : 1);
   const int64_t grid = (int64_t)((p.N + kCols - 1) / kCols) * std::min(p.E, p.cap);
-  hipLaunchKernelGGL((few_rows_kernel<NF, FP8, GATED>), dim3((unsigned)grid), dim3(kFewWaves * kWave), 0, stream, p);
+  hipLaunchKernelGGL((few_rows_kernel<NF, FP8, GATED>), dim3((unsigned)grid), dim3(kFewWaves * kWave), 0,
+                     stream, p);
   return hipGetLastError();
 }
 
