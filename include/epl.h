@@ -413,9 +413,9 @@ epl_status epl_experts_linear(const epl_config *cfg, const epl_linear *lin, cons
                               const void *bias, const void *residual, void *out, void *pre, void *stream);
 
 /* Its gradients (bf16; EPL_ERR_UNSUPPORTED for E4M3). The residual's gradient is dy itself.
- *   dy       [rows][N] without gaps (out_pitch is not used).
+ *   dy       rows of N, out_pitch apart (as combine's gradient writes them); residual_pitch is not used.
  *   pre      what the forward call kept; ignored (may be NULL) for EPL_ACT_NONE.
- *   dpre     [rows][N]: dy * act'(pre), rounded to bf16. May be pre or dy. Ignored (may be NULL) for EPL_ACT_NONE.
+ *   dpre     [rows][N] without gaps: dy * act'(pre), rounded to bf16. May be pre. Ignored (may be NULL) for EPL_ACT_NONE.
  *   da       rows of K, in_pitch apart: dpre w[e].   dw  [E][N][K] without gaps: dpre^T a.
  *   dbias    NULL, or [E*N] bf16: the sum of the unrounded dpre over the expert's rows.
  * da must not alias a.                                                                                */

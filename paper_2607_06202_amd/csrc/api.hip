@@ -602,6 +602,7 @@ EPL_EXPORT epl_status epl_experts_gated_backward(const epl_config* cfg, const ep
   if (e != hipSuccess) return from_hip(e);
   epl::RowGradArgs r{};
   r.d = static_cast<const char*>(dpre);
+  r.d_ld = (int64_t)I * 4;
   r.w = static_cast<const char*>(w_gate);
   r.w2 = static_cast<const char*>(w_up);
   r.dx = static_cast<char*>(drecv);
@@ -616,6 +617,7 @@ EPL_EXPORT epl_status epl_experts_gated_backward(const epl_config* cfg, const ep
   if ((e = epl::launch_row_grad(r, s)) != hipSuccess) return from_hip(e);
   epl::WeightGradArgs w{};
   w.d = static_cast<const char*>(dpre);
+  w.d_ld = (int64_t)I * 4;
   w.x = static_cast<const char*>(recv);
   w.dw = static_cast<char*>(dw_gate);
   w.dw2 = static_cast<char*>(dw_up);
@@ -676,10 +678,12 @@ EPL_EXPORT epl_status epl_experts_linear_backward(const epl_config* cfg, const e
   if (any && da == a) return EPL_ERR_INVALID_ARG;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const int E = cfg->num_experts, K = lin->in_features, N = lin->out_features, cap = cap_of(cfg);
-  hipError_t e = epl::launch_pre_grad(dy, pre, dpre, dbias, L->expert_off, E, cap, N, lin->activation, s);
+  const int64_t dy_ld = (int64_t)(lin->out_pitch ? lin->out_pitch : N) * 2;
+  hipError_t e = epl::launch_pre_grad(dy, dy_ld, pre, dpre, dbias, L->expert_off, E, cap, N, lin->activation, s);
   if (e != hipSuccess) return from_hip(e);
   epl::RowGradArgs r{};
   r.d = static_cast<const char*>(act ? dpre : dy);
+  r.d_ld = act ? (int64_t)N * 2 : dy_ld;
   r.w = static_cast<const char*>(w);
   r.dx = static_cast<char*>(da);
   r.expert_off = L->expert_off;
@@ -693,6 +697,7 @@ EPL_EXPORT epl_status epl_experts_linear_backward(const epl_config* cfg, const e
   if ((e = epl::launch_row_grad(r, s)) != hipSuccess) return from_hip(e);
   epl::WeightGradArgs g{};
   g.d = r.d;
+  g.d_ld = r.d_ld;
   g.x = static_cast<const char*>(a);
   g.dw = static_cast<char*>(dw);
   g.expert_off = L->expert_off;

@@ -24,20 +24,20 @@ struct ForwardArgs {
 };
 
 struct RowGradArgs {
-  const char* d;  // [rows][parts * N] bf16
+  const char* d;  // rows of parts * N bf16
   const char *w, *w2;
   char* dx;
   const int32_t* expert_off;
-  int64_t dx_ld, expert_stride;
+  int64_t d_ld, dx_ld, expert_stride;
   int E, cap, N, K, parts;
 };
 
 struct WeightGradArgs {
-  const char* d;  // [rows][parts * N] bf16
+  const char* d;  // rows of parts * N bf16
   const char* x;
   char *dw, *dw2;  // [E][N][K] bf16
   const int32_t* expert_off;
-  int64_t x_ld;
+  int64_t d_ld, x_ld;
   int E, cap, N, K, parts;
 };
 
@@ -60,9 +60,9 @@ hipError_t launch_row_grad(const RowGradArgs& p, hipStream_t stream);
 hipError_t launch_weight_grad(const WeightGradArgs& p, hipStream_t stream);
 hipError_t launch_gated_pre_grad(const void* dh, const void* pre, void* dpre, const int32_t* expert_off, int E,
                                  int cap, int I, int act, hipStream_t stream);
-// dpre (with an activation) and, unless dbias is null, dbias.
-hipError_t launch_pre_grad(const void* dy, const void* pre, void* dpre, void* dbias, const int32_t* expert_off, int E,
-                           int cap, int N, int act, hipStream_t stream);
+// dpre (with an activation) and, unless dbias is null, dbias. dy rows dy_ld bytes apart.
+hipError_t launch_pre_grad(const void* dy, int64_t dy_ld, const void* pre, void* dpre, void* dbias,
+                           const int32_t* expert_off, int E, int cap, int N, int act, hipStream_t stream);
 
 struct RouteArgs {
   const void* logits;  // [T][E] fp32 or bf16

@@ -263,14 +263,14 @@ struct RowGradJob {
   }
   template <class A, class B>
   __device__ __forceinline__ void begin(const Tile& t, A& a, B& b) const {
-    a.lanes(t.rows, (int64_t)p.N * p.parts * 2, wave, lane);
+    a.lanes(t.rows, p.d_ld, wave, lane);
     b.lanes(std::min(p.K - t.col0, S::BN), (int64_t)p.K * 2, wave, lane);
     start(t, 0, p.w, a, b);
   }
   template <class A, class B>
   __device__ __forceinline__ void start(const Tile& t, int part, const char* w, A& a, B& b) const {
-    const int64_t lda = (int64_t)p.N * p.parts * 2, ldb = (int64_t)p.K * 2;
-    a.start_rows(p.d + t.row0 * lda + (int64_t)part * p.N * 2, nullptr, t.rows, lda, p.N * 2);
+    const int64_t ldb = (int64_t)p.K * 2;
+    a.start_rows(p.d + t.row0 * p.d_ld + (int64_t)part * p.N * 2, nullptr, t.rows, p.d_ld, p.N * 2);
     b.start_cols(w + (t.e * p.expert_stride + t.col0) * 2, p.N, std::min(p.K - t.col0, S::BN), ldb);
   }
   // The second part's first step. (An only part's padded step may have that number too.)
@@ -345,11 +345,10 @@ struct WeightGradJob {
   __device__ __forceinline__ void turn(const Tile&, int, A&, B&) const {}
   template <class A, class B>
   __device__ __forceinline__ void begin(const Tile& t, A& a, B& b) const {
-    const int64_t lda = (int64_t)p.N * p.parts * 2;
     const int m = std::min(p.N - t.m0, S::BM), cols = std::min(p.K - t.col0, S::BN);
-    a.lanes(m, lda, wave, lane);
+    a.lanes(m, p.d_ld, wave, lane);
     b.lanes(cols, p.x_ld, wave, lane);
-    a.start_cols(p.d + t.beg * lda + ((int64_t)t.part * p.N + t.m0) * 2, t.rows, m, lda);
+    a.start_cols(p.d + t.beg * p.d_ld + ((int64_t)t.part * p.N + t.m0) * 2, t.rows, m, p.d_ld);
     b.start_cols(p.x + t.beg * p.x_ld + t.col0 * 2ll, t.rows, cols, p.x_ld);
   }
   template <int N>
@@ -403,13 +402,15 @@ __global__ void __launch_bounds__(256) gated_pre_grad_kernel(const char* dh, con
   }
 }
 
-// Linear: dpre = dy act'(pre) in bf16.
-__global__ void __launch_bounds__(256) pre_grad_kernel(const char* dy, const char* pre, char* dpre,
+// Linear: dpre = dy act'(pre) in bf16; dy rows dy_ld bytes apart.
+__global__ void __launch_bounds__(256) pre_grad_kernel(const char* dy, int64_t dy_ld, const char* pre, char* dpre,
                                                        const int32_t* expert_off, int E, int cap, int N, int act) {
-  const int64_t n = std::min(std::max(expert_off[E], 0), cap) * (int64_t)(N / 8);
+  const int64_t nv = N / 8;
+  const int64_t n = std::min(std::max(expert_off[E], 0), cap) * nv;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / nv;
     float d[8], v[8];
-    unpack8(((const u32x4*)dy)[i], d);
+    unpack8(*(const u32x4*)(dy + r * dy_ld + (i - r * nv) * 16), d);
     unpack8(((const u32x4*)pre)[i], v);
     with_activation(act, [&](auto act_) EPL_INLINE {
 #pragma unroll
@@ -422,8 +423,9 @@ __global__ void __launch_bounds__(256) pre_grad_kernel(const char* dy, const cha
 // The same with dbias[e][n] = the sum of the unrounded dpre over the expert's rows, in one pass over dy and pre (without
 // an activation there is no dpre to write). A workgroup takes 64 columns of one expert: 8 lanes of 8 columns, 32 row
 // lanes that take every 32nd row, two at a time; fp32 sums, added over the row lanes in order.
-__global__ void __launch_bounds__(256) pre_bias_grad_kernel(const char* dy, const char* pre, char* dpre, char* dbias,
-                                                            const int32_t* expert_off, int cap, int N, int act) {
+__global__ void __launch_bounds__(256) pre_bias_grad_kernel(const char* dy, int64_t dy_ld, const char* pre, char* dpre,
+                                                            char* dbias, const int32_t* expert_off, int cap, int N,
+                                                            int act) {
   constexpr int kLanes = 32;
   __shared__ float part[kLanes][8][8 + 1];
   const int cv = threadIdx.x % 8, rl = threadIdx.x / 8;
@@ -437,9 +439,9 @@ __global__ void __launch_bounds__(256) pre_bias_grad_kernel(const char* dy, cons
       u32x4 dw[2], vw[2];
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        const int64_t at = (std::min<int64_t>(r0 + k * kLanes, end - 1) * N + c) * 2;
-        dw[k] = *(const u32x4*)(dy + at);
-        if (act != EPL_ACT_NONE) vw[k] = *(const u32x4*)(pre + at);
+        const int64_t r = std::min<int64_t>(r0 + k * kLanes, end - 1);
+        dw[k] = *(const u32x4*)(dy + r * dy_ld + c * 2);
+        if (act != EPL_ACT_NONE) vw[k] = *(const u32x4*)(pre + (r * N + c) * 2);
       }
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
@@ -531,14 +533,14 @@ hipError_t launch_gated_pre_grad(const void* dh, const void* pre, void* dpre, co
   return hipGetLastError();
 }
 
-hipError_t launch_pre_grad(const void* dy, const void* pre, void* dpre, void* dbias, const int32_t* expert_off, int E,
-                           int cap, int N, int act, hipStream_t stream) {
+hipError_t launch_pre_grad(const void* dy, int64_t dy_ld, const void* pre, void* dpre, void* dbias,
+                           const int32_t* expert_off, int E, int cap, int N, int act, hipStream_t stream) {
   if (dbias)
     hipLaunchKernelGGL(pre_bias_grad_kernel, dim3((unsigned)((N + 63) / 64 * E)), dim3(256), 0, stream, (const char*)dy,
-                       (const char*)pre, (char*)dpre, (char*)dbias, expert_off, cap, N, act);
+                       dy_ld, (const char*)pre, (char*)dpre, (char*)dbias, expert_off, cap, N, act);
   else if (act != EPL_ACT_NONE && cap > 0)
     hipLaunchKernelGGL(pre_grad_kernel, dim3(elementwise_grid((int64_t)cap * (N / 8))), dim3(256), 0, stream,
-                       (const char*)dy, (const char*)pre, (char*)dpre, expert_off, E, cap, N, act);
+                       (const char*)dy, dy_ld, (const char*)pre, (char*)dpre, expert_off, E, cap, N, act);
   return hipGetLastError();
 }
 

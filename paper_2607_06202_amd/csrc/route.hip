@@ -7,12 +7,17 @@
 // With a selection bias the order is that of score + bias, which fp32 arithmetic can get wrong where two experts
 // nearly tie. So the fp32 keys choose only where every gap between one choice and the next best exceeds what the
 // rounding can make of it; the rare other tokens are chosen again from fp64 scores.
+#include <type_traits>
+
 #include "epl_internal.h"
 #include "experts.h"
 
 namespace epl {
 
 constexpr int kRouteWaves = 4;
+// Most workgroups of a launch. 131072 tokens, 256 experts, us with 2048 / 4096 / 8192 / 16384: biased choice 126 / 120 /
+// 117 / 114, gradient 95 / 90 / 83 / 82; one token to a wave, without the next token's loads in flight: 135 and 111.
+constexpr int kRouteGrid = 16384;
 
 __device__ __forceinline__ uint32_t order_key(float v) {
   const uint32_t u = __float_as_uint(v + 0.0f);  // -0 counts as 0
@@ -27,8 +32,8 @@ __device__ __forceinline__ float key_value(uint32_t k) {
 }
 
 template <int CTRL, int ROW_MASK>
-__device__ __forceinline__ uint32_t dpp_max(uint32_t v) {
-  const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, ROW_MASK, 0xf, false);
+__device__ __forceinline__ uint32_t dpp_max(uint32_t v) {  // lanes without a source take 0, the least key
+  const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROW_MASK, 0xf, true);
   return v > o ? v : o;
 }
 // Maximum over the wave, uniform. Row shifts by 1, 2, 4, 8, then the broadcasts of lane 15 and lane 31.
@@ -49,11 +54,24 @@ __device__ __forceinline__ uint64_t wave_max(uint64_t v) {
   }
   return v;
 }
-template <class F>
-__device__ __forceinline__ F wave_total(F v) {
+__device__ __forceinline__ double wave_total(double v) {
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, kWave);
   return v;
+}
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ float dpp_add(float v) {
+  return v + __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, ROW_MASK, 0xf, false));
+}
+// Sum over the wave in a fixed tree, uniform. Lanes without a source add 0.
+__device__ __forceinline__ float wave_total(float v) {
+  v = dpp_add<0x111, 0xf>(v);
+  v = dpp_add<0x112, 0xf>(v);
+  v = dpp_add<0x114, 0xf>(v);
+  v = dpp_add<0x118, 0xf>(v);
+  v = dpp_add<0x142, 0xa>(v);
+  v = dpp_add<0x143, 0xc>(v);
+  return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), 63));
 }
 
 template <bool BF16>
@@ -76,20 +94,52 @@ __device__ __forceinline__ F sigmoid(F l) {
     return 1.0f / (1.0f + expf(-l));
 }
 
-// Takes the k largest keys in order; lane j ends up with choice j (or -1). next: the largest key left.
-template <int SLOTS, class K>
+// The same from the hardware's exponential and reciprocal (one unit in the last place each), for keys whose error is
+// bounded below and for nothing that is returned.
+__device__ __forceinline__ float exp_near(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504089f); }
+__device__ __forceinline__ float sigmoid_near(float l) { return __builtin_amdgcn_rcpf(1.0f + exp_near(-l)); }
+
+// Takes the k largest keys in order; lane j ends up with choice j (or -1). NEXT: also the largest key left.
+template <int SLOTS, bool NEXT, class K>
 __device__ __forceinline__ int take_top(K (&key)[SLOTS], int k, int lane, K* picked, K* next) {
   int mine = -1;
   K mine_key = 0;
   K best = 0;
-  for (int j = 0; j <= k; ++j) {
-    K b = 0;
-    int bs = 0;
+  // A lane's keys in descending order, the lower slot first among equals (neighbours exchanged, so stable), with
+  // their slots: a choice then only moves its lane's keys up. Sorting costs less than looking for the lane's
+  // largest at every choice up to four slots.
+  constexpr bool kSorted = SLOTS <= 4;
+  uint32_t order = 0x03020100u;  // the sorted keys' slots, a byte each
+  if constexpr (kSorted) {
+    uint32_t slots[SLOTS];
 #pragma unroll
-    for (int s = 0; s < SLOTS; ++s) {
-      if (key[s] > b) {  // strictly: the lowest slot among equals
-        b = key[s];
-        bs = s;
+    for (int s = 0; s < SLOTS; ++s) slots[s] = s;
+#pragma unroll
+    for (int n = SLOTS - 1; n > 0; --n)
+#pragma unroll
+      for (int s = 0; s < n; ++s) {
+        const bool swap = key[s] < key[s + 1];
+        const K hi = swap ? key[s + 1] : key[s], lo = swap ? key[s] : key[s + 1];
+        const uint32_t hs = swap ? slots[s + 1] : slots[s], ls = swap ? slots[s] : slots[s + 1];
+        key[s] = hi;
+        key[s + 1] = lo;
+        slots[s] = hs;
+        slots[s + 1] = ls;
+      }
+    order = 0;
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s) order |= slots[s] << (8 * s);
+  }
+  for (int j = 0; j < k + (NEXT ? 1 : 0); ++j) {
+    K b = key[0];
+    int bs = kSorted ? (int)(order & 255u) : 0;
+    if constexpr (!kSorted) {
+#pragma unroll
+      for (int s = 1; s < SLOTS; ++s) {
+        if (key[s] > b) {  // strictly: the lowest slot among equals
+          b = key[s];
+          bs = s;
+        }
       }
     }
     best = wave_max(b);
@@ -113,9 +163,17 @@ __device__ __forceinline__ int take_top(K (&key)[SLOTS], int k, int lane, K* pic
       mine = slot * kWave + owner;
       mine_key = best;
     }
+    if constexpr (kSorted) {
+      const bool move = lane == owner;
 #pragma unroll
-    for (int s = 0; s < SLOTS; ++s)
-      if (lane == owner && s == slot) key[s] = 0;
+      for (int s = 0; s + 1 < SLOTS; ++s) key[s] = move ? key[s + 1] : key[s];
+      key[SLOTS - 1] = move ? 0 : key[SLOTS - 1];
+      order = move ? order >> 8 : order;
+    } else {
+#pragma unroll
+      for (int s = 0; s < SLOTS; ++s)
+        if (lane == owner && s == slot) key[s] = 0;
+    }
   }
   *picked = mine_key;
   *next = best;
@@ -143,7 +201,7 @@ __device__ __forceinline__ int take_top_wide(const float (&l)[SLOTS], const floa
       if (v > -INFINITY) key[s] = order_key(v);
     }
   }
-  return take_top<SLOTS, uint64_t>(key, k, lane, &a, &b);
+  return take_top<SLOTS, false, uint64_t>(key, k, lane, &a, &b);
 }
 
 // Weight of each chosen logit among the choices, p_j / sum of the chosen p, from scores scaled so that the largest
@@ -165,62 +223,88 @@ __device__ __forceinline__ float share(float l, bool valid, bool sig) {
   return total > 0.0f ? s / total : 0.0f;
 }
 
+// A token's logits: experts lane, lane + 64, ...; -inf past the last expert.
 template <int SLOTS, bool BF16>
+__device__ __forceinline__ void load_row(const void* logits, int64_t g, int E, int lane, float (&l)[SLOTS]) {
+#pragma unroll
+  for (int s = 0; s < SLOTS; ++s) {
+    const int e = s * kWave + lane;
+    const float v = load_logit<BF16>(logits, g * E + std::min(e, E - 1));  // no branch for the last lanes
+    l[s] = e < E ? v : -INFINITY;
+  }
+}
+// Expert e's logit, of a row in registers; e differs from lane to lane.
+template <int SLOTS>
+__device__ __forceinline__ float pick_logit(const float (&l)[SLOTS], int e) {
+  float v = -INFINITY;
+#pragma unroll
+  for (int s = 0; s < SLOTS; ++s) {
+    const float o = __shfl(l[s], e & (kWave - 1), kWave);
+    v = (e >> 6) == s ? o : v;
+  }
+  return v;
+}
+
+// The next token's logits load while a token is worked on. What bounds it is instructions: about 40 for each choice (the
+// wave maximum takes six dependent steps), not the 128 MiB of logits.
+template <int SLOTS, bool BF16, bool SIGMOID, bool BIASED>
 __global__ void __launch_bounds__(kRouteWaves* kWave) route_kernel(RouteArgs p) {
   const int lane = threadIdx.x % kWave;
   const int E = p.E, k = p.k;
-  for (int64_t g = (int64_t)blockIdx.x * kRouteWaves + threadIdx.x / kWave; g < p.T;
-       g += (int64_t)gridDim.x * kRouteWaves) {
+  const int64_t stride = (int64_t)gridDim.x * kRouteWaves;
+  int64_t g = (int64_t)blockIdx.x * kRouteWaves + threadIdx.x / kWave;
+  float coming[SLOTS], bias[SLOTS];
+  if (g < p.T) load_row<SLOTS, BF16>(p.logits, g, E, lane, coming);
+  if constexpr (BIASED) load_row<SLOTS, false>(p.bias, 0, E, lane, bias);
+  const bool need_sum = !SIGMOID && (!p.normalize || BIASED);
+  for (; g < p.T; g += stride) {
     float l[SLOTS];
 #pragma unroll
-    for (int s = 0; s < SLOTS; ++s) {
-      const int e = s * kWave + lane;
-      l[s] = e < E ? load_logit<BF16>(p.logits, g * E + e) : -INFINITY;
-    }
-    // The largest logit, and for the softmax scores the sum.
-    uint32_t top = 0;
-#pragma unroll
-    for (int s = 0; s < SLOTS; ++s) top = can_choose(l[s]) ? std::max(top, order_key(l[s])) : top;
-    const bool need_sum = !p.sigmoid && (!p.normalize || p.bias);
-    float m = 0.0f, sum = 1.0f;
+    for (int s = 0; s < SLOTS; ++s) l[s] = coming[s];
+    if (g + stride < p.T) load_row<SLOTS, BF16>(p.logits, g + stride, E, lane, coming);
+    // For the softmax scores, the largest logit and the sum.
+    float m = 0.0f, sum = 1.0f, inv = 1.0f;
     if (need_sum) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int s = 0; s < SLOTS; ++s) top = can_choose(l[s]) ? std::max(top, order_key(l[s])) : top;
       m = key_value(wave_max(top));
       sum = 0.0f;
 #pragma unroll
       for (int s = 0; s < SLOTS; ++s) sum += can_choose(l[s]) ? exp_below(l[s], m) : 0.0f;
       sum = wave_total(sum);
+      inv = __builtin_amdgcn_rcpf(sum);
     }
     uint32_t key[SLOTS], picked, next;
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s) {
-      key[s] = 0;
-      if (!can_choose(l[s])) continue;
-      if (p.bias) {
-        const float v = (p.sigmoid ? sigmoid(l[s]) : exp_below(l[s], m) / sum) + p.bias[s * kWave + lane];
-        if (v > -INFINITY) key[s] = order_key(v);
-      } else {
-        key[s] = order_key(l[s]);
-      }
+      float v = l[s];
+      if constexpr (BIASED)
+        v = (SIGMOID ? sigmoid_near(l[s]) : (l[s] == m ? 1.0f : exp_near(l[s] - m)) * inv) + bias[s];
+      const uint32_t kv = order_key(v);
+      key[s] = can_choose(l[s]) && v > -INFINITY ? kv : 0u;
     }
-    int e = take_top<SLOTS, uint32_t>(key, k, lane, &picked, &next);
-    if (p.bias) {
-      // Error of an fp32 key: the exponential and its argument 1e-7, the sum of up to 1024 terms (16 per lane,
-      // then a tree of 6) and the division 1.4e-6, all relative to a score of at most 1, and half a unit of the
-      // final sum. Two keys further apart than twice that are in the right order.
+    int e = take_top<SLOTS, BIASED, uint32_t>(key, k, lane, &picked, &next);
+    if constexpr (BIASED) {
+      // Error of an fp32 key: the exponential's argument x (rounded twice and multiplied by log2 e, 2e-7 |x| e^x
+      // <= 1e-7), the exponential and the reciprocal 2.4e-7, the sum of up to 1024 terms (16 per lane, then a tree of
+      // 6) and its own exponentials 1.5e-6, the multiplication 6e-8, all relative to a score of at most 1, and half a
+      // unit of the final sum. Two keys further apart than twice that are in the right order.
       uint32_t after = (uint32_t)__shfl_down((int)picked, 1, kWave);
       if (lane == k - 1) after = next;
       const float a = key_value(picked), b = key_value(after);
       const bool near = lane < k && picked && after && !(a - b > 4e-6f + 2.4e-7f * (fabsf(a) + fabsf(b)));
-      if (__ballot(near)) e = take_top_wide<SLOTS>(l, p.bias, m, E, k, p.sigmoid, lane);
+      if (__ballot(near)) e = take_top_wide<SLOTS>(l, p.bias, m, E, k, SIGMOID, lane);
     }
     // Lane j: the score and weight of choice j.
     const bool valid = lane < k && e >= 0;
-    const float le = valid ? load_logit<BF16>(p.logits, g * E + e) : -INFINITY;
+    const float chosen = pick_logit<SLOTS>(l, valid ? e : 0);
+    const float le = valid ? chosen : -INFINITY;
     float sc = 0.0f;
     if (p.normalize)
-      sc = share(le, valid, p.sigmoid);
+      sc = share(le, valid, SIGMOID);
     else if (valid)
-      sc = p.sigmoid ? sigmoid(le) : exp_below(le, m) / sum;
+      sc = SIGMOID ? sigmoid(le) : exp_below(le, m) / sum;
     if (lane < k) {
       p.idx[g * k + lane] = e;
       p.w[g * k + lane] = sc * p.scale;
@@ -239,29 +323,50 @@ template <int SLOTS, bool BF16>
 __global__ void __launch_bounds__(kRouteWaves* kWave) route_backward_kernel(RouteArgs p) {
   const int lane = threadIdx.x % kWave;
   const int E = p.E, k = p.k;
-  for (int64_t g = (int64_t)blockIdx.x * kRouteWaves + threadIdx.x / kWave; g < p.T;
-       g += (int64_t)gridDim.x * kRouteWaves) {
-    const int e = lane < k ? p.idx[g * k + lane] : -1;
+  const bool need_row = !p.sigmoid && !p.normalize;
+  const int64_t stride = (int64_t)gridDim.x * kRouteWaves;
+  int64_t g = (int64_t)blockIdx.x * kRouteWaves + threadIdx.x / kWave;
+  // The next token's choices, gradients and (where the whole row counts) logits load while a token is worked on.
+  int coming_e = -1;
+  float coming_dw = 0.0f, coming[SLOTS];
+  const auto load = [&](int64_t t) __attribute__((always_inline)) {
+    if (lane < k) {
+      coming_e = p.idx[t * k + lane];
+      coming_dw = p.dw[t * k + lane];
+    }
+    if (need_row) load_row<SLOTS, BF16>(p.logits, t, E, lane, coming);
+  };
+  if (g < p.T) load(g);
+  for (; g < p.T; g += stride) {
+    const int e = coming_e;
+    float dw = coming_dw;
     const bool in = e >= 0 && e < E;
-    const float le = in ? load_logit<BF16>(p.logits, g * E + e) : -INFINITY;
-    const bool valid = in && can_choose(le);
-    float dw = valid ? p.dw[g * k + lane] * p.scale : 0.0f;
-    const bool need_row = !p.sigmoid && !p.normalize;
-    float l[SLOTS], m = 0.0f, sum = 1.0f;
+    float le;
+    float p_row[SLOTS], m = 0.0f, sum = 1.0f;  // p_row: exp(l - m), 0 for a masked expert
     if (need_row) {
+      float l[SLOTS];
       uint32_t top = 0;
 #pragma unroll
       for (int s = 0; s < SLOTS; ++s) {
-        const int ee = s * kWave + lane;
-        l[s] = ee < E ? load_logit<BF16>(p.logits, g * E + ee) : -INFINITY;
+        l[s] = coming[s];
         top = can_choose(l[s]) ? std::max(top, order_key(l[s])) : top;
       }
+      if (g + stride < p.T) load(g + stride);
       m = key_value(wave_max(top));
       sum = 0.0f;
 #pragma unroll
-      for (int s = 0; s < SLOTS; ++s) sum += can_choose(l[s]) ? exp_below(l[s], m) : 0.0f;
+      for (int s = 0; s < SLOTS; ++s) {
+        p_row[s] = can_choose(l[s]) ? exp_below(l[s], m) : 0.0f;
+        sum += p_row[s];
+      }
       sum = wave_total(sum);
+      le = pick_logit<SLOTS>(l, in ? e : 0);
+    } else {
+      le = in ? load_logit<BF16>(p.logits, g * E + e) : -INFINITY;
+      if (g + stride < p.T) load(g + stride);
     }
+    const bool valid = in && can_choose(le);
+    dw = valid ? dw * p.scale : 0.0f;
     // What each choice adds to its expert's logit.
     float sc;
     if (p.normalize) {
@@ -272,11 +377,10 @@ __global__ void __launch_bounds__(kRouteWaves* kWave) route_backward_kernel(Rout
     }
     float add = valid ? dw * sc : 0.0f;
     if (p.sigmoid && valid) add *= sigmoid(-le);
-    const float dot = need_row ? wave_total(add) : 0.0f;
+    const float all = need_row && sum > 0.0f ? wave_total(add) / sum : 0.0f;
     float d[SLOTS];
 #pragma unroll
-    for (int s = 0; s < SLOTS; ++s)
-      d[s] = need_row && can_choose(l[s]) ? -(exp_below(l[s], m) / sum) * dot : 0.0f;
+    for (int s = 0; s < SLOTS; ++s) d[s] = need_row ? -p_row[s] * all : 0.0f;
     for (int j = 0; j < k; ++j) {
       const int ej = __builtin_amdgcn_readlane(valid ? e : -1, j);
       const float aj = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(add), j));
@@ -305,16 +409,28 @@ static void launch_slots(const RouteArgs& p, bool back, dim3 grid, hipStream_t s
     else
       hipLaunchKernelGGL((route_backward_kernel<SLOTS, false>), grid, block, 0, s, p);
   } else {
+    const auto score = [&](auto bf16, auto sigmoid) {
+      if (p.bias)
+        hipLaunchKernelGGL((route_kernel<SLOTS, bf16, sigmoid, true>), grid, block, 0, s, p);
+      else
+        hipLaunchKernelGGL((route_kernel<SLOTS, bf16, sigmoid, false>), grid, block, 0, s, p);
+    };
+    const auto type = [&](auto bf16) {
+      if (p.sigmoid)
+        score(bf16, std::true_type{});
+      else
+        score(bf16, std::false_type{});
+    };
     if (p.bf16)
-      hipLaunchKernelGGL((route_kernel<SLOTS, true>), grid, block, 0, s, p);
+      type(std::true_type{});
     else
-      hipLaunchKernelGGL((route_kernel<SLOTS, false>), grid, block, 0, s, p);
+      type(std::false_type{});
   }
 }
 
 static hipError_t launch(const RouteArgs& p, bool back, hipStream_t s) {
   if (p.T == 0) return hipSuccess;
-  const dim3 grid((unsigned)std::min<int64_t>((p.T + kRouteWaves - 1) / kRouteWaves, 1 << 20));
+  const dim3 grid((unsigned)std::min<int64_t>((p.T + kRouteWaves - 1) / kRouteWaves, kRouteGrid));
   if (p.E <= 64)
     launch_slots<1>(p, back, grid, s);
   else if (p.E <= 128)

@@ -1026,15 +1026,15 @@ def experts_linear_backward(cfg: Config, dy: torch.Tensor, a: torch.Tensor, L: L
                             pre: torch.Tensor | None = None, activation: str = "none", need_dbias: bool = False,
                             dpre: torch.Tensor | None = None, da: torch.Tensor | None = None,
                             dw: torch.Tensor | None = None, dbias: torch.Tensor | None = None):
-    """epl_experts_linear_backward: from dy [T*k, N] (contiguous; the residual's gradient is dy itself) and, with an
-    activation, the kept pre -> (da [T*k, K] at a's pitch, dw [E, N, K], dbias [E, N] or None), all bf16. dpre
-    [T*k, N] is scratch for the gradient of pre; it may be pre or dy."""
+    """epl_experts_linear_backward: from dy [T*k, N] (rows any pitch apart; the residual's gradient is dy itself) and,
+    with an activation, the kept pre -> (da [T*k, K] at a's pitch, dw [E, N, K], dbias [E, N] or None), all bf16. dpre
+    [T*k, N] is scratch for the gradient of pre; it may be pre itself."""
     dev = a.device
     bf = torch.bfloat16
     stride = _matrices(w, "w", bf, cfg)
     N, K = w.shape[1], w.shape[2]
     lda = _packed(a, "a", bf, K, cfg)
-    _packed(dy, "dy", bf, N, cfg, N)
+    ldy = _packed(dy, "dy", bf, N, cfg)
     act = _one_of(ACTIVATION, activation, "activation")
     if act:
         _packed(pre, "pre", bf, N, cfg, N)
@@ -1052,7 +1052,7 @@ def experts_linear_backward(cfg: Config, dy: torch.Tensor, a: torch.Tensor, L: L
     bp = _biases(dbias, "dbias", cfg, N)
     _check_layout(cfg, L, dev)
     _same_device(dev, dy=dy, pre=pre, dpre=dpre, w=w, da=da, dw=dw, dbias=dbias)
-    lin = Linear(K, N, lda, 0, 0, act, PAYLOAD_BF16, stride)
+    lin = Linear(K, N, lda, ldy, 0, act, PAYLOAD_BF16, stride)
     bufs = L.buffers()
     rows = min(t.shape[0] for t in (a, dy, da, pre, dpre) if t is not None)
     with _on(dev):

@@ -218,10 +218,10 @@ def test_linear_forward(case):
 
 @pytest.mark.parametrize("case", LINEAR_CASES, ids=lambda c: "-".join(map(str, c)))
 def test_linear_backward(case):
-    counts, K, N, ip, _, name, has_bias, _, gap = case
+    counts, K, N, ip, op, name, has_bias, _, gap = case
     g = torch.Generator().manual_seed(5)
     pk = packed(counts, max(N, 8))
-    a, dy = pk.buffer(g, K, ip), pk.buffer(g, N)
+    a, dy = pk.buffer(g, K, ip), pk.buffer(g, N, op)
     pre = pk.buffer(g, N) if name != "none" else None
     w = weights(g, 8, N, K, pk.dev, N * K + gap if gap else 0)
     da = pk.out(K, ip)
