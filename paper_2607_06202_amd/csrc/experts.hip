@@ -72,32 +72,30 @@ struct ForwardJob {
   static constexpr int kEsize = FP8 ? 1 : 2;
   struct Tile {
     int64_t t;
+    RowTile at;
     int e, row0, rows, col0, steps;
   };
   const ForwardArgs& p;
-  const RowTable& tab;
   int wave, lane, nt, steps;
-  int64_t total;
   LanePlace<S, GATED> at;
-  __device__ __forceinline__ ForwardJob(const ForwardArgs& p_, const RowTable& tab_, int wave_, int lane_)
-      : p(p_), tab(tab_), wave(wave_), lane(lane_), at(wave_, lane_) {
+  __device__ __forceinline__ ForwardJob(const ForwardArgs& p_, int wave_, int lane_)
+      : p(p_), wave(wave_), lane(lane_), at(wave_, lane_) {
     nt = (p.N + kCols - 1) / kCols;
     steps = S::steps(p.K * kEsize, FP8);
-    total = (int64_t)uniform(tab.mt[p.E]) * nt;
   }
   __device__ __forceinline__ bool place(Tile& t) const {
-    if (t.t >= total) return false;
+    if (!t.at.template find<S::BM>(p.expert_off, p.E, p.cap, t.t / nt, lane)) return false;
     int m, n;
-    t.e = uniform(quaternary_find(tab.mt, p.E, t.t / nt));
-    const int m0 = uniform(tab.mt[t.e]), beg = uniform(tab.off[t.e]), end = uniform(tab.off[t.e + 1]);
-    band_tile(t.t - (int64_t)m0 * nt, uniform(tab.mt[t.e + 1]) - m0, nt, 8, m, n);
-    t.row0 = beg + m * S::BM;
-    t.rows = std::min(end - t.row0, S::BM);
+    t.e = t.at.e;
+    band_tile(t.t - t.at.before * nt, t.at.count, nt, 8, m, n);
+    t.row0 = t.at.beg + m * S::BM;
+    t.rows = std::min(t.at.end - t.row0, S::BM);
     t.col0 = n * kCols;
     t.steps = steps;
     return true;
   }
   __device__ __forceinline__ bool first(Tile& t) const {
+    t = Tile{};
     t.t = xcd_slot(blockIdx.x, gridDim.x);
     return place(t);
   }
@@ -214,11 +212,9 @@ struct ForwardJob {
 
 template <class S, bool FP8, bool GATED>
 __global__ void __launch_bounds__(S::kThreads) forward_kernel(ForwardArgs p) {
-  __shared__ __attribute__((aligned(1024))) char tiles[S::STAGES * S::stage(FP8)];
-  __shared__ RowTable tab;
+  __shared__ __attribute__((aligned(1024))) char tiles[S::lds(FP8)];
   const int wave = uniform(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-  fill_row_table<S::BM>(p.expert_off, p.E, p.cap, tab);
-  ForwardJob<S, FP8, GATED> job(p, tab, wave, lane);
+  ForwardJob<S, FP8, GATED> job(p, wave, lane);
   run_tiles<S, false, false, FP8, GATED>(job, lds_addr(tiles), wave, lane);
 }
 
@@ -226,34 +222,33 @@ __global__ void __launch_bounds__(S::kThreads) forward_kernel(ForwardArgs p) {
 // dx[r] = sum over parts and n of d[r][part * N + n] w_part[e][n]: the reduction runs over the weights' rows.
 template <class S>
 struct RowGradJob {
+  static_assert(!S::RING, "turn() sets both operands up for one step");
   struct Tile {
     int64_t t;
+    RowTile at;
     int e, row0, rows, col0, steps;
   };
   const RowGradArgs& p;
-  const RowTable& tab;
   int wave, lane, nt, part_steps;
-  int64_t total;
   LanePlace<S> at;
-  __device__ __forceinline__ RowGradJob(const RowGradArgs& p_, const RowTable& tab_, int wave_, int lane_)
-      : p(p_), tab(tab_), wave(wave_), lane(lane_), at(wave_, lane_) {
+  __device__ __forceinline__ RowGradJob(const RowGradArgs& p_, int wave_, int lane_)
+      : p(p_), wave(wave_), lane(lane_), at(wave_, lane_) {
     nt = (p.K + S::BN - 1) / S::BN;
     part_steps = (p.N * 2 + S::STEP - 1) / S::STEP;
-    total = (int64_t)uniform(tab.mt[p.E]) * nt;
   }
   __device__ __forceinline__ bool place(Tile& t) const {
-    if (t.t >= total) return false;
+    if (!t.at.template find<S::BM>(p.expert_off, p.E, p.cap, t.t / nt, lane)) return false;
     int m, n;
-    t.e = uniform(quaternary_find(tab.mt, p.E, t.t / nt));
-    const int m0 = uniform(tab.mt[t.e]), beg = uniform(tab.off[t.e]), end = uniform(tab.off[t.e + 1]);
-    band_tile(t.t - (int64_t)m0 * nt, uniform(tab.mt[t.e + 1]) - m0, nt, 8, m, n);
-    t.row0 = beg + m * S::BM;
-    t.rows = std::min(end - t.row0, S::BM);
+    t.e = t.at.e;
+    band_tile(t.t - t.at.before * nt, t.at.count, nt, 8, m, n);
+    t.row0 = t.at.beg + m * S::BM;
+    t.rows = std::min(t.at.end - t.row0, S::BM);
     t.col0 = n * S::BN;
-    t.steps = S::steps(part_steps * p.parts * S::STEP, false);
+    t.steps = S::steps((int64_t)part_steps * p.parts * S::STEP, false);
     return true;
   }
   __device__ __forceinline__ bool first(Tile& t) const {
+    t = Tile{};
     t.t = xcd_slot(blockIdx.x, gridDim.x);
     return place(t);
   }
@@ -293,11 +288,9 @@ struct RowGradJob {
 
 template <class S>
 __global__ void __launch_bounds__(S::kThreads) row_grad_kernel(RowGradArgs p) {
-  __shared__ __attribute__((aligned(1024))) char tiles[S::STAGES * S::stage(false)];
-  __shared__ RowTable tab;
+  __shared__ __attribute__((aligned(1024))) char tiles[S::lds(false)];
   const int wave = uniform(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-  fill_row_table<S::BM>(p.expert_off, p.E, p.cap, tab);
-  RowGradJob<S> job(p, tab, wave, lane);
+  RowGradJob<S> job(p, wave, lane);
   run_tiles<S, false, true, false, false>(job, lds_addr(tiles), wave, lane);
 }
 
@@ -311,11 +304,10 @@ struct WeightGradJob {
     int e, part, m0, col0, beg, rows, steps;
   };
   const WeightGradArgs& p;
-  const RowTable& tab;
   int wave, lane, mt, nt;
   LanePlace<S> at;
-  __device__ __forceinline__ WeightGradJob(const WeightGradArgs& p_, const RowTable& tab_, int wave_, int lane_)
-      : p(p_), tab(tab_), wave(wave_), lane(lane_), at(wave_, lane_) {
+  __device__ __forceinline__ WeightGradJob(const WeightGradArgs& p_, int wave_, int lane_)
+      : p(p_), wave(wave_), lane(lane_), at(wave_, lane_) {
     mt = (p.N + S::BM - 1) / S::BM;
     nt = (p.K + S::BN - 1) / S::BN;
   }
@@ -324,16 +316,18 @@ struct WeightGradJob {
     if (t.t >= per * p.E) return false;
     int m, n;
     t.e = (int)(t.t / per);
-    t.beg = uniform(tab.off[t.e]);
-    t.rows = uniform(tab.off[t.e + 1]) - t.beg;
+    const int beg = std::min(std::max(p.expert_off[t.e], 0), p.cap);
+    t.beg = uniform(beg);
+    t.rows = uniform(std::min(std::max(p.expert_off[t.e + 1], beg), p.cap)) - t.beg;
     band_tile(t.t - t.e * per, mt * p.parts, nt, 8, m, n);
     t.part = m >= mt;
     t.m0 = (t.part ? m - mt : m) * S::BM;
     t.col0 = n * S::BN;
-    t.steps = S::steps(t.rows * 2, false);
+    t.steps = S::steps(t.rows * 2ll, false);
     return true;
   }
   __device__ __forceinline__ bool first(Tile& t) const {
+    t = Tile{};
     t.t = xcd_slot(blockIdx.x, gridDim.x);
     return place(t);
   }
@@ -367,11 +361,9 @@ struct WeightGradJob {
 
 template <class S>
 __global__ void __launch_bounds__(S::kThreads) weight_grad_kernel(WeightGradArgs p) {
-  __shared__ __attribute__((aligned(1024))) char tiles[S::STAGES * S::stage(false)];
-  __shared__ RowTable tab;
+  __shared__ __attribute__((aligned(1024))) char tiles[S::lds(false)];
   const int wave = uniform(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-  fill_row_table<0>(p.expert_off, p.E, p.cap, tab);
-  WeightGradJob<S> job(p, tab, wave, lane);
+  WeightGradJob<S> job(p, wave, lane);
   run_tiles<S, true, true, false, false>(job, lds_addr(tiles), wave, lane);
 }
 
@@ -474,7 +466,7 @@ __global__ void __launch_bounds__(256) pre_bias_grad_kernel(const char* dy, int6
 }
 
 // ---------------------------------------------------------------- launches
-using Big = Shape<256, 256, 2, 4, 128, 2>;
+using Big = Shape<256, 256, 2, 4, 128, 2, true>;
 using Mid = Shape<128, 256, 2, 4, 128, 3>;
 using Short = Shape<64, 256, 1, 4, 128, 3>;
 

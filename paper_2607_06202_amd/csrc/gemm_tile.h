@@ -166,18 +166,22 @@ __device__ __forceinline__ i32x4 read_cols(uint32_t addr) {
 }
 
 // BM x BN tile by WM x WN waves. MF x NF fragments of 16 x 16 per wave. STEP: reduction bytes of a row per step (64 or
-// 128; 128 for fp8); STAGES: steps that LDS holds.
-template <int BM_, int BN_, int WM_, int WN_, int STEP_, int STAGES_>
+// 128; 128 for fp8); STAGES: steps that LDS holds; RING: and half a step more (see run_tiles).
+template <int BM_, int BN_, int WM_, int WN_, int STEP_, int STAGES_, bool RING_ = false>
 struct Shape {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STEP = STEP_, STAGES = STAGES_;
+  static constexpr bool RING = RING_;
+  static constexpr int kFinal = RING ? 3 : STAGES;  // last steps of a tile, which load less or nothing
   static constexpr int kWaves = WM * WN, kThreads = kWaves * kWave;
   static constexpr int MF = BM / WM / 16, NF = BN / WN / 16;
   // A tile, B tile and (fp8) the scales of A's rows.
   static constexpr int stage(bool fp8) { return (BM + BN) * STEP + (fp8 ? 1024 : 0); }
+  static constexpr int lds(bool fp8) { return RING ? 5 * BM * STEP : STAGES * stage(fp8); }
+  static_assert(!RING || (BM == BN && STAGES == 2), "a ring of five equal operand tiles");
   static_assert(NF % 2 == 0, "fragments of B come in pairs");
   // Steps of a tile with n bytes of reduction: at least what LDS holds, and even where a step is one set of groups.
-  __host__ __device__ static constexpr int steps(int n, bool fp8) {
-    const int s = std::max((n + STEP - 1) / STEP, STAGES);
+  __host__ __device__ static constexpr int steps(int64_t n, bool fp8) {
+    const int s = std::max((int)((n + STEP - 1) / STEP), kFinal);
     return fp8 || STEP == 64 ? (s + 1) & ~1 : s;
   }
 };
@@ -191,15 +195,15 @@ __device__ __forceinline__ void static_for(F&& f) {
   }
 }
 
-// Fragments of one wave inside a stage (A tile first, then B).
+// Fragments of one wave inside the operands' tiles in LDS.
 //   SPLIT: the B tile's first half of rows are gate rows and its second half up rows; a wave takes the same
 //   columns of both: fragments 0..NF/2-1 are gate, the rest up.
 template <class S, bool ACOLS, bool BCOLS, bool SPLIT>
 struct Fragments {
   static constexpr int kStep = S::STEP, kPieces = kStep / 64;  // 16-byte pieces of a lane's row
   static constexpr int kA = ACOLS ? 4 : kPieces, kB = BCOLS ? S::NF / 2 : kPieces;
-  uint32_t a[kA], b[kB];    // offsets in a stage
-  uint32_t ra[kA], rb[kB];  // addresses in the stage being read
+  uint32_t a[kA], b[kB];    // offsets in an operand's tile
+  uint32_t ra[kA], rb[kB];  // addresses in the tiles being read
   static_assert(!BCOLS || (S::BN >= 128 && !SPLIT), "column swizzle of B");
   static_assert(!ACOLS || (S::MF >= 4 && S::BM >= 64), "column swizzle of A");
 
@@ -208,7 +212,6 @@ struct Fragments {
     const int m0 = (wave / S::WN) * S::MF * 16;
     const int n0 = (wave % S::WN) * S::NF * 16 / (SPLIT ? 2 : 1);
     const int kr = q * 8 + (rho >> 2);
-    const uint32_t bt = S::BM * kStep;
     const int key = kStep == 128 ? rho & 7 : (rho >> 1) & 3;  // the key of the rows this lane reads, in both operands
 #pragma unroll
     for (int i = 0; i < kA; ++i) {
@@ -220,20 +223,20 @@ struct Fragments {
 #pragma unroll
     for (int i = 0; i < kB; ++i) {
       if constexpr (!BCOLS)
-        b[i] = bt + (n0 + (rho >> 2) * 8 + (rho & 3)) * kStep + (((q + 4 * i) ^ key) * 16);
+        b[i] = (n0 + (rho >> 2) * 8 + (rho & 3)) * kStep + (((q + 4 * i) ^ key) * 16);
       else
-        b[i] = bt + kr * S::BN * 2 + (((n0 / 8 + i * 4 + (rho & 3)) ^ ((rho >> 2) * 4)) * 16);
+        b[i] = kr * S::BN * 2 + (((n0 / 8 + i * 4 + (rho & 3)) ^ ((rho >> 2) * 4)) * 16);
     }
   }
-  __device__ __forceinline__ void stage(uint32_t lds) {
+  __device__ __forceinline__ void point(uint32_t at_a, uint32_t at_b) {
 #pragma unroll
     for (int i = 0; i < kA; ++i) {
-      ra[i] = lds + a[i];
+      ra[i] = at_a + a[i];
       asm volatile("" : "+v"(ra[i]));
     }
 #pragma unroll
     for (int i = 0; i < kB; ++i) {
-      rb[i] = lds + b[i];
+      rb[i] = at_b + b[i];
       asm volatile("" : "+v"(rb[i]));
     }
   }
@@ -288,6 +291,11 @@ __device__ __forceinline__ void arrived(T& v) {
 // branch, and the last STAGES steps, which load nothing, are written out: a taken branch refetches instructions, which
 // costs as much as several products.
 //
+// What a compute unit gets out of its L2 is bounded by the lines it can have in flight, so the loads must not pause. Two
+// stages of a 256 x 256 tile are 128 KiB; while a step waits for the whole next stage nothing else is in flight, and a
+// step took as long as loading one (3100 cycles against 2048 of products). LDS has room for half a stage more: as a ring
+// of five operand tiles the row operand's loads run one step further ahead and stay in flight across the wait.
+//
 // The next tile's first steps are loaded before this one's results are worked out and stored. Loads and stores leave
 // one in-order counter, so the first steps of a tile wait for all but the stores behind their loads.
 template <class S, bool ACOLS, bool BCOLS, bool FP8, bool SPLIT, class Job>
@@ -303,6 +311,7 @@ __device__ __forceinline__ void run_tiles(Job& job, uint32_t lds, int wave, int 
   static_assert(kGroups % kRing == 0, "ring of row fragments");
   static_assert(!FP8 || (!ACOLS && !BCOLS && S::STEP == 128), "fp8 operands are rows of 128-element blocks");
   static_assert(kHalves == 2 || S::STAGES % 2 == 0 || S::STAGES == 3, "written-out steps alternate");
+  static_assert(!S::RING || kHalves == 2, "a ring holds bf16 steps of 128 bytes");
   Fragments<S, ACOLS, BCOLS, SPLIT> fr;
   fr.init(wave, lane);
   const uint32_t scale_at = A::kBytes + B::kBytes + ((wave / S::WN) * S::MF * 16 + (lane & 15)) * 4;
@@ -313,14 +322,22 @@ __device__ __forceinline__ void run_tiles(Job& job, uint32_t lds, int wave, int 
   f32x4 acc[S::MF][S::NF];
   int at = 0;  // steps of the tile being loaded
   typename Job::Tile tile;
-  const auto load = [&](uint32_t stage, auto i) EPL_INLINE {
-    if constexpr (i < A::kLoads)
-      a.template load<i>(stage, wave);
+  // Load i of a step, B's first, into the tiles at to_a and to_b (fp8: the scales behind them).
+  const auto load = [&](uint32_t to_a, uint32_t to_b, auto i) EPL_INLINE {
+    if constexpr (i < B::kLoads)
+      b.template load<i>(to_b, wave);
     else if constexpr (i < A::kLoads + B::kLoads)
-      b.template load<i - A::kLoads>(stage + A::kBytes, wave);
+      a.template load<i - B::kLoads>(to_a, wave);
     else if constexpr (FP8)
-      job.load_scales(tile, at - 1, stage + A::kBytes + B::kBytes);
+      job.load_scales(tile, at - 1, to_b + B::kBytes);
   };
+  // The operand tile n places on in the ring.
+  const auto ahead = [&](uint32_t at_tile, int n) EPL_INLINE {
+    const uint32_t t = at_tile + n * A::kBytes;
+    return t >= lds + 5 * A::kBytes ? t - 5 * A::kBytes : t;
+  };
+  // B's tile of the step whose A tile is at t.
+  const auto b_of = [&](uint32_t t) EPL_INLINE { return S::RING ? ahead(t, 1) : t + A::kBytes; };
   // Of the stage that fr points to: column fragment n of half h into fb[to]; the row fragment of group g.
   const auto read_b = [&](auto to, auto n, auto h) EPL_INLINE {
     if constexpr (FP8) {
@@ -343,29 +360,33 @@ __device__ __forceinline__ void run_tiles(Job& job, uint32_t lds, int wave, int 
   };
   using Zero = std::integral_constant<int, 0>;
   using One = std::integral_constant<int, 1>;
-  // The first reads of a stage: its column fragments (and row scales).
-  const auto open_stage = [&](auto to, uint32_t stage) EPL_INLINE {
-    fr.stage(stage);
-    static_for<0, S::NF>([&](auto n) EPL_INLINE { read_b(to, n, Zero{}); });
-    if constexpr (FP8) static_for<0, S::MF>([&](auto f) EPL_INLINE { read_scale(to, f, stage); });
-  };
-  // Set up a tile's operands and issue the loads of its first STAGES steps.
+  // Set up a tile's operands and issue the loads of its first steps: STAGES of them, and the next one's A in a ring.
   const auto begin_tile = [&]() EPL_INLINE {
     job.begin(tile, a, b);
     at = 1;
     static_for<0, S::STAGES>([&](auto i) EPL_INLINE {
-      static_for<0, kLoads>([&](auto j) EPL_INLINE { load(lds + i * kStage, j); });
+      const uint32_t t = lds + i * kStage;
+      if constexpr (S::RING) {  // in the ring's order
+        static_for<0, A::kLoads>([&](auto j) EPL_INLINE { a.template load<j>(t, wave); });
+        static_for<0, B::kLoads>([&](auto j) EPL_INLINE { b.template load<j>(t + A::kBytes, wave); });
+      } else {
+        static_for<0, kLoads>([&](auto j) EPL_INLINE { load(t, t + A::kBytes, j); });
+      }
       job.turn(tile, at, a, b);
       ++at;
     });
+    if constexpr (S::RING) static_for<0, A::kLoads>([&](auto j) EPL_INLINE { a.template load<j>(lds + 4 * A::kBytes, wave); });
   };
 
-  uint32_t cur = lds;  // stage of the current step
+  uint32_t cur = lds;  // A's tile of the current step
   int stored = 0;  // steps still to come whose loads are in front of the previous tile's stores
-  // One step. par: its parity. left: steps of the tile after it, or STAGES if this stage is loaded again.
+  // One step. par: its parity. left: steps of the tile after it, kFinal for that many or more.
   const auto step = [&](auto par, auto left) EPL_INLINE {
-    const uint32_t here = cur;
-    cur = cur == lds + (S::STAGES - 1) * kStage ? lds : cur + kStage;
+    const uint32_t here = cur, here_b = b_of(cur);
+    if constexpr (S::RING)
+      cur = ahead(cur, 2);
+    else
+      cur = cur == lds + (S::STAGES - 1) * kStage ? lds : cur + kStage;
     static_for<0, kGroups>([&](auto g) EPL_INLINE {
       constexpr int m = g % S::MF, bi = kHalves == 2 ? g / S::MF : par;
       if constexpr (g == kTail) {
@@ -374,8 +395,9 @@ __device__ __forceinline__ void run_tiles(Job& job, uint32_t lds, int wave, int 
         static_for<0, kAhead>([&](auto i) EPL_INLINE { arrived(fa[(g + i) % kRing]); });
         if constexpr (kHalves == 2) static_for<0, S::NF>([&](auto n) EPL_INLINE { arrived(fb[1][n]); });
         if constexpr (left > 0) {
-          job.template wait<kLoads * std::min(kLater, left - 1)>(stored > 0);
-          fr.stage(cur);
+          constexpr int behind = S::RING ? (left > 1 ? A::kLoads : 0) : kLoads * std::min(kLater, left - 1);
+          job.template wait<behind>(stored > 0);
+          fr.point(cur, b_of(cur));
         }
       }
       static_for<0, S::NF>([&](auto n) EPL_INLINE {
@@ -408,23 +430,25 @@ __device__ __forceinline__ void run_tiles(Job& job, uint32_t lds, int wave, int 
           if constexpr (g == kTail + 2 && n == 0) read_a(std::integral_constant<int, 2>{});
           if constexpr (FP8 && slot == S::NF)
             static_for<0, S::MF>([&](auto f) EPL_INLINE { read_scale(std::integral_constant<int, to>{}, f, cur); });
-          if constexpr (left == S::STAGES) {
-            constexpr int per = (kLoads + kSlots - 1) / kSlots, begin = kSlots - (kLoads + per - 1) / per;
+          // The freed tiles: in a ring they take B of the step after the next and then A of the one behind it.
+          constexpr int issue = left == S::kFinal ? kLoads : S::RING && left == 2 ? B::kLoads : 0;
+          if constexpr (issue > 0) {
+            constexpr int per = (issue + kSlots - 1) / kSlots, begin = kSlots - (issue + per - 1) / per;
             if constexpr (slot >= begin)
-              static_for<(slot - begin) * per, std::min((slot - begin + 1) * per, kLoads)>(
-                  [&](auto i) EPL_INLINE { load(here, i); });
+              static_for<(slot - begin) * per, std::min((slot - begin + 1) * per, issue)>(
+                  [&](auto i) EPL_INLINE { load(S::RING ? here_b : here, S::RING ? here : here_b, i); });
           }
         }
       });
       __builtin_amdgcn_sched_barrier(0);
     });
     stored -= stored > 0;
-    if constexpr (left == S::STAGES) {
+    if constexpr (left == S::kFinal) {
       job.turn(tile, at, a, b);
       ++at;
     }
   };
-  using Middle = std::integral_constant<int, S::STAGES>;
+  using Middle = std::integral_constant<int, S::kFinal>;
 
   if (!job.first(tile)) return;
   begin_tile();
@@ -433,21 +457,23 @@ __device__ __forceinline__ void run_tiles(Job& job, uint32_t lds, int wave, int 
     for (int m = 0; m < S::MF; ++m)
 #pragma unroll
       for (int n = 0; n < S::NF; ++n) acc[m][n] = f32x4{0, 0, 0, 0};
-    job.template wait<kLoads*(S::STAGES - 1)>(stored > 0);
+    job.template wait<S::RING ? 2 * A::kLoads + B::kLoads : kLoads*(S::STAGES - 1)>(stored > 0);
     cur = lds;
-    open_stage(Zero{}, cur);
+    fr.point(cur, b_of(cur));
+    static_for<0, S::NF>([&](auto n) EPL_INLINE { read_b(Zero{}, n, Zero{}); });
+    if constexpr (FP8) static_for<0, S::MF>([&](auto f) EPL_INLINE { read_scale(Zero{}, f, cur); });
     static_for<0, kAhead>(read_a);
     constexpr int kOdd = kHalves == 2 ? 0 : S::STAGES % 2;  // an odd number of written-out steps
     if constexpr (kOdd) {
       if (tile.steps > S::STAGES) step(Zero{}, Middle{});
     }
-    for (int s = tile.steps - S::STAGES - kOdd; s > 0; s -= kHalves == 2 ? 1 : 2) {
+    for (int s = tile.steps - S::kFinal - kOdd; s > 0; s -= kHalves == 2 ? 1 : 2) {
       step(std::integral_constant<int, kHalves == 2 ? 0 : kOdd>{}, Middle{});
       if constexpr (kHalves == 1) step(std::integral_constant<int, 1 - kOdd>{}, Middle{});
     }
-    static_for<0, S::STAGES>([&](auto i) EPL_INLINE {
+    static_for<0, S::kFinal>([&](auto i) EPL_INLINE {
       step(std::integral_constant<int, kHalves == 2 ? 0 : (kOdd + i) % 2>{},
-           std::integral_constant<int, S::STAGES - 1 - i>{});
+           std::integral_constant<int, S::kFinal - 1 - i>{});
     });
     const typename Job::Tile done = tile;
     const bool more = job.next(tile);
@@ -460,42 +486,38 @@ __device__ __forceinline__ void run_tiles(Job& job, uint32_t lds, int wave, int 
 }
 
 // ---------------------------------------------------------------- tiles over the experts' rows
-// The experts' row offsets, clipped, and the number of row tiles before each, in LDS.
-struct RowTable {
-  int off[EPL_MAX_EXPERTS + 1];  // expert e: rows [off[e], end(e))
-  int mt[EPL_MAX_EXPERTS + 1];
-};
+// Where a row tile lies: expert e, its rows [beg, end), the row tiles before it and its own.
+struct RowTile {
+  int e = 0, beg = 0, end = 0;
+  int64_t before = 0;
+  int count = 0;
+  int64_t chunk_before = 0;  // row tiles before e's group of 64 experts
 
-// Fills the table (BM rows a tile; 0: offsets alone); returns after a barrier. The clipped offsets are made
-// monotonic by a running maximum, so that expert e's rows are [off[e], off[e + 1]).
-template <int BM>
-__device__ __forceinline__ void fill_row_table(const int32_t* expert_off, int E, int cap, RowTable& tab) {
-  if (threadIdx.x < kWave) {
-    const int lane = threadIdx.x;
-    int carry = 0, top = 0;
-    for (int e0 = 0; e0 <= E; e0 += kWave) {
-      const int e = e0 + lane;
-      int o = e <= E ? std::min(std::max(expert_off[e], 0), cap) : 0;
-#pragma unroll
-      for (int d = 1; d < kWave; d <<= 1) {
-        const int v = __shfl_up(o, d, kWave);
-        if (lane >= d) o = std::max(o, v);
+  // Finds row tile m (BM rows a tile), not before the one found last; false past the last one. A wave works it out from
+  // the offsets, 64 experts at a time, from the group where it last was: a table in LDS would cost the room of the
+  // ring. Offsets are clipped to the buffer, so that whatever they hold, no access leaves it.
+  template <int BM>
+  __device__ __forceinline__ bool find(const int32_t* expert_off, int E, int cap, int64_t m, int lane) {
+    for (int e0 = e & ~(kWave - 1); e0 < E; e0 += kWave) {
+      const int mine = std::min(e0 + lane, E - 1);
+      const int b0 = std::min(std::max(expert_off[mine], 0), cap), b1 = std::min(std::max(expert_off[mine + 1], b0), cap);
+      const uint32_t n = e0 + lane < E ? (uint32_t)(b1 - b0 + BM - 1) / BM : 0u;
+      const uint32_t sum = (uint32_t)wave_inclusive_sum((int)n);
+      const uint64_t past = __ballot(chunk_before + sum > m);
+      if (past) {
+        const int l = __builtin_ctzll(past);
+        e = e0 + l;
+        beg = __builtin_amdgcn_readlane(b0, l);
+        end = __builtin_amdgcn_readlane(b1, l);
+        count = __builtin_amdgcn_readlane((int)n, l);
+        before = chunk_before + (uint32_t)__builtin_amdgcn_readlane((int)sum, l) - (uint32_t)count;
+        return true;
       }
-      o = std::max(o, top);
-      if (e <= E) tab.off[e] = o;
-      if constexpr (BM > 0) {
-        int before = __shfl_up(o, 1, kWave);  // the offset before this one
-        if (lane == 0) before = top;
-        const int n = e > 0 && e <= E ? (o - before + BM - 1) / BM : 0;  // row tiles of expert e - 1
-        const int inc = wave_inclusive_sum(n) + carry;
-        if (e <= E) tab.mt[e] = inc;
-        carry = __shfl(inc, kWave - 1, kWave);
-      }
-      top = __shfl(o, kWave - 1, kWave);
+      chunk_before += (uint32_t)__builtin_amdgcn_readlane((int)sum, kWave - 1);
     }
+    return false;
   }
-  __syncthreads();
-}
+};
 
 // Workgroup -> slot in the current round of tiles: consecutive slots share operands, and consecutive workgroups
 // go to different XCDs, so each XCD (its own L2) takes a run of gridDim / 8 slots.
