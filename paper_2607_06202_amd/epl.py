@@ -877,6 +877,8 @@ def _matrices(t, name: str, dtype, cfg: Config, shape=None) -> int:
             name, cfg.num_experts, "out, in" if shape is None else "%d, %d" % tuple(shape), tuple(t.shape)))
     if t.stride(2) != 1 or t.stride(1) != t.shape[2]:
         raise ValueError("%s: each expert's matrix must be contiguous, got strides %s" % (name, t.stride()))
+    if t.shape[0] > 1 and t.stride(0) < t.shape[1] * t.shape[2]:  # an expanded or overlapping view; 0 means packed in C
+        raise ValueError("%s: the experts' matrices overlap, got strides %s" % (name, t.stride()))
     return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
 
 

@@ -270,3 +270,148 @@ def test_linear_forward_fp8():
         y = v.clamp_min(0)
         assert_within(out[r0:r1], y, rounded(y, err), "out")
     pk.assert_untouched(out, "out")
+
+
+def test_residual_in_place():
+    g = torch.Generator().manual_seed(7)
+    for counts, K, N in (("edges", 136, 264), ("one_token", 64, 72)):
+        pk = packed(counts, N)
+        a, w, res = pk.buffer(g, K), weights(g, 8, N, K, pk.dev), pk.buffer(g, N)
+        want, _ = epl.experts_linear(pk.cfg, a, pk.L, w, residual=res)
+        out = res.clone()
+        epl.experts_linear(pk.cfg, a, pk.L, w, residual=out, out=out)
+        torch.cuda.synchronize()
+        assert torch.equal(out[: pk.P], want[: pk.P])
+
+
+def test_many_rows_take_the_large_tiles():
+    """1024 rows an expert and more run on 256 x 256 tiles: odd features and ragged counts there too."""
+    g = torch.Generator().manual_seed(8)
+    rng = np.random.default_rng(8)
+    counts = [1030, 1281, 777, 1200]
+    pk = Packed(routing_of_counts(counts, 4, 2, rng), 4, 264, device())
+    assert pk.rows // 4 >= 1024
+    x, wg, wu = pk.buffer(g, 264), weights(g, 4, 152, 264, pk.dev), weights(g, 4, 152, 264, pk.dev)
+    h, pre = pk.out(152), pk.out(304)
+    epl.experts_gated(pk.cfg, x, pk.L, wg, wu, "silu", h=h, pre=pre)
+    wd, bias, res = weights(g, 4, 264, 152, pk.dev), torch.randn(4, 264, generator=g).bfloat16().to(pk.dev), pk.buffer(g, 264)
+    a = pk.buffer(g, 152)
+    out = pk.out(264)
+    epl.experts_linear(pk.cfg, a, pk.L, wd, bias, res, "none", out=out)
+    torch.cuda.synchronize()
+    want, bound, wpre, pbound = gated_reference(pk, x[: pk.P].cpu().double(), wg.cpu().double(), wu.cpu().double(), "silu")
+    assert_within(h[: pk.P], want, bound, "h")
+    assert_within(pre[: pk.P], wpre, pbound, "pre")
+    ad, wd = a.cpu().double(), wd.cpu().double()
+    for e, r0, r1 in pk.experts():
+        b, r = bias[e].cpu().double(), res[r0:r1].cpu().double()
+        y = ad[r0:r1] @ wd[e].T + b + r
+        err = sum_error(152 + 2, ad[r0:r1].abs() @ wd[e].abs().T) + FEW * (y.abs() + b.abs() + r.abs())
+        assert_within(out[r0:r1], y, rounded(y, err), "out")
+    pk.assert_untouched(out, "out")
+
+
+def test_fp8_many_rows():
+    """256 rows an expert and more take the 128-row tiles; fewer the 64-row ones."""
+    g = torch.Generator().manual_seed(10)
+    rng = np.random.default_rng(10)
+    pk = Packed(routing_of_counts([300, 270, 1, 510], 4, 1, rng), 4, 384, device(), payload="fp8")
+    q, s = quantise_rows(torch.randn(pk.rows, 384, generator=g))
+    qg, sg = quantise_weights(torch.randn(4, 136, 384, generator=g) * 384 ** -0.5)
+    qu, su = quantise_weights(torch.randn(4, 136, 384, generator=g) * 384 ** -0.5)
+    d = pk.dev
+    h, pre = pk.out(136), pk.out(272)
+    epl.experts_gated(pk.cfg, q.to(d), pk.L, qg.to(d), qu.to(d), "silu", s.to(d), sg.to(d), su.to(d), h, pre)
+    torch.cuda.synchronize()
+    want, bound, wpre, pbound = gated_reference(pk, dequantise_rows(q, s), dequantise_weights(qg, sg),
+                                                dequantise_weights(qu, su), "silu")
+    assert_within(h[: pk.P], want, bound, "h")
+    assert_within(pre[: pk.P], wpre, pbound, "pre")
+
+
+def test_offsets_that_hold_anything_stay_in_the_buffers():
+    """expert_off is read on the device: whatever it holds, the rows read and written are the buffer's own."""
+    g = torch.Generator().manual_seed(11)
+    pk = packed("edges", 64)
+    x, wg, wu = pk.buffer(g, 64), weights(g, 8, 64, 64, pk.dev), weights(g, 8, 64, 64, pk.dev)
+    x.nan_to_num_(0.0)
+    guard = torch.full((3 * pk.rows, 64), 77.0, dtype=torch.bfloat16, device=pk.dev)
+    h = guard[pk.rows:2 * pk.rows]
+    for off in ([-5] * 9, [2 ** 31 - 1] * 9, [0, 10 ** 9, 5, -7, 3, 2 ** 31 - 1, 0, 1, 10 ** 9], list(range(900, 0, -100))):
+        pk.L.expert_off.copy_(torch.tensor(off, dtype=torch.int32))
+        epl.experts_gated(pk.cfg, x, pk.L, wg, wu, h=h)
+        dpre = torch.zeros(pk.rows, 128, dtype=torch.bfloat16, device=pk.dev)
+        epl.experts_gated_backward(pk.cfg, x, dpre, x, pk.L, wg, wu, drecv=h)
+        torch.cuda.synchronize()
+        assert bool((guard[: pk.rows] == 77.0).all()) and bool((guard[2 * pk.rows:] == 77.0).all())
+
+
+@pytest.mark.parametrize("E", [65, 200, 1024])
+def test_many_experts_mostly_empty(E):
+    """Row tiles are found 64 experts at a time: rows in the first and last expert of each group, none in most."""
+    g = torch.Generator().manual_seed(E)
+    rng = np.random.default_rng(E)
+    counts = [0] * E
+    for e in {0, 1, 63, 64, E - 1, E // 2, min(128, E - 1), min(191, E - 1)}:
+        counts[e] = int(rng.integers(1, 150))
+    pk = Packed(routing_of_counts(counts, E, 2, rng), E, 64, device())
+    x, wg, wu = pk.buffer(g, 64), weights(g, E, 72, 64, pk.dev), weights(g, E, 72, 64, pk.dev)
+    h, pre = epl.experts_gated(pk.cfg, x, pk.L, wg, wu, keep_pre=True)
+    dh = pk.buffer(g, 72)
+    dx, dwg, dwu = epl.experts_gated_backward(pk.cfg, dh, pre, x, pk.L, wg, wu)
+    torch.cuda.synchronize()
+    want, bound, wpre, pbound = gated_reference(pk, x[: pk.P].cpu().double(), wg.cpu().double(), wu.cpu().double(), "silu")
+    assert_within(h[: pk.P], want, bound, "h")
+    assert_within(pre[: pk.P], wpre, pbound, "pre")
+    p, d, xd = pre.cpu().double(), dh.cpu().double(), x.cpu().double()
+    for e, a, b in pk.experts():
+        if a == b:
+            assert not dwg[e].any() and not dwu[e].any(), e
+            continue
+        gg, u = p[a:b, :72], p[a:b, 72:]
+        dg, du = d[a:b] * u * act_grad("silu", gg), d[a:b] * act("silu", gg)
+        eg, eu = rounded(dg, FEW * (d[a:b] * u).abs() * SLOPE), rounded(du, FEW * (d[a:b] * gg).abs())
+        w = (wg[e].cpu().double(), wu[e].cpu().double())
+        want = dg @ w[0] + du @ w[1]
+        err = eg @ w[0].abs() + eu @ w[1].abs() + sum_error(146, (dg.abs() + eg) @ w[0].abs() + (du.abs() + eu) @ w[1].abs())
+        assert_within(dx[a:b], want, rounded(want, err), "drecv")
+        want = dg.T @ xd[a:b]
+        err = eg.T @ xd[a:b].abs() + sum_error(b - a + 2, (dg.abs() + eg).T @ xd[a:b].abs())
+        assert_within(dwg[e], want, rounded(want, err), "dw_gate")
+
+
+def test_no_tokens():
+    """No rows at all: nothing to do forward, zero gradients of the weights backward."""
+    dev = device()
+    cfg = epl.config(2, 4, 2, 64, 0)
+    L = epl.layout(cfg, torch.empty(0, 2, dtype=torch.int32, device=dev))
+    x = torch.empty(0, 64, dtype=torch.bfloat16, device=dev)
+    g = torch.Generator().manual_seed(1)
+    w = weights(g, 4, 32, 64, dev)
+    h, pre = epl.experts_gated(cfg, x, L, w, w, keep_pre=True)
+    _, dwg, dwu = epl.experts_gated_backward(cfg, h, pre, x, L, w, w)
+    y, _ = epl.experts_linear(cfg, x, L, w)
+    _, dw, db = epl.experts_linear_backward(cfg, y, x, L, w, need_dbias=True)
+    torch.cuda.synchronize()
+    assert not dwg.any() and not dwu.any() and not dw.any() and not db.any()
+
+
+def test_refused_tensors():
+    """What the binding refuses before a launch: overlapping matrices, short buffers, wrong pitches and types."""
+    g = torch.Generator().manual_seed(2)
+    pk = packed("few", 64)
+    x, w = pk.buffer(g, 64), weights(g, 8, 32, 64, pk.dev)
+    with pytest.raises(ValueError, match="overlap"):
+        epl.experts_gated(pk.cfg, x, pk.L, w[:1].expand(8, 32, 64), w[:1].expand(8, 32, 64))
+    with pytest.raises(ValueError, match="rows"):
+        epl.experts_gated(pk.cfg, x[:-1], pk.L, w, w)
+    with pytest.raises(ValueError, match="apart"):
+        epl.experts_gated(pk.cfg, pk.buffer(g, 64, 128), pk.L, w, w)
+    with pytest.raises(ValueError, match="contiguous"):
+        epl.experts_linear(pk.cfg, x, pk.L, w.transpose(1, 2))
+    with pytest.raises(ValueError):
+        epl.experts_linear(pk.cfg, x.float(), pk.L, w)
+    with pytest.raises(epl.EplError, match="ALIGN"):
+        epl.experts_linear(pk.cfg, x, pk.L, w, bias=torch.zeros(8 * 32 + 1, dtype=torch.bfloat16, device=pk.dev)[1:].view(8, 32))
+    with pytest.raises(epl.EplError, match="INVALID"):
+        epl.experts_gated_backward(pk.cfg, pk.buffer(g, 32), pk.buffer(g, 64), x, pk.L, w, w, drecv=x)
