@@ -119,7 +119,8 @@ struct ForwardJob {
   __device__ __forceinline__ void load_scales(const Tile& t, int step, uint32_t lds) const {
     constexpr int kSpans = S::BM / kWave;
     const int span = wave % kSpans * kWave, nb = p.K / 128;
-    const u32x4 rs = make_rsrc((uint64_t)(p.a_scale + (int64_t)t.row0 * nb + step), step < nb ? ((int64_t)(t.rows - 1) * nb + 1) * 4 : 0);
+    const int64_t bytes = step < nb ? ((int64_t)(t.rows - 1) * nb + 1) * 4 : 0;
+    const u32x4 rs = make_rsrc((uint64_t)(p.a_scale + (int64_t)t.row0 * nb + step), bytes);
     load_words_to_lds(rs, lds + span * 4, (span + lane) * nb * 4);
   }
   template <int N>
@@ -234,7 +235,7 @@ struct RowGradJob {
   __device__ __forceinline__ RowGradJob(const RowGradArgs& p_, int wave_, int lane_)
       : p(p_), wave(wave_), lane(lane_), at(wave_, lane_) {
     nt = (p.K + S::BN - 1) / S::BN;
-    part_steps = (p.N * 2 + S::STEP - 1) / S::STEP;
+    part_steps = (p.N * 2 + kStepBytes - 1) / kStepBytes;
   }
   __device__ __forceinline__ bool place(Tile& t) const {
     if (!t.at.template find<S::BM>(p.expert_off, p.E, p.cap, t.t / nt, lane)) return false;
@@ -244,7 +245,7 @@ struct RowGradJob {
     t.row0 = t.at.beg + m * S::BM;
     t.rows = std::min(t.at.end - t.row0, S::BM);
     t.col0 = n * S::BN;
-    t.steps = S::steps((int64_t)part_steps * p.parts * S::STEP, false);
+    t.steps = S::steps((int64_t)part_steps * p.parts * kStepBytes, false);
     return true;
   }
   __device__ __forceinline__ bool first(Tile& t) const {
@@ -466,9 +467,9 @@ __global__ void __launch_bounds__(256) pre_bias_grad_kernel(const char* dy, int6
 }
 
 // ---------------------------------------------------------------- launches
-using Big = Shape<256, 256, 2, 4, 128, 2, true>;
-using Mid = Shape<128, 256, 2, 4, 128, 3>;
-using Short = Shape<64, 256, 1, 4, 128, 3>;
+using Big = Shape<256, 256, 2, 4, 2, true>;
+using Mid = Shape<128, 256, 2, 4, 3>;
+using Short = Shape<64, 256, 1, 4, 3>;
 
 static unsigned persistent_grid(int64_t tiles, int per_cu) {
   return (unsigned)std::min<int64_t>(tiles, (int64_t)kCus * per_cu);

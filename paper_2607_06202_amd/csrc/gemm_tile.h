@@ -1,9 +1,10 @@
 // Matrix-instruction tile shared by the experts' products (device only).
 //
 // A workgroup computes a BM x BN tile of D = A * B^T with 64-wide waves in a WM x WN arrangement. Both
-// operands pass through LDS in steps of 64 or 128 bytes of the reduction (32 or 64 bf16, 128 E4M3 elements), and each may be stored either way round in memory:
-//   * reduction-contiguous ("rows"): LDS holds [rows][step bytes]; a lane reads 16 bytes of its row;
-//   * reduction-major ("columns"):   LDS holds [reduction rows][columns]; a lane reads two 4x16 blocks that
+// operands pass through LDS in steps of 128 bytes of the reduction (64 bf16 or 128 E4M3 elements), and each may be
+// stored either way round in memory:
+//   * reduction-contiguous ("rows"): LDS holds [rows][128 bytes]; a lane reads 16 bytes of its row;
+//   * reduction-major ("columns"):   LDS holds [64 reduction rows][columns]; a lane reads two 4x16 blocks that
 //     the transposing LDS read turns to its own column (ds_read_b64_tr_b16).
 // Either way a lane ends up with the same eight reduction elements of one row, so the two mix freely: forward
 // (rows x rows), input gradient (rows x columns) and weight gradient (columns x columns) are one loop.
@@ -33,6 +34,7 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 // Lambdas over register arrays: out of line they would put the arrays in memory.
 #define EPL_INLINE __attribute__((always_inline))
 
+constexpr int kStepBytes = 128;       // reduction bytes of a row per step: 64 bf16 or 128 E4M3 elements
 constexpr int kOutOfRange = INT_MIN;  // as an unsigned offset, past every descriptor below 2 GiB
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
@@ -57,7 +59,7 @@ __device__ __forceinline__ void load_to_lds(u32x4 rsrc, uint32_t lds, int voff) 
       "s_nop 0\n\t"
       "buffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(uniform((int)lds)),
       "v"(voff), "s"(rsrc)
-      : "memory");
+      : "memory", "m0");
 }
 
 // 64 lanes x 4 bytes, the same way.
@@ -67,20 +69,19 @@ __device__ __forceinline__ void load_words_to_lds(u32x4 rsrc, uint32_t lds, int 
       "s_nop 0\n\t"
       "buffer_load_dword %1, %2, 0 offen lds" ::"s"(uniform((int)lds)),
       "v"(voff), "s"(rsrc)
-      : "memory");
+      : "memory", "m0");
 }
 
 // One operand's stream of steps. Wave-uniform except the lane's offsets.
 //   COLS: reduction-major in memory (reduction rows ld bytes apart, columns contiguous);
-//   ROWS: rows (columns) of the tile; NW waves share its loads; STEP: reduction bytes of a row per step; B: the B
-//   operand's swizzle key.
+//   ROWS: rows (columns) of the tile; NW waves share its loads; B: the B operand's swizzle key.
 // A second base serves a tile whose second half of rows comes from another matrix (gate and up projections).
-template <bool COLS, int ROWS, int NW, int STEP, bool B, bool SPLIT = false>
+template <bool COLS, int ROWS, int NW, bool B, bool SPLIT = false>
 struct Operand {
-  static constexpr int kBytes = ROWS * STEP;
+  static constexpr int kBytes = ROWS * kStepBytes;
   static constexpr int kLoads = kBytes / 1024 / NW;  // per wave and step
   static_assert(kLoads >= 1 && kLoads * NW * 1024 == kBytes, "tile not a whole number of loads");
-  static constexpr int kRowsPerLoad = 1024 / STEP, kSlots = STEP / 16;
+  static constexpr int kRowsPerLoad = 1024 / kStepBytes, kSlots = kStepBytes / 16;
 
   uint64_t base, base2;
   int64_t bytes;
@@ -91,10 +92,7 @@ struct Operand {
 
   // The slot of a row's piece c is c ^ key(row), so that the rows that lanes read together meet different banks.
   static __device__ __forceinline__ int key(int row) {
-    if constexpr (STEP == 64)
-      return B ? ((row >> 1) & 1) | ((row >> 2) & 2) : (row >> 1) & 3;
-    else
-      return B ? (row & 3) | ((row >> 1) & 4) : row & 7;
+    return B ? (row & 3) | ((row >> 1) & 4) : row & 7;
   }
   // rows: `n` valid rows ld bytes apart. columns: `n` valid columns (of 2 bytes), reduction rows ld bytes apart.
   __device__ __forceinline__ void lanes(int n, int64_t ld, int wave, int lane) {
@@ -121,7 +119,7 @@ struct Operand {
     base = (uint64_t)p;
     base2 = (uint64_t)p2;
     bytes = n <= 0 ? 0 : (n - 1) * ld + kbytes;
-    step = STEP;
+    step = kStepBytes;
     left = kbytes;
   }
   // k reduction rows, n columns
@@ -129,7 +127,7 @@ struct Operand {
     base = (uint64_t)p;
     base2 = 0;
     bytes = k <= 0 ? 0 : (k - 1) * ld + n * 2;
-    step = STEP / 2 * ld;
+    step = kStepBytes / 2 * ld;
     left = 0;
   }
   // Load I of the next step into the tile at lds; the last one moves on to the step after.
@@ -143,7 +141,7 @@ struct Operand {
       base += step;
       if constexpr (SPLIT) base2 += step;
       bytes -= step;
-      left -= STEP;
+      left -= kStepBytes;
     }
   }
 };
@@ -165,24 +163,25 @@ __device__ __forceinline__ i32x4 read_cols(uint32_t addr) {
   return i32x4{a[0], a[1], b[0], b[1]};
 }
 
-// BM x BN tile by WM x WN waves. MF x NF fragments of 16 x 16 per wave. STEP: reduction bytes of a row per step (64 or
-// 128; 128 for fp8); STAGES: steps that LDS holds; RING: and half a step more (see run_tiles).
-template <int BM_, int BN_, int WM_, int WN_, int STEP_, int STAGES_, bool RING_ = false>
+// BM x BN tile by WM x WN waves. MF x NF fragments of 16 x 16 per wave. STAGES: steps that LDS holds; RING: and half a
+// step more (see run_tiles).
+template <int BM_, int BN_, int WM_, int WN_, int STAGES_, bool RING_ = false>
 struct Shape {
-  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STEP = STEP_, STAGES = STAGES_;
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_;
   static constexpr bool RING = RING_;
   static constexpr int kFinal = RING ? 3 : STAGES;  // last steps of a tile, which load less or nothing
   static constexpr int kWaves = WM * WN, kThreads = kWaves * kWave;
   static constexpr int MF = BM / WM / 16, NF = BN / WN / 16;
   // A tile, B tile and (fp8) the scales of A's rows.
-  static constexpr int stage(bool fp8) { return (BM + BN) * STEP + (fp8 ? 1024 : 0); }
-  static constexpr int lds(bool fp8) { return RING ? 5 * BM * STEP : STAGES * stage(fp8); }
+  static constexpr int stage(bool fp8) { return (BM + BN) * kStepBytes + (fp8 ? 1024 : 0); }
+  static constexpr int lds(bool fp8) { return RING ? 5 * BM * kStepBytes : STAGES * stage(fp8); }
   static_assert(!RING || (BM == BN && STAGES == 2), "a ring of five equal operand tiles");
   static_assert(NF % 2 == 0, "fragments of B come in pairs");
-  // Steps of a tile with n bytes of reduction: at least what LDS holds, and even where a step is one set of groups.
+  // Steps of a tile with n bytes of reduction: at least those that are written out, and even for fp8, where a step is one
+  // set of groups and the column fragments of successive steps alternate.
   __host__ __device__ static constexpr int steps(int64_t n, bool fp8) {
-    const int s = std::max((int)((n + STEP - 1) / STEP), kFinal);
-    return fp8 || STEP == 64 ? (s + 1) & ~1 : s;
+    const int s = std::max((int)((n + kStepBytes - 1) / kStepBytes), kFinal);
+    return fp8 ? (s + 1) & ~1 : s;
   }
 };
 
@@ -200,7 +199,7 @@ __device__ __forceinline__ void static_for(F&& f) {
 //   columns of both: fragments 0..NF/2-1 are gate, the rest up.
 template <class S, bool ACOLS, bool BCOLS, bool SPLIT>
 struct Fragments {
-  static constexpr int kStep = S::STEP, kPieces = kStep / 64;  // 16-byte pieces of a lane's row
+  static constexpr int kStep = kStepBytes, kPieces = 2;  // 16-byte pieces of a lane's row
   static constexpr int kA = ACOLS ? 4 : kPieces, kB = BCOLS ? S::NF / 2 : kPieces;
   uint32_t a[kA], b[kB];    // offsets in an operand's tile
   uint32_t ra[kA], rb[kB];  // addresses in the tiles being read
@@ -212,7 +211,7 @@ struct Fragments {
     const int m0 = (wave / S::WN) * S::MF * 16;
     const int n0 = (wave % S::WN) * S::NF * 16 / (SPLIT ? 2 : 1);
     const int kr = q * 8 + (rho >> 2);
-    const int key = kStep == 128 ? rho & 7 : (rho >> 1) & 3;  // the key of the rows this lane reads, in both operands
+    const int key = rho & 7;  // the key of the rows this lane reads, in both operands
 #pragma unroll
     for (int i = 0; i < kA; ++i) {
       if constexpr (!ACOLS)
@@ -301,16 +300,16 @@ __device__ __forceinline__ void arrived(T& v) {
 template <class S, bool ACOLS, bool BCOLS, bool FP8, bool SPLIT, class Job>
 __device__ __forceinline__ void run_tiles(Job& job, uint32_t lds, int wave, int lane) {
   constexpr int kStage = S::stage(FP8);
-  using A = Operand<ACOLS, S::BM, S::kWaves, S::STEP, false>;
-  using B = Operand<BCOLS, S::BN, S::kWaves, S::STEP, true, SPLIT>;
+  using A = Operand<ACOLS, S::BM, S::kWaves, false>;
+  using B = Operand<BCOLS, S::BN, S::kWaves, true, SPLIT>;
   using Frag = std::conditional_t<FP8, i32x8, i32x4>;
-  constexpr int kHalves = FP8 ? 1 : S::STEP / 64;
+  constexpr int kHalves = FP8 ? 1 : 2;
   constexpr int kGroups = kHalves * S::MF, kRing = 4, kAhead = 3, kTail = kGroups - kAhead;
   constexpr int kLoads = A::kLoads + B::kLoads + (FP8 ? 1 : 0);
   constexpr int kLater = S::STAGES - 2;  // steps loading behind the one that a step waits for
   static_assert(kGroups % kRing == 0, "ring of row fragments");
-  static_assert(!FP8 || (!ACOLS && !BCOLS && S::STEP == 128), "fp8 operands are rows of 128-element blocks");
-  static_assert(kHalves == 2 || S::STAGES % 2 == 0 || S::STAGES == 3, "written-out steps alternate");
+  static_assert(!FP8 || (!ACOLS && !BCOLS), "fp8 operands are rows of 128-element blocks");
+  static_assert(kHalves == 2 || S::STAGES == 3, "steps() gives an fp8 tile one step more than the written-out three");
   static_assert(!S::RING || kHalves == 2, "a ring holds bf16 steps of 128 bytes");
   Fragments<S, ACOLS, BCOLS, SPLIT> fr;
   fr.init(wave, lane);
@@ -375,7 +374,8 @@ __device__ __forceinline__ void run_tiles(Job& job, uint32_t lds, int wave, int 
       job.turn(tile, at, a, b);
       ++at;
     });
-    if constexpr (S::RING) static_for<0, A::kLoads>([&](auto j) EPL_INLINE { a.template load<j>(lds + 4 * A::kBytes, wave); });
+    if constexpr (S::RING)
+      static_for<0, A::kLoads>([&](auto j) EPL_INLINE { a.template load<j>(lds + 4 * A::kBytes, wave); });
   };
 
   uint32_t cur = lds;  // A's tile of the current step
@@ -464,9 +464,7 @@ __device__ __forceinline__ void run_tiles(Job& job, uint32_t lds, int wave, int 
     if constexpr (FP8) static_for<0, S::MF>([&](auto f) EPL_INLINE { read_scale(Zero{}, f, cur); });
     static_for<0, kAhead>(read_a);
     constexpr int kOdd = kHalves == 2 ? 0 : S::STAGES % 2;  // an odd number of written-out steps
-    if constexpr (kOdd) {
-      if (tile.steps > S::STAGES) step(Zero{}, Middle{});
-    }
+    if constexpr (kOdd) step(Zero{}, Middle{});
     for (int s = tile.steps - S::kFinal - kOdd; s > 0; s -= kHalves == 2 ? 1 : 2) {
       step(std::integral_constant<int, kHalves == 2 ? 0 : kOdd>{}, Middle{});
       if constexpr (kHalves == 1) step(std::integral_constant<int, 1 - kOdd>{}, Middle{});
