@@ -1,5 +1,5 @@
 /*
- * epl.h -- MoE expert-parallel token dispatch and combine on one MI355X (gfx950), C ABI.
+ * epl.h -- MoE router, expert-parallel token dispatch, experts' products and combine on one MI355X (gfx950), C ABI.
  *
  * The operation (UBEP paper, Background "Deploying MoE on CM384" and the Overview):
  *   - Dispatch routes every (token, chosen expert) pair to the rank hosting that expert.
@@ -64,7 +64,7 @@ typedef enum {
   EPL_OK = 0,
   EPL_ERR_INVALID_ARG = 1, /* bad config value, NULL where a buffer is required            */
   EPL_ERR_ALIGN = 2,       /* a pointer violates the alignment rule above                 */
-  EPL_ERR_CAPACITY = 3,    /* recv_rows_cap < T*k                                          */
+  EPL_ERR_CAPACITY = 3,    /* recv_rows_cap (or rows) < T*k                                */
   EPL_ERR_WORKSPACE = 4,   /* workspace smaller than epl_workspace_bytes()                 */
   EPL_ERR_UNSUPPORTED = 5, /* fp8 payload with H % 128 != 0, unknown payload kind          */
   EPL_ERR_DEVICE = 6       /* the HIP runtime refused a launch                             */

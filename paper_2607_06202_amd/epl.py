@@ -780,6 +780,19 @@ def combine(cfg: Config, y: torch.Tensor, topk_w: torch.Tensor, L: Layout, out: 
     return out
 
 
+def _call(dev: torch.device, name: str, *args) -> None:
+    """The C function on dev's current stream. Decoding calls take a few microseconds on the GPU, so the device is
+    switched only where it has to be and the stream is asked for by its number."""
+    f = getattr(_lib or lib(), name)
+    if torch._C._cuda_getDevice() == dev.index:
+        status = f(*args, torch._C._cuda_getCurrentRawStream(dev.index))
+    else:
+        with torch.cuda.device(dev):
+            status = f(*args, torch._C._cuda_getCurrentRawStream(dev.index))
+    if status:
+        raise EplError(status, name)
+
+
 def _one_of(table: dict, value, name: str) -> int:
     if value not in table:
         raise ValueError("%s must be one of %s, got %r" % (name, ", ".join(map(str, table)), value))
@@ -820,10 +833,7 @@ def route(cfg: Config, logits: torch.Tensor, bias: torch.Tensor | None = None, s
     _per_choice(cfg, topk_idx, "topk_idx", torch.int32)
     _per_choice(cfg, topk_w, "topk_w", torch.float32)
     _same_device(dev, bias=bias, topk_idx=topk_idx, topk_w=topk_w)
-    with _on(dev):
-        _check(lib().epl_route(ctypes.byref(cfg), ctypes.byref(opts), logits.data_ptr(),
-                               None if bias is None else bias.data_ptr(), topk_idx.data_ptr(), topk_w.data_ptr(),
-                               _stream(dev)), "epl_route")
+    _call(dev, "epl_route", ctypes.byref(cfg), ctypes.byref(opts), logits.data_ptr(), None if bias is None else bias.data_ptr(), topk_idx.data_ptr(), topk_w.data_ptr())
     return topk_idx, topk_w
 
 
@@ -842,17 +852,14 @@ def route_backward(cfg: Config, logits: torch.Tensor, topk_idx: torch.Tensor, dt
     if _rows_of(dlogits, "dlogits", cfg.num_experts) < cfg.T:
         raise ValueError("dlogits has %d rows, needs T = %d" % (dlogits.shape[0], cfg.T))
     _same_device(dev, topk_idx=topk_idx, dtopk_w=dtopk_w, dlogits=dlogits)
-    with _on(dev):
-        _check(lib().epl_route_backward(ctypes.byref(cfg), ctypes.byref(opts), logits.data_ptr(),
-                                        topk_idx.data_ptr(), dtopk_w.data_ptr(), dlogits.data_ptr(), _stream(dev)),
-               "epl_route_backward")
+    _call(dev, "epl_route_backward", ctypes.byref(cfg), ctypes.byref(opts), logits.data_ptr(), topk_idx.data_ptr(), dtopk_w.data_ptr(), dlogits.data_ptr())
     return dlogits
 
 
 def _packed(t, name: str, dtype, width: int, cfg: Config, pitch: int | None = None) -> int:
     """A buffer of packed rows: 2-D [>= T*k, width] on the GPU with dense columns and one stride between rows
     (pitch, if given) -> elements from one row to the next."""
-    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError("%s must be a GPU tensor" % name)
     if t.dtype != dtype:
         raise ValueError("%s must be %s, got %s" % (name, dtype, t.dtype))
@@ -868,7 +875,7 @@ def _packed(t, name: str, dtype, width: int, cfg: Config, pitch: int | None = No
 
 def _matrices(t, name: str, dtype, cfg: Config, shape=None) -> int:
     """The experts' matrices [E, out, in]: each one dense, any stride between experts -> that stride."""
-    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError("%s must be a GPU tensor" % name)
     if t.dtype != dtype:
         raise ValueError("%s must be %s, got %s" % (name, dtype, t.dtype))
@@ -931,10 +938,7 @@ def experts_gated(cfg: Config, recv: torch.Tensor, L: Layout, w_gate: torch.Tens
     _same_device(dev, w_gate=w_gate, w_up=w_up, h=h, pre=pre)
     g = Gated(inner, _one_of(ACTIVATION, activation, "activation"), stride)
     bufs = L.buffers()
-    with _on(dev):
-        _check(lib().epl_experts_gated(ctypes.byref(cfg), ctypes.byref(g), recv.data_ptr(), sp[0], recv.shape[0],
-                                       ctypes.byref(bufs), w_gate.data_ptr(), w_up.data_ptr(), sp[1], sp[2],
-                                       h.data_ptr(), _ptr(pre), _stream(dev)), "epl_experts_gated")
+    _call(dev, "epl_experts_gated", ctypes.byref(cfg), ctypes.byref(g), recv.data_ptr(), sp[0], recv.shape[0], ctypes.byref(bufs), w_gate.data_ptr(), w_up.data_ptr(), sp[1], sp[2], h.data_ptr(), _ptr(pre))
     return h, pre
 
 
@@ -970,11 +974,7 @@ def experts_gated_backward(cfg: Config, dh: torch.Tensor, pre: torch.Tensor, rec
     g = Gated(inner, _one_of(ACTIVATION, activation, "activation"), stride)
     bufs = L.buffers()
     rows = min(t.shape[0] for t in (recv, dh, pre, dpre, drecv))
-    with _on(dev):
-        _check(lib().epl_experts_gated_backward(ctypes.byref(cfg), ctypes.byref(g), dh.data_ptr(), pre.data_ptr(),
-                                                recv.data_ptr(), rows, ctypes.byref(bufs), w_gate.data_ptr(),
-                                                w_up.data_ptr(), dpre.data_ptr(), drecv.data_ptr(), dw_gate.data_ptr(),
-                                                dw_up.data_ptr(), _stream(dev)), "epl_experts_gated_backward")
+    _call(dev, "epl_experts_gated_backward", ctypes.byref(cfg), ctypes.byref(g), dh.data_ptr(), pre.data_ptr(), recv.data_ptr(), rows, ctypes.byref(bufs), w_gate.data_ptr(), w_up.data_ptr(), dpre.data_ptr(), drecv.data_ptr(), dw_gate.data_ptr(), dw_up.data_ptr())
     return drecv, dw_gate, dw_up
 
 
@@ -1017,10 +1017,7 @@ def experts_linear(cfg: Config, a: torch.Tensor, L: Layout, w: torch.Tensor, bia
                  PAYLOAD_FP8_E4M3 if dt == torch.uint8 else PAYLOAD_BF16, stride)
     bufs = L.buffers()
     rows = min(a.shape[0], out.shape[0])
-    with _on(dev):
-        _check(lib().epl_experts_linear(ctypes.byref(cfg), ctypes.byref(lin), a.data_ptr(), sp[0], rows,
-                                        ctypes.byref(bufs), w.data_ptr(), sp[1], bp, _ptr(residual), out.data_ptr(),
-                                        _ptr(pre), _stream(dev)), "epl_experts_linear")
+    _call(dev, "epl_experts_linear", ctypes.byref(cfg), ctypes.byref(lin), a.data_ptr(), sp[0], rows, ctypes.byref(bufs), w.data_ptr(), sp[1], bp, _ptr(residual), out.data_ptr(), _ptr(pre))
     return out, pre
 
 
@@ -1057,11 +1054,7 @@ def experts_linear_backward(cfg: Config, dy: torch.Tensor, a: torch.Tensor, L: L
     lin = Linear(K, N, lda, ldy, 0, act, PAYLOAD_BF16, stride)
     bufs = L.buffers()
     rows = min(t.shape[0] for t in (a, dy, da, pre, dpre) if t is not None)
-    with _on(dev):
-        _check(lib().epl_experts_linear_backward(ctypes.byref(cfg), ctypes.byref(lin), dy.data_ptr(), _ptr(pre),
-                                                 a.data_ptr(), rows, ctypes.byref(bufs), w.data_ptr(), _ptr(dpre),
-                                                 da.data_ptr(), dw.data_ptr(), bp, _stream(dev)),
-               "epl_experts_linear_backward")
+    _call(dev, "epl_experts_linear_backward", ctypes.byref(cfg), ctypes.byref(lin), dy.data_ptr(), _ptr(pre), a.data_ptr(), rows, ctypes.byref(bufs), w.data_ptr(), _ptr(dpre), da.data_ptr(), dw.data_ptr(), bp)
     return da, dw, dbias
 
 
@@ -1083,10 +1076,7 @@ def combine_backward(cfg: Config, dout: torch.Tensor, y: torch.Tensor, topk_w: t
     _per_choice(cfg, dtopk_w, "dtopk_w", torch.float32)
     _same_device(dev, dout=dout, topk_w=topk_w, dy=dy, dtopk_w=dtopk_w)
     bufs = L.buffers()
-    with _on(dev):
-        _check(lib().epl_combine_backward(ctypes.byref(cfg), dout.data_ptr(), y.data_ptr(), topk_w.data_ptr(),
-                                          ctypes.byref(bufs), dy.data_ptr(), dy.shape[0], dtopk_w.data_ptr(),
-                                          _stream(dev)), "epl_combine_backward")
+    _call(dev, "epl_combine_backward", ctypes.byref(cfg), dout.data_ptr(), y.data_ptr(), topk_w.data_ptr(), ctypes.byref(bufs), dy.data_ptr(), dy.shape[0], dtopk_w.data_ptr())
     return dy, dtopk_w
 
 
