@@ -361,7 +361,8 @@ epl_status epl_route_backward(const epl_config *cfg, const epl_route_opts *opts,
  * are summed in fp32 and rounded once to bf16 (RNE), with no atomics: identical inputs give identical outputs.
  * Weights are [E] row-major matrices [out][in] (as a linear layer keeps them), expert_stride elements apart.
  * Matrices, rows and biases are bf16 unless stated, 16-byte aligned; feature counts and pitches are multiples of
- * 8 (expert_stride and pitches of 16 for E4M3), feature counts at most EPL_MAX_HIDDEN.                 */
+ * 8 (expert_stride and pitches of 16 for E4M3), feature counts at most EPL_MAX_HIDDEN. An output must not
+ * overlap an input or another output unless stated; the same address is refused (EPL_ERR_INVALID_ARG).  */
 typedef enum { EPL_ACT_NONE = 0, EPL_ACT_SILU = 1, EPL_ACT_GELU = 2, EPL_ACT_RELU = 3 } epl_activation; /* GELU: erf */
 
 typedef struct {
@@ -405,7 +406,7 @@ typedef struct {
 
 /* out[r] = act(a[r] w[e]^T + bias[e]) + residual[r].
  *   a_scale, w_scale  E4M3 only (else ignored): [rows*K/128] and [E*N] fp32.
- *   bias     [E*N] or NULL.   residual  rows of N, or NULL; may be out.
+ *   bias     [E*N] or NULL.   residual  rows of N, or NULL; may be out (with one pitch).
  *   pre      NULL, or [rows][N]: the activation's argument, kept for the backward pass.
  * EPL_ERR_UNSUPPORTED for E4M3 with K % 128 != 0.                                                     */
 epl_status epl_experts_linear(const epl_config *cfg, const epl_linear *lin, const void *a, const float *a_scale,
@@ -426,8 +427,8 @@ epl_status epl_experts_linear_backward(const epl_config *cfg, const epl_linear *
 /* Gradient of epl_combine:
  *   dout     [T*H] bf16;   y, topk_w  as epl_combine read them.
  *   dy       rows of cfg's pitch: dy[pair_row[p]] = topk_w[p] * dout[g] (bf16, RNE); rows >= P untouched. `rows`
- *            rows, rows >= T*k. May be y itself.
- *   dtopk_w  [T*k] fp32: the fp32 product sum of dout[g] and y[pair_row[p]]; 0 for an invalid pair.
+ *            rows, rows >= T*k. May be y itself, but not dout.
+ *   dtopk_w  [T*k] fp32: the fp32 product sum of dout[g] and y[pair_row[p]]; 0 for an invalid pair. Must not be topk_w.
  * bf16 rows, whatever cfg's payload. (Dispatch's gradient is epl_combine of drecv with weights of one.) */
 epl_status epl_combine_backward(const epl_config *cfg, const void *dout, const void *y, const float *topk_w,
                                 const epl_layout_buffers *L, void *dy, int64_t rows, float *dtopk_w, void *stream);

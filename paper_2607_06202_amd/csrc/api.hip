@@ -523,6 +523,14 @@ epl_status check_linear(const epl_config* cfg, const epl_linear* l, const epl_la
   return EPL_OK;
 }
 
+// True if out is there and one of the buffers that other workgroups may still read is the same.
+bool is_one_of(const void* out, std::initializer_list<const void*> others) {
+  if (out)
+    for (const void* p : others)
+      if (p == out) return true;
+  return false;
+}
+
 int cap_of(const epl_config* cfg) { return (int)(tokens_of(cfg) * cfg->topk); }
 
 }  // namespace
@@ -562,6 +570,8 @@ EPL_EXPORT epl_status epl_experts_gated(const epl_config* cfg, const epl_gated* 
   if (fp8 && cfg->hidden % 128 != 0) return EPL_ERR_UNSUPPORTED;
   if ((st = check_ptrs({{recv, any}, {w_gate, any}, {w_up, any}, {h, any}, {pre, false}}, 16)) != EPL_OK) return st;
   if (fp8 && (st = check_ptrs({{recv_scale, any}, {gate_scale, any}, {up_scale, any}}, 4)) != EPL_OK) return st;
+  if (any && (is_one_of(h, {recv, pre, w_gate, w_up}) || is_one_of(pre, {recv, w_gate, w_up})))
+    return EPL_ERR_INVALID_ARG;
   const int esize = fp8 ? 1 : 2;
   epl::ForwardArgs p{};
   p.a = static_cast<const char*>(recv);
@@ -595,7 +605,11 @@ EPL_EXPORT epl_status epl_experts_gated_backward(const epl_config* cfg, const ep
   if ((st = check_ptrs({{dh, any}, {pre, any}, {recv, any}, {w_gate, any}, {w_up, any}, {dpre, any}, {drecv, any},
                         {dw_gate, true}, {dw_up, true}}, 16)) != EPL_OK)
     return st;
-  if (any && drecv == recv) return EPL_ERR_INVALID_ARG;
+  if (any && (is_one_of(dpre, {dh, recv, w_gate, w_up}) || is_one_of(drecv, {recv, dpre, w_gate, w_up}) ||
+              is_one_of(dw_gate, {recv, dpre}) || is_one_of(dw_up, {recv, dpre})))
+    return EPL_ERR_INVALID_ARG;
+  if (dw_gate == dw_up)
+    return EPL_ERR_INVALID_ARG;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const int E = cfg->num_experts, I = gated->inner, cap = cap_of(cfg);
   hipError_t e = epl::launch_gated_pre_grad(dh, pre, dpre, L->expert_off, E, cap, I, gated->activation, s);
@@ -642,6 +656,10 @@ EPL_EXPORT epl_status epl_experts_linear(const epl_config* cfg, const epl_linear
     return st;
   if (fp8 && (st = check_ptrs({{a_scale, any}, {w_scale, any}}, 4)) != EPL_OK) return st;
   const int K = lin->in_features, N = lin->out_features;
+  if (any && (is_one_of(out, {a, w, pre}) || is_one_of(pre, {a, w, residual}))) return EPL_ERR_INVALID_ARG;
+  if (any && out == residual &&
+      (lin->residual_pitch ? lin->residual_pitch : N) != (lin->out_pitch ? lin->out_pitch : N))
+    return EPL_ERR_INVALID_ARG;
   epl::ForwardArgs p{};
   p.a = static_cast<const char*>(a);
   p.a_scale = a_scale;
@@ -675,7 +693,12 @@ EPL_EXPORT epl_status epl_experts_linear_backward(const epl_config* cfg, const e
   if ((st = check_ptrs({{dy, any}, {act ? pre : nullptr, act && any}, {a, any}, {w, any},
                         {act ? dpre : nullptr, act && any}, {da, any}, {dw, true}, {dbias, false}}, 16)) != EPL_OK)
     return st;
-  if (any && da == a) return EPL_ERR_INVALID_ARG;
+  const void* const d = act ? dpre : dy;
+  if (any && ((act && is_one_of(dpre, {dy, a, w})) || is_one_of(da, {a, d, w}) || is_one_of(dw, {a, d}) ||
+              is_one_of(dbias, {a, d, w})))
+    return EPL_ERR_INVALID_ARG;
+  if (dbias == dw)
+    return EPL_ERR_INVALID_ARG;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const int E = cfg->num_experts, K = lin->in_features, N = lin->out_features, cap = cap_of(cfg);
   const int64_t dy_ld = (int64_t)(lin->out_pitch ? lin->out_pitch : N) * 2;
@@ -721,6 +744,7 @@ EPL_EXPORT epl_status epl_combine_backward(const epl_config* cfg, const void* do
   if ((st = check_ptrs({{dout, any}, {y, any}, {dy, any}}, 16)) != EPL_OK) return st;
   if ((st = check_ptrs({{topk_w, any}, {dtopk_w, any}}, 4)) != EPL_OK) return st;
   if (rows < cap_of(cfg)) return EPL_ERR_CAPACITY;
+  if (any && (is_one_of(dy, {dout}) || is_one_of(dtopk_w, {topk_w}))) return EPL_ERR_INVALID_ARG;
   return from_hip(epl::launch_combine_grad(dout, y, topk_w, L->pair_row, dy, dtopk_w, tokens_of(cfg), cfg->topk,
                                            cfg->hidden, pitch_of(cfg), cap_of(cfg), static_cast<hipStream_t>(stream)));
 }

@@ -50,9 +50,10 @@ inline bool few_rows(int64_t cap) { return cap <= 16; }
 // short_rows (fp8): 64 x 256 tiles against 128 x 256, us, 64 experts, 7168 to 2 x 2048: 8 rows each 351 / 494, 128 rows 728
 // / 897, 256 rows 1170 / 1136.
 inline bool short_rows(int64_t cap, int E) { return cap / E < 256; }
-// many_rows: 256 x 256 tiles against 128 x 256, us, 32 experts, 7168 to 2 x 2048: 256 rows each 607 / 658 (the smaller
-// tile first), 512 rows 1001 / 1023, 1024 rows 1844 / 1774, 2048 rows 3565 / 3421; 2048 to 7168: 980 / 1001 at 1024,
-// 1851 / 1833 at 2048.
+// many_rows: 256 x 256 tiles against 128 x 256 (the smaller tile first), us, two runs of each, 32 experts. 7168 to 2 x
+// 2048: 256 rows each 714-768 / 750-778, 512 rows 1131-1147 / 1143-1159, 1024 rows 1991-1993 / 1935-2008, 2048 rows
+// 3784-3786 / 3578-3585; 2048 to 7168: 589 / 598-610 at 512 rows, 1053-1071 / 1039-1047 at 1024, 2004-2008 / 1921-1938
+// at 2048.
 inline bool many_rows(int64_t cap, int E) { return cap / E >= 1024; }
 hipError_t launch_forward_few(const ForwardArgs& p, bool fp8, bool gated, hipStream_t stream);
 hipError_t launch_forward(const ForwardArgs& p, bool fp8, bool gated, hipStream_t stream);

@@ -422,8 +422,7 @@ __global__ void __launch_bounds__(256) pre_bias_grad_kernel(const char* dy, int6
   constexpr int kLanes = 32;
   __shared__ float part[kLanes][8][8 + 1];
   const int cv = threadIdx.x % 8, rl = threadIdx.x / 8;
-  const int ntiles = (N + 63) / 64;
-  const int e = blockIdx.x / ntiles, c = (blockIdx.x - e * ntiles) * 64 + cv * 8;
+  const int e = blockIdx.y, c = blockIdx.x * 64 + cv * 8;
   const int beg = std::min(std::max(expert_off[e], 0), cap);
   const int end = std::min(std::max(expert_off[e + 1], beg), cap);
   float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
@@ -529,7 +528,7 @@ hipError_t launch_gated_pre_grad(const void* dh, const void* pre, void* dpre, co
 hipError_t launch_pre_grad(const void* dy, int64_t dy_ld, const void* pre, void* dpre, void* dbias,
                            const int32_t* expert_off, int E, int cap, int N, int act, hipStream_t stream) {
   if (dbias)
-    hipLaunchKernelGGL(pre_bias_grad_kernel, dim3((unsigned)((N + 63) / 64 * E)), dim3(256), 0, stream, (const char*)dy,
+    hipLaunchKernelGGL(pre_bias_grad_kernel, dim3((unsigned)((N + 63) / 64), E), dim3(256), 0, stream, (const char*)dy,
                        dy_ld, (const char*)pre, (char*)dpre, (char*)dbias, expert_off, cap, N, act);
   else if (act != EPL_ACT_NONE && cap > 0)
     hipLaunchKernelGGL(pre_grad_kernel, dim3(elementwise_grid((int64_t)cap * (N / 8))), dim3(256), 0, stream,

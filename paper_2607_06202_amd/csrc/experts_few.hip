@@ -78,8 +78,8 @@ __global__ void __launch_bounds__(kFewWaves* kWave, 2) few_rows_kernel(ForwardAr
     const auto load = [&](int d, int s) EPL_INLINE {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int at = s * 128 + h * 64;
-        const bool in = at + q * 16 < kbytes;  // false past the last step too
+        const int at = std::min(s * 128 + h * 64, kbytes);  // the range check subtracts it from the descriptor's size
+        const bool in = at + q * 16 < kbytes;               // false past the last step too
 #pragma unroll
         for (int n = 0; n < NF; ++n)
           b[d][n][h] = __builtin_amdgcn_raw_buffer_load_b128(GATED && n >= NF / 2 ? rb2 : rb, in ? vb[n] : kOutOfRange,

@@ -833,7 +833,8 @@ def route(cfg: Config, logits: torch.Tensor, bias: torch.Tensor | None = None, s
     _per_choice(cfg, topk_idx, "topk_idx", torch.int32)
     _per_choice(cfg, topk_w, "topk_w", torch.float32)
     _same_device(dev, bias=bias, topk_idx=topk_idx, topk_w=topk_w)
-    _call(dev, "epl_route", ctypes.byref(cfg), ctypes.byref(opts), logits.data_ptr(), None if bias is None else bias.data_ptr(), topk_idx.data_ptr(), topk_w.data_ptr())
+    _call(dev, "epl_route", ctypes.byref(cfg), ctypes.byref(opts), logits.data_ptr(), _ptr(bias),
+          topk_idx.data_ptr(), topk_w.data_ptr())
     return topk_idx, topk_w
 
 
@@ -852,7 +853,8 @@ def route_backward(cfg: Config, logits: torch.Tensor, topk_idx: torch.Tensor, dt
     if _rows_of(dlogits, "dlogits", cfg.num_experts) < cfg.T:
         raise ValueError("dlogits has %d rows, needs T = %d" % (dlogits.shape[0], cfg.T))
     _same_device(dev, topk_idx=topk_idx, dtopk_w=dtopk_w, dlogits=dlogits)
-    _call(dev, "epl_route_backward", ctypes.byref(cfg), ctypes.byref(opts), logits.data_ptr(), topk_idx.data_ptr(), dtopk_w.data_ptr(), dlogits.data_ptr())
+    _call(dev, "epl_route_backward", ctypes.byref(cfg), ctypes.byref(opts), logits.data_ptr(), topk_idx.data_ptr(),
+          dtopk_w.data_ptr(), dlogits.data_ptr())
     return dlogits
 
 
@@ -938,7 +940,8 @@ def experts_gated(cfg: Config, recv: torch.Tensor, L: Layout, w_gate: torch.Tens
     _same_device(dev, w_gate=w_gate, w_up=w_up, h=h, pre=pre)
     g = Gated(inner, _one_of(ACTIVATION, activation, "activation"), stride)
     bufs = L.buffers()
-    _call(dev, "epl_experts_gated", ctypes.byref(cfg), ctypes.byref(g), recv.data_ptr(), sp[0], recv.shape[0], ctypes.byref(bufs), w_gate.data_ptr(), w_up.data_ptr(), sp[1], sp[2], h.data_ptr(), _ptr(pre))
+    _call(dev, "epl_experts_gated", ctypes.byref(cfg), ctypes.byref(g), recv.data_ptr(), sp[0], recv.shape[0],
+          ctypes.byref(bufs), w_gate.data_ptr(), w_up.data_ptr(), sp[1], sp[2], h.data_ptr(), _ptr(pre))
     return h, pre
 
 
@@ -974,7 +977,9 @@ def experts_gated_backward(cfg: Config, dh: torch.Tensor, pre: torch.Tensor, rec
     g = Gated(inner, _one_of(ACTIVATION, activation, "activation"), stride)
     bufs = L.buffers()
     rows = min(t.shape[0] for t in (recv, dh, pre, dpre, drecv))
-    _call(dev, "epl_experts_gated_backward", ctypes.byref(cfg), ctypes.byref(g), dh.data_ptr(), pre.data_ptr(), recv.data_ptr(), rows, ctypes.byref(bufs), w_gate.data_ptr(), w_up.data_ptr(), dpre.data_ptr(), drecv.data_ptr(), dw_gate.data_ptr(), dw_up.data_ptr())
+    _call(dev, "epl_experts_gated_backward", ctypes.byref(cfg), ctypes.byref(g), dh.data_ptr(), pre.data_ptr(),
+          recv.data_ptr(), rows, ctypes.byref(bufs), w_gate.data_ptr(), w_up.data_ptr(), dpre.data_ptr(),
+          drecv.data_ptr(), dw_gate.data_ptr(), dw_up.data_ptr())
     return drecv, dw_gate, dw_up
 
 
@@ -1017,7 +1022,8 @@ def experts_linear(cfg: Config, a: torch.Tensor, L: Layout, w: torch.Tensor, bia
                  PAYLOAD_FP8_E4M3 if dt == torch.uint8 else PAYLOAD_BF16, stride)
     bufs = L.buffers()
     rows = min(a.shape[0], out.shape[0])
-    _call(dev, "epl_experts_linear", ctypes.byref(cfg), ctypes.byref(lin), a.data_ptr(), sp[0], rows, ctypes.byref(bufs), w.data_ptr(), sp[1], bp, _ptr(residual), out.data_ptr(), _ptr(pre))
+    _call(dev, "epl_experts_linear", ctypes.byref(cfg), ctypes.byref(lin), a.data_ptr(), sp[0], rows,
+          ctypes.byref(bufs), w.data_ptr(), sp[1], bp, _ptr(residual), out.data_ptr(), _ptr(pre))
     return out, pre
 
 
@@ -1054,7 +1060,8 @@ def experts_linear_backward(cfg: Config, dy: torch.Tensor, a: torch.Tensor, L: L
     lin = Linear(K, N, lda, ldy, 0, act, PAYLOAD_BF16, stride)
     bufs = L.buffers()
     rows = min(t.shape[0] for t in (a, dy, da, pre, dpre) if t is not None)
-    _call(dev, "epl_experts_linear_backward", ctypes.byref(cfg), ctypes.byref(lin), dy.data_ptr(), _ptr(pre), a.data_ptr(), rows, ctypes.byref(bufs), w.data_ptr(), _ptr(dpre), da.data_ptr(), dw.data_ptr(), bp)
+    _call(dev, "epl_experts_linear_backward", ctypes.byref(cfg), ctypes.byref(lin), dy.data_ptr(), _ptr(pre),
+          a.data_ptr(), rows, ctypes.byref(bufs), w.data_ptr(), _ptr(dpre), da.data_ptr(), dw.data_ptr(), bp)
     return da, dw, dbias
 
 
@@ -1076,7 +1083,8 @@ def combine_backward(cfg: Config, dout: torch.Tensor, y: torch.Tensor, topk_w: t
     _per_choice(cfg, dtopk_w, "dtopk_w", torch.float32)
     _same_device(dev, dout=dout, topk_w=topk_w, dy=dy, dtopk_w=dtopk_w)
     bufs = L.buffers()
-    _call(dev, "epl_combine_backward", ctypes.byref(cfg), dout.data_ptr(), y.data_ptr(), topk_w.data_ptr(), ctypes.byref(bufs), dy.data_ptr(), dy.shape[0], dtopk_w.data_ptr())
+    _call(dev, "epl_combine_backward", ctypes.byref(cfg), dout.data_ptr(), y.data_ptr(), topk_w.data_ptr(),
+          ctypes.byref(bufs), dy.data_ptr(), dy.shape[0], dtopk_w.data_ptr())
     return dy, dtopk_w
 
 

@@ -164,6 +164,59 @@ def test_combine_backward_refusals(lib):
     assert call(L=buffers(pair_row=None)) == INVALID
 
 
+def test_buffers_that_would_race_are_refused(lib):
+    """Outputs at the address of a buffer that other workgroups may still read, all other buffers apart."""
+    def apart(*names):
+        return {n: (i + 1) * P for i, n in enumerate(names)}
+
+    one = ctypes.byref
+    L = buffers(expert_off=64 * P, pair_row=65 * P)
+
+    def gated_(**same):
+        v = apart("recv", "wg", "wu", "h", "pre")
+        v.update({a: v[b] for a, b in same.items()})
+        return lib.epl_experts_gated(one(CFG), one(epl.Gated(64, 1, 0)), v["recv"], None, 16, one(L), v["wg"], v["wu"],
+                                     None, None, v["h"], v["pre"], None)
+
+    def gated_back(**same):
+        v = apart("dh", "pre", "recv", "wg", "wu", "dpre", "drecv", "dwg", "dwu")
+        v.update({a: v[b] for a, b in same.items()})
+        return lib.epl_experts_gated_backward(one(CFG), one(epl.Gated(64, 1, 0)), v["dh"], v["pre"], v["recv"], 16,
+                                              one(L), v["wg"], v["wu"], v["dpre"], v["drecv"], v["dwg"], v["dwu"], None)
+
+    def linear_(l, **same):
+        v = apart("a", "w", "bias", "res", "out", "pre")
+        v.update({a: v[b] for a, b in same.items()})
+        return lib.epl_experts_linear(one(CFG), one(l), v["a"], None, 16, one(L), v["w"], None, v["bias"], v["res"],
+                                      v["out"], v["pre"], None)
+
+    def linear_back(l, **same):
+        v = apart("dy", "pre", "a", "w", "dpre", "da", "dw", "db")
+        v.update({a: v[b] for a, b in same.items()})
+        return lib.epl_experts_linear_backward(one(CFG), one(l), v["dy"], v["pre"], v["a"], 16, one(L), v["w"],
+                                               v["dpre"], v["da"], v["dw"], v["db"], None)
+
+    def combine_back(**same):
+        v = apart("dout", "y", "w", "dy", "dw")
+        v.update({a: v[b] for a, b in same.items()})
+        return lib.epl_combine_backward(one(CFG), v["dout"], v["y"], v["w"], one(L), v["dy"], 16, v["dw"], None)
+
+    for a, b in (("h", "recv"), ("h", "pre"), ("pre", "recv"), ("h", "wg"), ("pre", "wu")):
+        assert gated_(**{a: b}) == INVALID, (a, b)
+    for a, b in (("dpre", "dh"), ("dpre", "recv"), ("drecv", "recv"), ("drecv", "dpre"), ("drecv", "wu"), ("dwg", "dwu"),
+                 ("dwu", "recv"), ("dwg", "dpre")):
+        assert gated_back(**{a: b}) == INVALID, (a, b)
+    for a, b in (("out", "a"), ("out", "w"), ("out", "pre"), ("pre", "a"), ("pre", "res")):
+        assert linear_(lin(K=64, N=64), **{a: b}) == INVALID, (a, b)
+    assert linear_(lin(rp=40), out="res") == INVALID  # in place needs one pitch
+    for a, b in (("dpre", "dy"), ("da", "a"), ("da", "dpre"), ("da", "w"), ("dw", "a"), ("db", "dw"), ("db", "dpre")):
+        assert linear_back(lin(act=1), **{a: b}) == INVALID, (a, b)
+    for a, b in (("da", "dy"), ("dw", "dy"), ("db", "dy")):
+        assert linear_back(lin(), **{a: b}) == INVALID, (a, b)
+    for a, b in (("dy", "dout"), ("dw", "w")):
+        assert combine_back(**{a: b}) == INVALID, (a, b)
+
+
 def test_binding_refuses_cpu_tensors_and_wrong_names():
     l = torch.zeros(8, 8)
     with pytest.raises(ValueError):
