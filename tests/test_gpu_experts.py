@@ -415,3 +415,41 @@ def test_refused_tensors():
         epl.experts_linear(pk.cfg, x, pk.L, w, bias=torch.zeros(8 * 32 + 1, dtype=torch.bfloat16, device=pk.dev)[1:].view(8, 32))
     with pytest.raises(epl.EplError, match="INVALID"):
         epl.experts_gated_backward(pk.cfg, pk.buffer(g, 32), pk.buffer(g, 64), x, pk.L, w, w, drecv=x)
+
+
+@pytest.mark.parametrize("counts", [[3, 0], [20, 9]], ids=["few", "tiles"])
+def test_largest_feature_counts(counts):
+    """EPL_MAX_HIDDEN features on either side of a product. The inputs are small integers, mostly zero, so fp32 sums are
+    exact and a result is the integer, rounded once."""
+    N, E = 1 << 20, 2
+    g = torch.Generator(device=device()).manual_seed(12)
+    rng = np.random.default_rng(12)
+    pk = Packed(routing_of_counts(counts, E, 1, rng), E, N, device())
+
+    def small(*shape):
+        return torch.randint(-2, 3, shape, generator=g, device=pk.dev).bfloat16()
+
+    # A reduction over 2^20: sums stay below 2^22.
+    x, wg, wu = small(pk.rows, N), small(E, 8, N), small(E, 8, N)
+    _, pre = epl.experts_gated(pk.cfg, x, pk.L, wg, wu, "none", keep_pre=True)
+    # 2^20 results, and gradients that reduce over them.
+    a, w, bias = small(pk.rows, 8), small(E, N, 8), small(E, N)
+    out, _ = epl.experts_linear(pk.cfg, a, pk.L, w, bias)
+    dy = small(pk.rows, N)
+    da, dw, db = epl.experts_linear_backward(pk.cfg, dy, a, pk.L, w, need_dbias=True)
+    torch.cuda.synchronize()
+    for e, r0, r1 in pk.experts():
+        xs, ws, d = x[r0:r1].float(), w[e].float(), dy[r0:r1].float()
+        both = torch.cat([wg[e], wu[e]]).float()
+        for r in range(r1 - r0):  # integers, summed in 64 bits
+            want = (both.double() * xs[r].double()).sum(1)
+            assert torch.equal(pre[r0 + r], want.float().bfloat16()), (e, r)
+            want = (d[r].double()[:, None] * ws.double()).sum(0)
+            assert torch.equal(da[r0 + r], want.float().bfloat16()), (e, r)
+            want = (ws.double() * a[r0 + r].double()).sum(1) + bias[e].double()
+            assert torch.equal(out[r0 + r], want.float().bfloat16()), (e, r)
+        want = torch.zeros(N, 8, dtype=torch.float64, device=pk.dev)
+        for r in range(r0, r1):
+            want += dy[r].double()[:, None] * a[r].double()[None]
+        assert torch.equal(dw[e], want.float().bfloat16()), e
+        assert torch.equal(db[e], dy[r0:r1].double().sum(0).float().bfloat16()), e

@@ -184,3 +184,15 @@ def test_no_tokens():
     idx, w = epl.route(cfg, torch.empty(0, 16, device=dev))
     assert idx.shape == (0, 2) and w.shape == (0, 2)
     assert epl.route_backward(cfg, torch.empty(0, 16, device=dev), idx, w).shape == (0, 16)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_one_renormalised_choice_has_no_gradient(score):
+    """Its weight is p / p = 1 whatever the logits are, so the gradient is exactly zero."""
+    dev = device()
+    cfg = epl.config(1, 40, 1, 8, 33)
+    l = torch.randn(33, 40, generator=torch.Generator().manual_seed(3)).to(dev)
+    idx, w = epl.route(cfg, l, score=score)
+    d = epl.route_backward(cfg, l, idx, torch.full((33, 1), 3.7, device=dev), score=score)
+    torch.cuda.synchronize()
+    assert bool((w == 1).all()) and not d.any()
