@@ -84,7 +84,18 @@ __device__ __forceinline__ float load_logit(const void* logits, int64_t i) {
 __device__ __forceinline__ bool can_choose(float l) { return l > -INFINITY; }  // false for NaN
 
 // exp(l - m) for l <= m, 1 where they are equal (also where both are infinite).
-__device__ __forceinline__ float exp_below(float l, float m) { return l == m ? 1.0f : expf(l - m); }
+// In fp32 from 2^t, t = x log2 e, with what the rounding of t left out put back to first order (log2 e in two parts): a
+// unit or two in the last place, as expf, without its handling of results below fp32's normal range, which are 0 here.
+// Past -150 the argument is clipped, also -inf under a maximum of +inf. Gradient of 131072 x 256 logits, same card: 74 us,
+// with expf 83, with expf and cached stores 84 to 87.
+__device__ __forceinline__ float exp_below(float l, float m) {
+  constexpr float kLog2e = 1.44269502f, kLog2eRest = 1.92596303e-8f, kLn2 = 0.693147181f;
+  const float x = fmaxf(l - m, -150.0f);
+  const float t = x * kLog2e;
+  const float rest = fmaf(x, kLog2eRest, fmaf(x, kLog2e, -t));
+  const float e = __builtin_amdgcn_exp2f(t);
+  return l == m ? 1.0f : fmaf(e, rest * kLn2, e);
+}
 __device__ __forceinline__ double exp_below(double l, double m) { return l == m ? 1.0 : exp(l - m); }
 template <class F>
 __device__ __forceinline__ F sigmoid(F l) {
@@ -395,7 +406,7 @@ __global__ void __launch_bounds__(kRouteWaves* kWave) route_backward_kernel(Rout
       if constexpr (BF16)
         ((uint16_t*)p.dlogits)[g * E + ee] = (uint16_t)f32x2_to_bf16x2(d[s], 0.0f);
       else
-        ((float*)p.dlogits)[g * E + ee] = d[s];
+        __builtin_nontemporal_store(d[s], (float*)p.dlogits + g * E + ee);
     }
   }
 }
