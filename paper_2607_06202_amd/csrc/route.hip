@@ -256,8 +256,9 @@ __device__ __forceinline__ float pick_logit(const float (&l)[SLOTS], int e) {
   return v;
 }
 
-// The next token's logits load while a token is worked on. What bounds it is instructions: about 40 for each choice (the
-// wave maximum takes six dependent steps), not the 128 MiB of logits.
+// The next token's logits load while a token is worked on. What bounds it is vector instructions, not the 128 MiB of
+// logits: with four slots 22 for each choice and one more round for the certificate, and the scores, the sort and the
+// weights around them.
 template <int SLOTS, bool BF16, bool SIGMOID, bool BIASED>
 __global__ void __launch_bounds__(kRouteWaves* kWave) route_kernel(RouteArgs p) {
   const int lane = threadIdx.x % kWave;
