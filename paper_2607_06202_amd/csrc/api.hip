@@ -531,6 +531,17 @@ bool is_one_of(const void* out, std::initializer_list<const void*> others) {
   return false;
 }
 
+// True if no output is at the address of an input or of another output (null: a buffer that is not there, or an input
+// that may be the output).
+bool apart(std::initializer_list<const void*> outs, std::initializer_list<const void*> ins) {
+  for (const void* const* o = outs.begin(); o != outs.end(); ++o) {
+    if (is_one_of(*o, ins)) return false;
+    for (const void* const* q = outs.begin(); q != o; ++q)
+      if (*o && *o == *q) return false;
+  }
+  return true;
+}
+
 int cap_of(const epl_config* cfg) { return (int)(tokens_of(cfg) * cfg->topk); }
 
 }  // namespace
@@ -570,7 +581,8 @@ EPL_EXPORT epl_status epl_experts_gated(const epl_config* cfg, const epl_gated* 
   if (fp8 && cfg->hidden % 128 != 0) return EPL_ERR_UNSUPPORTED;
   if ((st = check_ptrs({{recv, any}, {w_gate, any}, {w_up, any}, {h, any}, {pre, false}}, 16)) != EPL_OK) return st;
   if (fp8 && (st = check_ptrs({{recv_scale, any}, {gate_scale, any}, {up_scale, any}}, 4)) != EPL_OK) return st;
-  if (any && (is_one_of(h, {recv, pre, w_gate, w_up}) || is_one_of(pre, {recv, w_gate, w_up})))
+  const auto scale = [&](const float* p) { return fp8 ? p : nullptr; };
+  if (any && !apart({h, pre}, {recv, w_gate, w_up, scale(recv_scale), scale(gate_scale), scale(up_scale), L->expert_off}))
     return EPL_ERR_INVALID_ARG;
   const int esize = fp8 ? 1 : 2;
   epl::ForwardArgs p{};
@@ -605,11 +617,10 @@ EPL_EXPORT epl_status epl_experts_gated_backward(const epl_config* cfg, const ep
   if ((st = check_ptrs({{dh, any}, {pre, any}, {recv, any}, {w_gate, any}, {w_up, any}, {dpre, any}, {drecv, any},
                         {dw_gate, true}, {dw_up, true}}, 16)) != EPL_OK)
     return st;
-  if (any && (is_one_of(dpre, {dh, recv, w_gate, w_up}) || is_one_of(drecv, {recv, dpre, w_gate, w_up}) ||
-              is_one_of(dw_gate, {recv, dpre}) || is_one_of(dw_up, {recv, dpre})))
+  if (any && !apart({dpre, drecv, dw_gate, dw_up},
+                    {dh, dpre == pre ? nullptr : pre, recv, w_gate, w_up, L->expert_off}))
     return EPL_ERR_INVALID_ARG;
-  if (dw_gate == dw_up)
-    return EPL_ERR_INVALID_ARG;
+  if (!apart({dw_gate, dw_up}, {L->expert_off})) return EPL_ERR_INVALID_ARG;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const int E = cfg->num_experts, I = gated->inner, cap = cap_of(cfg);
   hipError_t e = epl::launch_gated_pre_grad(dh, pre, dpre, L->expert_off, E, cap, I, gated->activation, s);
@@ -656,7 +667,10 @@ EPL_EXPORT epl_status epl_experts_linear(const epl_config* cfg, const epl_linear
     return st;
   if (fp8 && (st = check_ptrs({{a_scale, any}, {w_scale, any}}, 4)) != EPL_OK) return st;
   const int K = lin->in_features, N = lin->out_features;
-  if (any && (is_one_of(out, {a, w, pre}) || is_one_of(pre, {a, w, residual}))) return EPL_ERR_INVALID_ARG;
+  const auto scale = [&](const float* p) { return fp8 ? p : nullptr; };
+  if (any && !apart({out, pre}, {a, w, scale(a_scale), scale(w_scale), bias, out == residual ? nullptr : residual,
+                                 L->expert_off}))
+    return EPL_ERR_INVALID_ARG;
   if (any && out == residual &&
       (lin->residual_pitch ? lin->residual_pitch : N) != (lin->out_pitch ? lin->out_pitch : N))
     return EPL_ERR_INVALID_ARG;
@@ -693,12 +707,10 @@ EPL_EXPORT epl_status epl_experts_linear_backward(const epl_config* cfg, const e
   if ((st = check_ptrs({{dy, any}, {act ? pre : nullptr, act && any}, {a, any}, {w, any},
                         {act ? dpre : nullptr, act && any}, {da, any}, {dw, true}, {dbias, false}}, 16)) != EPL_OK)
     return st;
-  const void* const d = act ? dpre : dy;
-  if (any && ((act && is_one_of(dpre, {dy, a, w})) || is_one_of(da, {a, d, w}) || is_one_of(dw, {a, d}) ||
-              is_one_of(dbias, {a, d, w})))
+  if (any && !apart({act ? dpre : nullptr, da, dw, dbias},
+                    {dy, act && dpre != pre ? pre : nullptr, a, w, L->expert_off}))
     return EPL_ERR_INVALID_ARG;
-  if (dbias == dw)
-    return EPL_ERR_INVALID_ARG;
+  if (!apart({dw, dbias}, {L->expert_off})) return EPL_ERR_INVALID_ARG;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const int E = cfg->num_experts, K = lin->in_features, N = lin->out_features, cap = cap_of(cfg);
   const int64_t dy_ld = (int64_t)(lin->out_pitch ? lin->out_pitch : N) * 2;
