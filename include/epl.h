@@ -342,7 +342,8 @@ typedef struct {
 
 /*   logits  [T*E] row-major, read-only; aligned to its type.
  *   bias    [E] fp32 or NULL.
- *   topk_idx [T*k] int32, topk_w [T*k] fp32: outputs, fully written.
+ *   topk_idx [T*k] int32, topk_w [T*k] fp32: outputs, fully written. They must not overlap the inputs or each other;
+ *           the same address is refused (EPL_ERR_INVALID_ARG), here and in the gradient.
  * Uses num_experts, topk and the token count of cfg. One launch.                                      */
 epl_status epl_route(const epl_config *cfg, const epl_route_opts *opts, const void *logits, const float *bias,
                      int32_t *topk_idx, float *topk_w, void *stream);
@@ -350,7 +351,7 @@ epl_status epl_route(const epl_config *cfg, const epl_route_opts *opts, const vo
 /* Gradient of the logits, given the choices (which it takes as constants; the bias has no gradient).
  *   topk_idx [T*k]  the choices; ids outside [0, E) count for nothing, an id that occurs twice counts twice.
  *   dtopk_w  [T*k]  fp32 gradient of topk_w.
- *   dlogits  [T*E]  output in the type of logits, fully written; must not alias logits.               */
+ *   dlogits  [T*E]  output in the type of logits, fully written; must not overlap an input.           */
 epl_status epl_route_backward(const epl_config *cfg, const epl_route_opts *opts, const void *logits,
                               const int32_t *topk_idx, const float *dtopk_w, void *dlogits, void *stream);
 
@@ -427,8 +428,9 @@ epl_status epl_experts_linear_backward(const epl_config *cfg, const epl_linear *
 /* Gradient of epl_combine:
  *   dout     [T*H] bf16;   y, topk_w  as epl_combine read them.
  *   dy       rows of cfg's pitch: dy[pair_row[p]] = topk_w[p] * dout[g] (bf16, RNE); rows >= P untouched. `rows`
- *            rows, rows >= T*k. May be y itself, but not dout.
- *   dtopk_w  [T*k] fp32: the fp32 product sum of dout[g] and y[pair_row[p]]; 0 for an invalid pair. Must not be topk_w.
+ *            rows, rows >= T*k. May be y itself.
+ *   dtopk_w  [T*k] fp32: the fp32 product sum of dout[g] and y[pair_row[p]]; 0 for an invalid pair.
+ * Otherwise the outputs must not overlap an input or each other; the same address is refused (EPL_ERR_INVALID_ARG).
  * bf16 rows, whatever cfg's payload. (Dispatch's gradient is epl_combine of drecv with weights of one.) */
 epl_status epl_combine_backward(const epl_config *cfg, const void *dout, const void *y, const float *topk_w,
                                 const epl_layout_buffers *L, void *dy, int64_t rows, float *dtopk_w, void *stream);

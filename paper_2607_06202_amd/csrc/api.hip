@@ -551,6 +551,7 @@ EPL_EXPORT epl_status epl_route(const epl_config* cfg, const epl_route_opts* opt
   const epl_status st = check_route(cfg, opts, logits, topk_idx, topk_w);
   if (st != EPL_OK) return st;
   if (!aligned(bias, 4)) return EPL_ERR_ALIGN;
+  if (tokens_of(cfg) > 0 && !apart({topk_idx, topk_w}, {logits, bias})) return EPL_ERR_INVALID_ARG;
   epl::RouteArgs p = route_args(cfg, opts, logits);
   p.bias = bias;
   p.idx = topk_idx;
@@ -562,7 +563,7 @@ EPL_EXPORT epl_status epl_route_backward(const epl_config* cfg, const epl_route_
                                          const int32_t* topk_idx, const float* dtopk_w, void* dlogits, void* stream) {
   const epl_status st = check_route(cfg, opts, logits, topk_idx, dtopk_w);
   if (st != EPL_OK) return st;
-  if (tokens_of(cfg) > 0 && (!dlogits || dlogits == logits)) return EPL_ERR_INVALID_ARG;
+  if (tokens_of(cfg) > 0 && (!dlogits || !apart({dlogits}, {logits, topk_idx, dtopk_w}))) return EPL_ERR_INVALID_ARG;
   if (!aligned(dlogits, opts->logits == EPL_LOGITS_F32 ? 4 : 2)) return EPL_ERR_ALIGN;
   epl::RouteArgs p = route_args(cfg, opts, logits);
   p.idx = const_cast<int32_t*>(topk_idx);
@@ -756,7 +757,7 @@ EPL_EXPORT epl_status epl_combine_backward(const epl_config* cfg, const void* do
   if ((st = check_ptrs({{dout, any}, {y, any}, {dy, any}}, 16)) != EPL_OK) return st;
   if ((st = check_ptrs({{topk_w, any}, {dtopk_w, any}}, 4)) != EPL_OK) return st;
   if (rows < cap_of(cfg)) return EPL_ERR_CAPACITY;
-  if (any && (is_one_of(dy, {dout}) || is_one_of(dtopk_w, {topk_w}))) return EPL_ERR_INVALID_ARG;
+  if (any && !apart({dy, dtopk_w}, {dout, dy == y ? nullptr : y, topk_w, L->pair_row})) return EPL_ERR_INVALID_ARG;
   return from_hip(epl::launch_combine_grad(dout, y, topk_w, L->pair_row, dy, dtopk_w, tokens_of(cfg), cfg->topk,
                                            cfg->hidden, pitch_of(cfg), cap_of(cfg), static_cast<hipStream_t>(stream)));
 }

@@ -1,4 +1,4 @@
-"""Refusals of the products on the host, from a call that is right in everything but one argument: the unchanged call
+"""Refusals of the products, the router and combine's gradient on the host, from a call that is right in everything but one argument: the unchanged call
 passes every check (its status is then that of a launch where there is no device), so a refusal is the argument's.
 The pointers are fake addresses: on a machine with a GPU the unchanged calls would launch, so nothing runs there."""
 import ctypes
@@ -73,6 +73,11 @@ ARGS = {
     "linear_backward": lambda lib, v, L: lib.epl_experts_linear_backward(
         one(v["cfg"]), one(v["l"]), v["dy"], v["pre"], v["a"], v["rows"], one(L), v["w"], v["dpre"], v["da"], v["dw"],
         v["db"], None),
+    "route": lambda lib, v, L: lib.epl_route(one(v["cfg"]), one(v["o"]), v["logits"], v["bias"], v["idx"], v["w"], None),
+    "route_backward": lambda lib, v, L: lib.epl_route_backward(
+        one(v["cfg"]), one(v["o"]), v["logits"], v["idx"], v["dw"], v["dl"], None),
+    "combine_backward": lambda lib, v, L: lib.epl_combine_backward(
+        one(v["cfg"]), v["dout"], v["y"], v["w"], one(L), v["dy"], v["rows"], v["dw"], None),
 }
 
 GATED = dict(cfg=CFG, inner=64, act=1, stride=0)
@@ -91,6 +96,11 @@ CALLS = {
     # Without an activation pre and dpre are ignored.
     "linear_backward_none": Call("linear_backward", "dy pre a w dpre da dw db", dict(cfg=CFG, l=lin(act=0)),
                                  "dy a w expert_off", "da dw db"),
+    "route": Call("route", "logits bias idx w", dict(cfg=CFG, o=epl.RouteOpts(0, 0, 1, 1.0)), "logits bias", "idx w"),
+    "route_backward": Call("route_backward", "logits idx dw dl", dict(cfg=CFG, o=epl.RouteOpts(0, 0, 1, 1.0)),
+                           "logits idx dw", "dl"),
+    "combine_backward": Call("combine_backward", "dout y w dy dw", dict(cfg=CFG), "dout y w pair_row", "dy dw",
+                             [("dy", "y")]),
 }
 
 
