@@ -123,3 +123,126 @@ def test_without_tokens_the_weights_gradients_are_still_written(lib):
         assert CALLS[name](lib, cfg=EMPTY) == DEVICE
         assert CALLS[name](lib, cfg=EMPTY, **{o: other}) == INVALID, (name, o, other)
     assert CALLS["gated"](lib, cfg=EMPTY, h="recv") == OK  # nothing is read or written
+
+
+WIDE = (1 << 20) + 8  # more features than EPL_MAX_HIDDEN
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_missing_and_misaligned_buffers(lib, name):
+    """A buffer that the call uses is refused where it is null (unless optional) or misaligned; one that it ignores is
+    not looked at."""
+    call = CALLS[name]
+    word = {"rs", "gs", "us", "asc", "wsc", "logits", "bias", "idx", "w", "dw", "dl", "expert_off", "pair_row"} \
+        if "route" in name or name == "combine_backward" else {"rs", "gs", "us", "asc", "wsc", "expert_off"}
+    if name == "combine_backward":
+        word = {"w", "dw", "pair_row"}
+    optional = {"gated": {"pre"}, "gated_fp8": {"pre"}, "linear": {"bias", "res", "pre"},
+                "linear_fp8": {"bias", "res", "pre"}, "linear_backward": {"db"}, "linear_backward_none": {"db"},
+                "route": {"bias"}}.get(name, set())
+    used = call.inputs + call.outputs
+    for n in used:
+        assert call(lib, **{n: None}) == (DEVICE if n in optional else INVALID), n
+        assert call(lib, **{n: call.at[n] + (2 if n in word else 8)}) == ALIGN, n
+    for n in call.at:
+        if n not in used:
+            assert call(lib, **{n: None}) == call(lib, **{n: call.at[n] + 1}) == DEVICE, n
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_bad_configs_and_row_counts(lib, name):
+    call = CALLS[name]
+    for bad in (epl.config(3, 8, 2, 128, 4), epl.config(2, 8, 0, 128, 4), epl.config(2, 8, 2, 124, 4),
+                epl.config(2, 8, 2, 128, -1)):
+        assert call(lib, cfg=bad) == INVALID
+    if "route" in name:
+        return
+    for rows in (15, 0, -1):
+        assert call(lib, rows=rows) == CAPACITY
+    assert call(lib, rows=17) == DEVICE
+
+
+@pytest.mark.parametrize("name", ["gated", "gated_fp8", "gated_backward"])
+def test_gated_fields(lib, name):
+    call = CALLS[name]
+    piece = 16 if "fp8" in name else 8  # elements of 16 bytes
+    for inner in (0, 4, 12, -8, WIDE):
+        assert call(lib, inner=inner) == INVALID, inner
+    for act in (-1, 4):
+        assert call(lib, act=act) == INVALID, act
+    for act in range(4):
+        assert call(lib, act=act) == DEVICE, act
+    dense = 64 * 128
+    for stride in (dense - piece, dense + piece // 2, -piece, 1 << 62, (1 << 63) - 1):
+        assert call(lib, stride=stride) == INVALID, stride
+    for stride in (0, dense, dense + piece, 1 << 40):
+        assert call(lib, stride=stride) == DEVICE, stride
+    assert call(lib, inner=8) == call(lib, inner=1 << 20) == DEVICE
+
+
+def test_payloads(lib):
+    assert CALLS["gated"](lib, cfg=epl.config(2, 8, 2, 136, 4, "fp8")) == UNSUPPORTED
+    assert CALLS["gated_backward"](lib, cfg=FP8) == UNSUPPORTED
+    assert CALLS["linear"](lib, l=lin(payload=2)) == UNSUPPORTED
+    assert CALLS["linear"](lib, l=lin(K=64, payload=1)) == UNSUPPORTED
+    assert CALLS["linear_backward"](lib, l=lin(payload=1)) == UNSUPPORTED
+    assert CALLS["combine_backward"](lib, cfg=FP8) == DEVICE  # its rows are bf16 whatever the payload
+
+
+@pytest.mark.parametrize("name", ["linear", "linear_fp8", "linear_backward", "linear_backward_none"])
+def test_linear_fields(lib, name):
+    call = CALLS[name]
+    fp8 = "fp8" in name
+    own = dict(payload=int(fp8), act=0 if "none" in name else 1)
+    bad = [dict(K=4), dict(N=12), dict(K=WIDE, ip=0), dict(N=WIDE), dict(ip=120), dict(ip=132), dict(op=56),
+           dict(op=68), dict(rp=56), dict(rp=68), dict(op=-64), dict(ip=WIDE), dict(act=4), dict(act=-1),
+           dict(stride=128 * 64 - 16), dict(stride=128 * 64 + 4), dict(stride=1 << 62), dict(stride=-128 * 64)]
+    if fp8:
+        bad += [dict(ip=136), dict(stride=128 * 64 + 8)]  # E4M3 in 16-byte pieces
+    for kw in bad:
+        assert call(lib, l=lin(**{**own, **kw})) == INVALID, kw
+    good = [dict(), dict(ip=128), dict(ip=144), dict(op=72), dict(rp=72), dict(stride=128 * 64), dict(stride=128 * 64 + 16),
+            dict(N=8), dict(N=1 << 20), dict(K=1 << 20)]
+    for kw in good:
+        assert call(lib, l=lin(**{**own, **kw})) == DEVICE, kw
+    if not name.startswith("linear_backward"):
+        assert call(lib, out="res", l=lin(**own, rp=72)) == INVALID  # in place needs one pitch
+        assert call(lib, out="res", l=lin(**own, rp=72, op=72)) == DEVICE
+
+
+def test_route_fields(lib):
+    nan, inf = float("nan"), float("inf")
+    for name in ("route", "route_backward"):
+        call = CALLS[name]
+        for o in ((2, 0, 1, 1.0), (-1, 0, 1, 1.0), (0, 2, 1, 1.0), (0, -1, 1, 1.0), (0, 0, 2, 1.0), (0, 0, 1, nan),
+                  (0, 0, 1, inf), (0, 0, 0, -inf)):
+            assert call(lib, o=epl.RouteOpts(*o)) == INVALID, (name, o)
+        for o in ((0, 0, 0, 1.0), (1, 1, 1, -2.5), (1, 0, 1, 0.0)):
+            assert call(lib, o=epl.RouteOpts(*o)) == DEVICE, (name, o)
+        assert call(lib, o=epl.RouteOpts(1, 0, 1, 1.0), logits=call.at["logits"] + 2) == DEVICE  # bf16
+        assert call(lib, o=epl.RouteOpts(1, 0, 1, 1.0), logits=call.at["logits"] + 1) == ALIGN
+
+
+def test_missing_structs(lib):
+    L = epl.LayoutBuffers(*layout().values())
+    g, l = epl.Gated(64, 1, 0), lin()
+    p = [i * P for i in range(1, 12)]
+    assert lib.epl_experts_gated(one(CFG), None, p[0], None, 16, one(L), p[1], p[2], None, None, p[3], None, None) == INVALID
+    assert lib.epl_experts_gated(one(CFG), one(g), p[0], None, 16, None, p[1], p[2], None, None, p[3], None, None) == INVALID
+    assert lib.epl_experts_gated(None, one(g), p[0], None, 16, one(L), p[1], p[2], None, None, p[3], None, None) == INVALID
+    assert lib.epl_experts_linear(one(CFG), None, p[0], None, 16, one(L), p[1], None, None, None, p[2], None, None) == INVALID
+    assert lib.epl_experts_linear(one(CFG), one(l), p[0], None, 16, None, p[1], None, None, None, p[2], None, None) == INVALID
+    assert lib.epl_combine_backward(one(CFG), p[0], p[1], p[2], None, p[3], 16, p[4], None) == INVALID
+    assert lib.epl_route(one(CFG), None, p[0], None, p[1], p[2], None) == INVALID
+
+
+def test_without_tokens_nothing_but_weights_is_needed(lib):
+    for name, needed in (("gated", ()), ("gated_fp8", ()), ("linear", ()), ("linear_fp8", ()), ("route", ()),
+                         ("route_backward", ()), ("combine_backward", ()), ("gated_backward", ("dwg", "dwu")),
+                         ("linear_backward", ("dw",))):
+        call = CALLS[name]
+        cfg = epl.config(2, 8, 2, 128, 0, "fp8" if name == "gated_fp8" else "bf16")
+        none = {n: None for n in call.inputs + call.outputs if n not in needed and n not in ("expert_off", "pair_row")}
+        assert call(lib, cfg=cfg, rows=0, **none) == (DEVICE if needed else OK), name
+        for n in needed:
+            assert call(lib, cfg=cfg, rows=0, **none, **{n: None}) == INVALID, (name, n)
