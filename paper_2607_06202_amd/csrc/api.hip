@@ -481,7 +481,7 @@ epl_status check_products(const epl_config* cfg, const epl_layout_buffers* L, in
 
 // stride: 0 (packed) or at least one matrix, in whole 16-byte pieces.
 bool stride_ok(int64_t stride, int64_t matrix, int esize) {
-  return stride == 0 || (stride >= matrix && stride * esize % 16 == 0 && stride <= INT64_MAX / (2 * EPL_MAX_EXPERTS));
+  return stride == 0 || (stride >= matrix && stride <= INT64_MAX / (2 * EPL_MAX_EXPERTS) && stride * esize % 16 == 0);
 }
 bool pitch_ok(int pitch, int features, int esize) {
   return pitch == 0 || (pitch >= features && pitch <= EPL_MAX_HIDDEN && pitch * esize % 16 == 0);
