@@ -546,10 +546,39 @@ __device__ __forceinline__ void unpack8(u32x4 w, float (&v)[8]) {
 }
 
 // ---------------------------------------------------------------- activations (fp32)
+// What is left of the normal distribution past a >= 0, 1 - Phi(a) = tail_ratio(a) exp(-a^2 / 2). The ratio is t times a
+// polynomial of t = 1 / (1 + 0.35 a), fitted here to erfc in 64 bits over [0, 14.5] for the least maximum of the relative
+// error (weighted least squares, the weights multiplied by the error until it levels out): 3.2e-8.
+__device__ __forceinline__ float tail_ratio(float a) {
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.35f, a, 1.0f));
+  float p = -0.02915786f;
+  p = fmaf(p, t, 0.14403081f);
+  p = fmaf(p, t, -0.25583878f);
+  p = fmaf(p, t, 0.15931946f);
+  p = fmaf(p, t, -0.023212211f);
+  p = fmaf(p, t, 0.10555245f);
+  p = fmaf(p, t, 0.1198213f);
+  p = fmaf(p, t, 0.13986352f);
+  p = fmaf(p, t, 0.1396213f);
+  return t * p;
+}
+// exp(-v^2 / 4): twice as a factor, so that products with exp(-v^2 / 2) below fp32's normal range still come out.
+__device__ __forceinline__ float bell_root(float v) { return __builtin_amdgcn_exp2f(v * v * -0.36067376022224085f); }
+
 template <int ACT>
 __device__ __forceinline__ float activate(float v) {
   if constexpr (ACT == EPL_ACT_SILU) return v / (1.0f + expf(-v));
-  if constexpr (ACT == EPL_ACT_GELU) return 0.5f * v * (1.0f + erff(v * 0.70710678118654752f));
+  if constexpr (ACT == EPL_ACT_GELU) {
+    // v Phi(v) = max(v, 0) - |v| (1 - Phi(|v|)). From 1 + erf it would cancel for negative v: 4% off at -5, 0 from -5.6.
+    // Past 16 the second term is 0 in fp32.
+    const float a = fabsf(v);
+    float r = v < 0.0f ? 0.0f : v;
+    if (a < 16.0f) {
+      const float e = bell_root(v);
+      r = fmaf(-(e * tail_ratio(a) * a), e, r);
+    }
+    return r;
+  }
   if constexpr (ACT == EPL_ACT_RELU) return v < 0.0f ? 0.0f : v;
   return v;
 }
