@@ -109,7 +109,7 @@ def test_forward(name, payload, E):
         assert_close(h[:, 0], want * up, (err + FEW * want.abs()) * up.abs() + FLOOR * up.abs(), "gated " + name, v)
 
 
-@pytest.mark.parametrize("name", ["relu"])
+@pytest.mark.parametrize("name", ["gelu", "relu"])
 def test_gradient(name):
     v = points(LIMIT[name]) if name != "relu" else points(100.0)
     pk = rows_of(v, 8)
