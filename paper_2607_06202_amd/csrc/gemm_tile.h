@@ -567,7 +567,11 @@ __device__ __forceinline__ float bell_root(float v) { return __builtin_amdgcn_ex
 
 template <int ACT>
 __device__ __forceinline__ float activate(float v) {
-  if constexpr (ACT == EPL_ACT_SILU) return v / (1.0f + expf(-v));
+  if constexpr (ACT == EPL_ACT_SILU) {
+    // From exp(-|v|), which cannot overflow: v / (1 + exp(-v)) is 0 below -88.7, where the value is -2.6e-37.
+    const float e = expf(-fabsf(v));
+    return (v < 0.0f ? v * e : v) / (1.0f + e);
+  }
   if constexpr (ACT == EPL_ACT_GELU) {
     // v Phi(v) = max(v, 0) - |v| (1 - Phi(|v|)). From 1 + erf it would cancel for negative v: 4% off at -5, 0 from -5.6.
     // Past 16 the second term is 0 in fp32.
@@ -585,8 +589,9 @@ __device__ __forceinline__ float activate(float v) {
 template <int ACT>
 __device__ __forceinline__ float activate_grad(float v) {
   if constexpr (ACT == EPL_ACT_SILU) {
-    const float s = 1.0f / (1.0f + expf(-v));
-    return s * (1.0f + v * (1.0f - s));
+    const float e = expf(-fabsf(v)), r = 1.0f / (1.0f + e);
+    const float s = v < 0.0f ? e * r : r;  // sigmoid(v), as in activate
+    return s * (1.0f + v * (v < 0.0f ? r : e * r));
   }
   if constexpr (ACT == EPL_ACT_GELU) {
     // Phi(v) + v phi(v) = [v > 0] + (v / sqrt(2 pi) -+ tail_ratio(|v|)) exp(-v^2 / 2). At every bf16 value off by at most

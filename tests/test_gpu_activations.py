@@ -71,7 +71,7 @@ LIMIT = {"silu": 100.0, "gelu": 14.0, "relu": 1e30, "none": 1e30}
 
 
 @pytest.mark.parametrize("payload,E", KERNELS, ids=lambda p: str(p))
-@pytest.mark.parametrize("name", ["gelu", "relu", "none"])
+@pytest.mark.parametrize("name", ["silu", "gelu", "relu", "none"])
 def test_forward(name, payload, E):
     v = points(LIMIT[name]) if name in ("silu", "gelu") else points(100.0)
     if E == 16:
@@ -109,7 +109,7 @@ def test_forward(name, payload, E):
         assert_close(h[:, 0], want * up, (err + FEW * want.abs()) * up.abs() + FLOOR * up.abs(), "gated " + name, v)
 
 
-@pytest.mark.parametrize("name", ["gelu", "relu"])
+@pytest.mark.parametrize("name", ["silu", "gelu", "relu"])
 def test_gradient(name):
     v = points(LIMIT[name]) if name != "relu" else points(100.0)
     pk = rows_of(v, 8)
