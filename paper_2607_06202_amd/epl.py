@@ -938,7 +938,7 @@ def experts_gated(cfg: Config, recv: torch.Tensor, L: Layout, w_gate: torch.Tens
         _packed(pre, "pre", torch.bfloat16, 2 * inner, cfg, 2 * inner)
     _check_layout(cfg, L, dev)
     _same_device(dev, w_gate=w_gate, w_up=w_up, h=h, pre=pre)
-    g = Gated(inner, _one_of(ACTIVATION, activation, "activation"), stride)
+    g = Gated(_int32(inner, "inner features"), _one_of(ACTIVATION, activation, "activation"), stride)
     bufs = L.buffers()
     _call(dev, "epl_experts_gated", ctypes.byref(cfg), ctypes.byref(g), recv.data_ptr(), sp[0], recv.shape[0],
           ctypes.byref(bufs), w_gate.data_ptr(), w_up.data_ptr(), sp[1], sp[2], h.data_ptr(), _ptr(pre))
@@ -974,13 +974,20 @@ def experts_gated_backward(cfg: Config, dh: torch.Tensor, pre: torch.Tensor, rec
             raise ValueError("%s must be contiguous" % n)
     _check_layout(cfg, L, dev)
     _same_device(dev, dh=dh, pre=pre, w_gate=w_gate, w_up=w_up, dpre=dpre, drecv=drecv, dw_gate=dw_gate, dw_up=dw_up)
-    g = Gated(inner, _one_of(ACTIVATION, activation, "activation"), stride)
+    g = Gated(_int32(inner, "inner features"), _one_of(ACTIVATION, activation, "activation"), stride)
     bufs = L.buffers()
     rows = min(t.shape[0] for t in (recv, dh, pre, dpre, drecv))
     _call(dev, "epl_experts_gated_backward", ctypes.byref(cfg), ctypes.byref(g), dh.data_ptr(), pre.data_ptr(),
           recv.data_ptr(), rows, ctypes.byref(bufs), w_gate.data_ptr(), w_up.data_ptr(), dpre.data_ptr(),
           drecv.data_ptr(), dw_gate.data_ptr(), dw_up.data_ptr())
     return drecv, dw_gate, dw_up
+
+
+def _int32(v: int, name: str) -> int:
+    """A feature count or pitch for a C struct, whose int32 fields would keep the low 32 bits without a word."""
+    if v > 0x7FFFFFFF:
+        raise EplError(1, "%s of %d elements" % (name, v))
+    return v
 
 
 def _biases(t, name: str, cfg: Config, width: int):
@@ -1018,7 +1025,8 @@ def experts_linear(cfg: Config, a: torch.Tensor, L: Layout, w: torch.Tensor, bia
         _packed(pre, "pre", torch.bfloat16, N, cfg, N)
     _check_layout(cfg, L, dev)
     _same_device(dev, w=w, bias=bias, residual=residual, out=out, pre=pre)
-    lin = Linear(K, N, lda, ldo, ldr, _one_of(ACTIVATION, activation, "activation"),
+    lin = Linear(_int32(K, "in_features"), _int32(N, "out_features"), _int32(lda, "a's pitch"), _int32(ldo, "out's pitch"),
+                 _int32(ldr, "residual's pitch"), _one_of(ACTIVATION, activation, "activation"),
                  PAYLOAD_FP8_E4M3 if dt == torch.uint8 else PAYLOAD_BF16, stride)
     bufs = L.buffers()
     rows = min(a.shape[0], out.shape[0])
@@ -1057,7 +1065,8 @@ def experts_linear_backward(cfg: Config, dy: torch.Tensor, a: torch.Tensor, L: L
     bp = _biases(dbias, "dbias", cfg, N)
     _check_layout(cfg, L, dev)
     _same_device(dev, dy=dy, pre=pre, dpre=dpre, w=w, da=da, dw=dw, dbias=dbias)
-    lin = Linear(K, N, lda, ldy, 0, act, PAYLOAD_BF16, stride)
+    lin = Linear(_int32(K, "in_features"), _int32(N, "out_features"), _int32(lda, "a's pitch"), _int32(ldy, "dy's pitch"), 0,
+                 act, PAYLOAD_BF16, stride)
     bufs = L.buffers()
     rows = min(t.shape[0] for t in (a, dy, da, pre, dpre) if t is not None)
     _call(dev, "epl_experts_linear_backward", ctypes.byref(cfg), ctypes.byref(lin), dy.data_ptr(), _ptr(pre),

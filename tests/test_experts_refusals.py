@@ -1,6 +1,7 @@
-"""Refusals of the products, the router and combine's gradient on the host, from a call that is right in everything but one argument: the unchanged call
-passes every check (its status is then that of a launch where there is no device), so a refusal is the argument's.
-The pointers are fake addresses: on a machine with a GPU the unchanged calls would launch, so nothing runs there."""
+"""Refusals of the products, the router and combine's gradient on the host, from a call that is right in everything but
+one argument: the unchanged call passes every check (its status is then that of a launch where there is no device), so a
+refusal is the argument's. The pointers are fake addresses: on a machine with a GPU the unchanged calls would launch, so
+nothing runs there."""
 import ctypes
 import os
 
@@ -246,3 +247,11 @@ def test_without_tokens_nothing_but_weights_is_needed(lib):
         assert call(lib, cfg=cfg, rows=0, **none) == (DEVICE if needed else OK), name
         for n in needed:
             assert call(lib, cfg=cfg, rows=0, **none, **{n: None}) == INVALID, (name, n)
+
+
+def test_counts_past_32_bits_do_not_lose_their_upper_half():
+    assert epl.Linear(64, 64, 2 ** 32 + 64, 0, 0, 0, 0, 0).in_pitch == 64  # what ctypes makes of it
+    assert epl._int32(2 ** 31 - 1, "pitch") == 2 ** 31 - 1
+    for v in (2 ** 31, 2 ** 32 + 64):
+        with pytest.raises(epl.EplError, match="INVALID"):
+            epl._int32(v, "pitch")

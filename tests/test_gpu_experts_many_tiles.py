@@ -236,3 +236,19 @@ def test_linear_backward():
         within(dw[e], want, rounded(want, er.T @ x.abs() + sum_error(b - a + 2, (d.abs() + er).T @ x.abs())), "dw")
         want = d.sum(0)
         within(db[e], want, rounded(want, sums.sum(0) + sum_error(b - a + 2, d.abs().sum(0))), "dbias")
+
+
+def test_pitches_past_32_bits_are_refused():
+    """Rows 2^32 + 64 elements apart (one buffer of 8.6 GB): the C structs hold 32 bits, of which 64 would be left."""
+    pk = Packed(np.zeros((2, 1), np.int32), 1, 64, device())
+    pitch = 2 ** 32 + 64
+    far = torch.empty(pitch + 64, dtype=torch.bfloat16, device=pk.dev).as_strided((2, 64), (pitch, 1))
+    near = torch.zeros(2, 64, dtype=torch.bfloat16, device=pk.dev)
+    w = torch.zeros(1, 64, 64, dtype=torch.bfloat16, device=pk.dev)
+    for kw in (dict(a=far), dict(residual=far), dict(out=far)):
+        with pytest.raises(epl.EplError, match="INVALID"):
+            epl.experts_linear(pk.cfg, kw.pop("a", near), pk.L, w, **kw)
+    # (Gradients of rows so far apart would be as large again.)
+    for kw in (dict(dy=far), dict(a=far, da=far)):
+        with pytest.raises(epl.EplError, match="INVALID"):
+            epl.experts_linear_backward(pk.cfg, kw.pop("dy", near), kw.pop("a", near), pk.L, w, **kw)
