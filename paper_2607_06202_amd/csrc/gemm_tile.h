@@ -53,10 +53,12 @@ __device__ __forceinline__ u32x4 make_rsrc(uint64_t base, int64_t bytes) {
 // 64 lanes x 16 bytes from the descriptor to consecutive LDS bytes at lds. Outside the compiler's view of
 // outstanding loads: wait_tiles is what waits for it. (The builtin makes the compiler wait for every such load
 // before any LDS read, which would end the overlap of a step's loads with the previous step's products.)
+// The compiler does not see that a memory instruction is in here either, so its distance from the vector instructions
+// that may have just written the descriptor is kept here: five wait states, one of s_mov and four of s_nop.
 __device__ __forceinline__ void load_to_lds(u32x4 rsrc, uint32_t lds, int voff) {
   asm volatile(
       "s_mov_b32 m0, %0\n\t"
-      "s_nop 0\n\t"
+      "s_nop 3\n\t"
       "buffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(uniform((int)lds)),
       "v"(voff), "s"(rsrc)
       : "memory", "m0");
@@ -66,7 +68,7 @@ __device__ __forceinline__ void load_to_lds(u32x4 rsrc, uint32_t lds, int voff) 
 __device__ __forceinline__ void load_words_to_lds(u32x4 rsrc, uint32_t lds, int voff) {
   asm volatile(
       "s_mov_b32 m0, %0\n\t"
-      "s_nop 0\n\t"
+      "s_nop 3\n\t"
       "buffer_load_dword %1, %2, 0 offen lds" ::"s"(uniform((int)lds)),
       "v"(voff), "s"(rsrc)
       : "memory", "m0");
