@@ -327,10 +327,12 @@ epl_status epl_combine(const epl_config *cfg, const void *y, const float *topk_w
  *           values by the lowest expert index;
  *   weight  w_j = scale * s_{e_j}, divided first by the sum of the chosen scores if normalize is set (all zero
  *           where the chosen sigmoids are 0 in 64 bits, below about -709).
- * An expert whose logit (or whose s_e + bias_e) is -inf or NaN is masked: it is never chosen and its score is 0. A
- * token with fewer than topk experts left gets expert id -1 and weight 0 in the remaining places, which the layout
- * skips: a padded token is a row of -inf. Of several logits of +inf each counts as the maximum.
- * The order of s_e + bias_e is that of 64-bit arithmetic; scores, sums and weights are fp32.          */
+ * An expert whose logit is -inf or NaN is masked: it is never chosen and its score is 0. One whose s_e + bias_e is -inf
+ * or NaN is never chosen either, but its score counts in the softmax as any other. A token with fewer than topk experts
+ * left gets expert id -1 and weight 0 in the remaining places, which the layout skips: a padded token is a row of -inf. Of
+ * several logits of +inf each counts as the maximum.
+ * The order of s_e + bias_e is that of 64-bit arithmetic; scores, sums and weights are fp32, and one below fp32's normal
+ * range may be 0.                                                                                     */
 typedef enum { EPL_SCORE_SOFTMAX = 0, EPL_SCORE_SIGMOID = 1 } epl_score;
 typedef enum { EPL_LOGITS_F32 = 0, EPL_LOGITS_BF16 = 1 } epl_logits;
 typedef struct {
@@ -359,7 +361,8 @@ epl_status epl_route_backward(const epl_config *cfg, const epl_route_opts *opts,
  * Rows [expert_off[e], expert_off[e+1]) of the packed buffers are expert e's. Every packed buffer below has
  * `rows` rows, rows >= T*k (EPL_ERR_CAPACITY otherwise); rows >= P are neither used nor written. expert_off is
  * the only field of L that is read, on the device; whatever it holds, no access leaves the buffers. Products
- * are summed in fp32 and rounded once to bf16 (RNE), with no atomics: identical inputs give identical outputs.
+ * are summed in fp32 and rounded once to bf16 (RNE), with no atomics: identical inputs give identical outputs. An
+ * activation is fp32 too, right to its rounding relative to its value down to fp32's normal range.
  * Weights are [E] row-major matrices [out][in] (as a linear layer keeps them), expert_stride elements apart.
  * Matrices, rows and biases are bf16 unless stated, 16-byte aligned; feature counts and pitches are multiples of
  * 8 (expert_stride and pitches of 16 for E4M3), feature counts at most EPL_MAX_HIDDEN. An output must not
