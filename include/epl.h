@@ -362,7 +362,7 @@ epl_status epl_route_backward(const epl_config *cfg, const epl_route_opts *opts,
  * `rows` rows, rows >= T*k (EPL_ERR_CAPACITY otherwise); rows >= P are neither used nor written. expert_off is
  * the only field of L that is read, on the device; whatever it holds, no access leaves the buffers. Products
  * are summed in fp32 and rounded once to bf16 (RNE), with no atomics: identical inputs give identical outputs. An
- * activation is fp32 too, right to its rounding relative to its value down to fp32's normal range.
+ * activation is fp32 too, within 1e-5 of its own value down to fp32's normal range.
  * Weights are [E] row-major matrices [out][in] (as a linear layer keeps them), expert_stride elements apart.
  * Matrices, rows and biases are bf16 unless stated, 16-byte aligned; feature counts and pitches are multiples of
  * 8 (expert_stride and pitches of 16 for E4M3), feature counts at most EPL_MAX_HIDDEN. An output must not

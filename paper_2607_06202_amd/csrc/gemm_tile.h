@@ -576,7 +576,8 @@ __device__ __forceinline__ float activate(float v) {
   }
   if constexpr (ACT == EPL_ACT_GELU) {
     // v Phi(v) = max(v, 0) - |v| (1 - Phi(|v|)). From 1 + erf it would cancel for negative v: 4% off at -5, 0 from -5.6.
-    // Past 16 the second term is 0 in fp32.
+    // Past 16 the second term is 0 in fp32. (A branch, not a clamp: with none in any activation the compiler keeps more of
+    // the epilogue's offsets across tiles than there are registers, which costs every forward product 3 to 6%.)
     const float a = fabsf(v);
     float r = v < 0.0f ? 0.0f : v;
     if (a < 16.0f) {
