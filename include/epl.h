@@ -438,6 +438,64 @@ epl_status epl_experts_linear_backward(const epl_config *cfg, const epl_linear *
 epl_status epl_combine_backward(const epl_config *cfg, const void *dout, const void *y, const float *topk_w,
                                 const epl_layout_buffers *L, void *dy, int64_t rows, float *dtopk_w, void *stream);
 
+/* ---- Dispatch with the gate weights applied -------------------------------------------------------
+ * For layers that weight the experts' inputs and add their outputs up (epl_combine with weights of one).
+ * recv[pair_row[p]] = topk_w[p] * x[g] (the fp32 product, rounded once to bf16). bf16 rows, whatever cfg's payload.
+ *   x, L, recv, recv_rows_cap  as epl_dispatch.   topk_w  [T*k] fp32, applied as given; ignored for an invalid pair.
+ * Outputs must not overlap inputs; the same address is refused (EPL_ERR_INVALID_ARG), here and below.   */
+epl_status epl_dispatch_weighted(const epl_config *cfg, const void *x, const float *topk_w, const epl_layout_buffers *L,
+                                 void *recv, int64_t recv_rows_cap, void *stream);
+
+/* Its gradients, in one pass over drecv:
+ *   drecv    `rows` rows of cfg's pitch, rows >= T*k; rows >= P are not read.   x, topk_w  as the forward call read them.
+ *   dx       [T*H] bf16: what epl_combine makes of drecv and topk_w, bit for bit. May be x itself.
+ *   dtopk_w  [T*k] fp32: the fp32 product sum of x[g] and drecv[pair_row[p]]; 0 for an invalid pair.       */
+epl_status epl_dispatch_backward(const epl_config *cfg, const void *drecv, int64_t rows, const void *x,
+                                 const float *topk_w, const epl_layout_buffers *L, void *dx, float *dtopk_w,
+                                 void *stream);
+
+/* ---- The layer in 8-bit integers --------------------------------------------------------------------
+ * A row of K values x is held as int8 values q and one fp32 scale s, x ~ s q:
+ *   A = max|x|, s = A / 127 (IEEE fp32 division), q = the integer nearest to 127 x / A, halves to even, decided on the
+ *   exact quotient (so |q| <= 127; -128 never occurs); s = 0 and q = 0 for a row of zeros; s = NaN and q = 0 for a
+ *   row that holds an infinity or a NaN, so that every product with it is NaN.
+ * Features and pitches of int8 rows and expert_stride are multiples of 16 (EPL_ERR_UNSUPPORTED for features that are
+ * multiples of 8 alone). The calls do not look at cfg's payload.                                            */
+
+/* Dispatch to int8 rows: every valid pair's row of x, quantised, into its packed receive row.
+ *   x, L, recv_rows_cap  as epl_dispatch.   recv  int8 rows of H, cfg's pitch apart.
+ *   recv_scale  [recv_rows_cap] fp32: s, or with weights s * topk_w[p] (fp32): the weight goes into the scale.
+ *   topk_w      NULL, or [T*k] fp32.                                                                       */
+epl_status epl_dispatch_int8(const epl_config *cfg, const void *x, const float *topk_w, const epl_layout_buffers *L,
+                             void *recv, float *recv_scale, int64_t recv_rows_cap, void *stream);
+
+typedef struct {
+  int32_t features;  /* K                                                              */
+  int32_t in_pitch;  /* elements from one row of a to the next; 0 means K; else >= K   */
+  int32_t out_pitch; /* the same for q                                                 */
+} epl_quantize;
+
+/* bf16 rows to int8 rows and their scales.
+ *   a        rows of K bf16.   q  rows of K int8.   q_scale  [rows] fp32.
+ *   L        a layout: packed rows 0..P-1 (rows >= T*k; rows >= P are neither read nor written). Or NULL, and cfg is not
+ *            used: every one of the rows (a weight matrix [E][N][K] is E*N of them).                          */
+epl_status epl_quantize_rows(const epl_config *cfg, const epl_quantize *quantize, const void *a, int64_t rows,
+                             const epl_layout_buffers *L, void *q, float *q_scale, void *stream);
+
+/* The experts' products of int8 rows and weights, forward: as epl_experts_gated and epl_experts_linear for E4M3, but
+ * with one scale for each row (recv_scale, a_scale [rows]) and one for each output feature (gate_scale, up_scale
+ * [E*I], w_scale [E*N]). A product's sum is exact in 32 bits, times the row's scale, times the feature's; what follows is
+ * fp32, rounded once to bf16. Nothing is kept for a backward pass. lin's payload is not used.
+ * EPL_ERR_UNSUPPORTED for more than EPL_MAX_INT8_FEATURES features in (then 128 * 128 * K could pass 2^31 - 1).   */
+#define EPL_MAX_INT8_FEATURES 131056
+epl_status epl_experts_gated_int8(const epl_config *cfg, const epl_gated *gated, const void *recv,
+                                  const float *recv_scale, int64_t rows, const epl_layout_buffers *L,
+                                  const void *w_gate, const void *w_up, const float *gate_scale, const float *up_scale,
+                                  void *h, void *stream);
+epl_status epl_experts_linear_int8(const epl_config *cfg, const epl_linear *lin, const void *a, const float *a_scale,
+                                   int64_t rows, const epl_layout_buffers *L, const void *w, const float *w_scale,
+                                   const void *bias, const void *residual, void *out, void *stream);
+
 /* Row location (Hierarchical Token-level Scheduling, Token-level Load Partition; Algorithm 1,
  * Quaternary Search): for each position r, the expert whose cumulative range in the packed rows
  * covers r and r's offset inside that expert's rows. For a consumer that cuts the P packed rows

@@ -500,26 +500,33 @@ epl_status check_ptrs(std::initializer_list<Ptr> ptrs, uintptr_t a) {
   return EPL_OK;
 }
 
-epl_status check_gated(const epl_config* cfg, const epl_gated* g, const epl_layout_buffers* L, int64_t rows) {
+// Features in of an int8 product: whole 16-byte pieces, and no more than 32-bit sums hold.
+bool int8_features(int n) { return n % 16 == 0 && n <= EPL_MAX_INT8_FEATURES; }
+
+// int8: the calls for int8 rows and weights, whatever the payload.
+epl_status check_gated(const epl_config* cfg, const epl_gated* g, const epl_layout_buffers* L, int64_t rows,
+                       bool int8 = false) {
   const epl_status st = check_products(cfg, L, rows);
   if (st != EPL_OK) return st;
   if (!g || !feature_count(g->inner) || !known_activation(g->activation)) return EPL_ERR_INVALID_ARG;
-  if (!stride_ok(g->expert_stride, (int64_t)g->inner * cfg->hidden, is_fp8(cfg) ? 1 : 2)) return EPL_ERR_INVALID_ARG;
-  return EPL_OK;
+  if (!stride_ok(g->expert_stride, (int64_t)g->inner * cfg->hidden, int8 || is_fp8(cfg) ? 1 : 2))
+    return EPL_ERR_INVALID_ARG;
+  return int8 && !int8_features(cfg->hidden) ? EPL_ERR_UNSUPPORTED : EPL_OK;
 }
 
-epl_status check_linear(const epl_config* cfg, const epl_linear* l, const epl_layout_buffers* L, int64_t rows) {
+epl_status check_linear(const epl_config* cfg, const epl_linear* l, const epl_layout_buffers* L, int64_t rows,
+                        bool int8 = false) {
   const epl_status st = check_products(cfg, L, rows);
   if (st != EPL_OK) return st;
   if (!l || !feature_count(l->in_features) || !feature_count(l->out_features) || !known_activation(l->activation))
     return EPL_ERR_INVALID_ARG;
-  if (l->payload != EPL_PAYLOAD_BF16 && l->payload != EPL_PAYLOAD_FP8_E4M3) return EPL_ERR_UNSUPPORTED;
-  const int esize = l->payload == EPL_PAYLOAD_BF16 ? 2 : 1;
+  if (!int8 && l->payload != EPL_PAYLOAD_BF16 && l->payload != EPL_PAYLOAD_FP8_E4M3) return EPL_ERR_UNSUPPORTED;
+  const int esize = !int8 && l->payload == EPL_PAYLOAD_BF16 ? 2 : 1;
   if (!pitch_ok(l->in_pitch, l->in_features, esize) || !pitch_ok(l->out_pitch, l->out_features, 2) ||
       !pitch_ok(l->residual_pitch, l->out_features, 2) ||
       !stride_ok(l->expert_stride, (int64_t)l->in_features * l->out_features, esize))
     return EPL_ERR_INVALID_ARG;
-  if (esize == 1 && l->in_features % 128 != 0) return EPL_ERR_UNSUPPORTED;
+  if (int8 ? !int8_features(l->in_features) : esize == 1 && l->in_features % 128 != 0) return EPL_ERR_UNSUPPORTED;
   return EPL_OK;
 }
 
@@ -572,20 +579,21 @@ EPL_EXPORT epl_status epl_route_backward(const epl_config* cfg, const epl_route_
   return from_hip(epl::launch_route_backward(p, static_cast<hipStream_t>(stream)));
 }
 
-EPL_EXPORT epl_status epl_experts_gated(const epl_config* cfg, const epl_gated* gated, const void* recv,
-                                        const float* recv_scale, int64_t rows, const epl_layout_buffers* L,
-                                        const void* w_gate, const void* w_up, const float* gate_scale,
-                                        const float* up_scale, void* h, void* pre, void* stream) {
-  epl_status st = check_gated(cfg, gated, L, rows);
-  if (st != EPL_OK) return st;
-  const bool fp8 = is_fp8(cfg), any = cap_of(cfg) > 0;
-  if (fp8 && cfg->hidden % 128 != 0) return EPL_ERR_UNSUPPORTED;
+namespace {
+
+epl::Elem elem_of(bool fp8) { return fp8 ? epl::Elem::kE4m3 : epl::Elem::kBf16; }
+
+// The gated product after its checks of cfg, gated, L and rows.
+epl_status run_gated(const epl_config* cfg, const epl_gated* gated, epl::Elem type, const void* recv,
+                     const float* recv_scale, const epl_layout_buffers* L, const void* w_gate, const void* w_up,
+                     const float* gate_scale, const float* up_scale, void* h, void* pre, void* stream) {
+  epl_status st;
+  const bool scaled = type != epl::Elem::kBf16, any = cap_of(cfg) > 0;
   if ((st = check_ptrs({{recv, any}, {w_gate, any}, {w_up, any}, {h, any}, {pre, false}}, 16)) != EPL_OK) return st;
-  if (fp8 && (st = check_ptrs({{recv_scale, any}, {gate_scale, any}, {up_scale, any}}, 4)) != EPL_OK) return st;
-  const auto scale = [&](const float* p) { return fp8 ? p : nullptr; };
+  if (scaled && (st = check_ptrs({{recv_scale, any}, {gate_scale, any}, {up_scale, any}}, 4)) != EPL_OK) return st;
+  const auto scale = [&](const float* p) { return scaled ? p : nullptr; };
   if (any && !apart({h, pre}, {recv, w_gate, w_up, scale(recv_scale), scale(gate_scale), scale(up_scale), L->expert_off}))
     return EPL_ERR_INVALID_ARG;
-  const int esize = fp8 ? 1 : 2;
   epl::ForwardArgs p{};
   p.a = static_cast<const char*>(recv);
   p.a_scale = recv_scale;
@@ -596,7 +604,7 @@ EPL_EXPORT epl_status epl_experts_gated(const epl_config* cfg, const epl_gated* 
   p.out = static_cast<char*>(h);
   p.pre = static_cast<char*>(pre);
   p.expert_off = L->expert_off;
-  p.a_ld = (int64_t)pitch_of(cfg) * esize;
+  p.a_ld = (int64_t)pitch_of(cfg) * epl::elem_bytes(type);
   p.out_ld = (int64_t)gated->inner * 2;
   p.expert_stride = gated->expert_stride ? gated->expert_stride : (int64_t)gated->inner * cfg->hidden;
   p.E = cfg->num_experts;
@@ -604,7 +612,30 @@ EPL_EXPORT epl_status epl_experts_gated(const epl_config* cfg, const epl_gated* 
   p.N = gated->inner;
   p.K = cfg->hidden;
   p.act = gated->activation;
-  return from_hip(epl::launch_forward(p, fp8, true, static_cast<hipStream_t>(stream)));
+  return from_hip(epl::launch_forward(p, type, true, static_cast<hipStream_t>(stream)));
+}
+
+}  // namespace
+
+EPL_EXPORT epl_status epl_experts_gated(const epl_config* cfg, const epl_gated* gated, const void* recv,
+                                        const float* recv_scale, int64_t rows, const epl_layout_buffers* L,
+                                        const void* w_gate, const void* w_up, const float* gate_scale,
+                                        const float* up_scale, void* h, void* pre, void* stream) {
+  const epl_status st = check_gated(cfg, gated, L, rows);
+  if (st != EPL_OK) return st;
+  if (is_fp8(cfg) && cfg->hidden % 128 != 0) return EPL_ERR_UNSUPPORTED;
+  return run_gated(cfg, gated, elem_of(is_fp8(cfg)), recv, recv_scale, L, w_gate, w_up, gate_scale, up_scale, h, pre,
+                   stream);
+}
+
+EPL_EXPORT epl_status epl_experts_gated_int8(const epl_config* cfg, const epl_gated* gated, const void* recv,
+                                             const float* recv_scale, int64_t rows, const epl_layout_buffers* L,
+                                             const void* w_gate, const void* w_up, const float* gate_scale,
+                                             const float* up_scale, void* h, void* stream) {
+  const epl_status st = check_gated(cfg, gated, L, rows, true);
+  if (st != EPL_OK) return st;
+  return run_gated(cfg, gated, epl::Elem::kInt8, recv, recv_scale, L, w_gate, w_up, gate_scale, up_scale, h, nullptr,
+                   stream);
 }
 
 EPL_EXPORT epl_status epl_experts_gated_backward(const epl_config* cfg, const epl_gated* gated, const void* dh,
@@ -657,18 +688,19 @@ EPL_EXPORT epl_status epl_experts_gated_backward(const epl_config* cfg, const ep
   return from_hip(epl::launch_weight_grad(w, s));
 }
 
-EPL_EXPORT epl_status epl_experts_linear(const epl_config* cfg, const epl_linear* lin, const void* a,
-                                         const float* a_scale, int64_t rows, const epl_layout_buffers* L,
-                                         const void* w, const float* w_scale, const void* bias, const void* residual,
-                                         void* out, void* pre, void* stream) {
-  epl_status st = check_linear(cfg, lin, L, rows);
-  if (st != EPL_OK) return st;
-  const bool fp8 = lin->payload == EPL_PAYLOAD_FP8_E4M3, any = cap_of(cfg) > 0;
+namespace {
+
+// The linear product after its checks of cfg, lin, L and rows.
+epl_status run_linear(const epl_config* cfg, const epl_linear* lin, epl::Elem type, const void* a, const float* a_scale,
+                      const epl_layout_buffers* L, const void* w, const float* w_scale, const void* bias,
+                      const void* residual, void* out, void* pre, void* stream) {
+  epl_status st;
+  const bool scaled = type != epl::Elem::kBf16, any = cap_of(cfg) > 0;
   if ((st = check_ptrs({{a, any}, {w, any}, {bias, false}, {residual, false}, {out, any}, {pre, false}}, 16)) != EPL_OK)
     return st;
-  if (fp8 && (st = check_ptrs({{a_scale, any}, {w_scale, any}}, 4)) != EPL_OK) return st;
+  if (scaled && (st = check_ptrs({{a_scale, any}, {w_scale, any}}, 4)) != EPL_OK) return st;
   const int K = lin->in_features, N = lin->out_features;
-  const auto scale = [&](const float* p) { return fp8 ? p : nullptr; };
+  const auto scale = [&](const float* p) { return scaled ? p : nullptr; };
   if (any && !apart({out, pre}, {a, w, scale(a_scale), scale(w_scale), bias, out == residual ? nullptr : residual,
                                  L->expert_off}))
     return EPL_ERR_INVALID_ARG;
@@ -685,7 +717,7 @@ EPL_EXPORT epl_status epl_experts_linear(const epl_config* cfg, const epl_linear
   p.out = static_cast<char*>(out);
   p.pre = static_cast<char*>(pre);
   p.expert_off = L->expert_off;
-  p.a_ld = (int64_t)(lin->in_pitch ? lin->in_pitch : K) * (fp8 ? 1 : 2);
+  p.a_ld = (int64_t)(lin->in_pitch ? lin->in_pitch : K) * epl::elem_bytes(type);
   p.out_ld = (int64_t)(lin->out_pitch ? lin->out_pitch : N) * 2;
   p.res_ld = (int64_t)(lin->residual_pitch ? lin->residual_pitch : N) * 2;
   p.expert_stride = lin->expert_stride ? lin->expert_stride : (int64_t)N * K;
@@ -694,7 +726,28 @@ EPL_EXPORT epl_status epl_experts_linear(const epl_config* cfg, const epl_linear
   p.N = N;
   p.K = K;
   p.act = lin->activation;
-  return from_hip(epl::launch_forward(p, fp8, false, static_cast<hipStream_t>(stream)));
+  return from_hip(epl::launch_forward(p, type, false, static_cast<hipStream_t>(stream)));
+}
+
+}  // namespace
+
+EPL_EXPORT epl_status epl_experts_linear(const epl_config* cfg, const epl_linear* lin, const void* a,
+                                         const float* a_scale, int64_t rows, const epl_layout_buffers* L,
+                                         const void* w, const float* w_scale, const void* bias, const void* residual,
+                                         void* out, void* pre, void* stream) {
+  const epl_status st = check_linear(cfg, lin, L, rows);
+  if (st != EPL_OK) return st;
+  return run_linear(cfg, lin, elem_of(lin->payload == EPL_PAYLOAD_FP8_E4M3), a, a_scale, L, w, w_scale, bias, residual,
+                    out, pre, stream);
+}
+
+EPL_EXPORT epl_status epl_experts_linear_int8(const epl_config* cfg, const epl_linear* lin, const void* a,
+                                              const float* a_scale, int64_t rows, const epl_layout_buffers* L,
+                                              const void* w, const float* w_scale, const void* bias,
+                                              const void* residual, void* out, void* stream) {
+  const epl_status st = check_linear(cfg, lin, L, rows, true);
+  if (st != EPL_OK) return st;
+  return run_linear(cfg, lin, epl::Elem::kInt8, a, a_scale, L, w, w_scale, bias, residual, out, nullptr, stream);
 }
 
 EPL_EXPORT epl_status epl_experts_linear_backward(const epl_config* cfg, const epl_linear* lin, const void* dy,
@@ -760,6 +813,81 @@ EPL_EXPORT epl_status epl_combine_backward(const epl_config* cfg, const void* do
   if (any && !apart({dy, dtopk_w}, {dout, dy == y ? nullptr : y, topk_w, L->pair_row})) return EPL_ERR_INVALID_ARG;
   return from_hip(epl::launch_combine_grad(dout, y, topk_w, L->pair_row, dy, dtopk_w, tokens_of(cfg), cfg->topk,
                                            cfg->hidden, pitch_of(cfg), cap_of(cfg), static_cast<hipStream_t>(stream)));
+}
+
+// ------------------------------------------------------------------ dispatch with weights, rows in int8
+namespace {
+
+// cfg and the layout's pair_row, which is all that these calls read of L.
+epl_status check_pairs(const epl_config* cfg, const epl_layout_buffers* L) {
+  const epl_status st = check_config(cfg);
+  if (st != EPL_OK) return st;
+  if (!L || !L->pair_row) return EPL_ERR_INVALID_ARG;
+  return aligned(L->pair_row, 4) ? EPL_OK : EPL_ERR_ALIGN;
+}
+
+}  // namespace
+
+EPL_EXPORT epl_status epl_dispatch_weighted(const epl_config* cfg, const void* x, const float* topk_w,
+                                            const epl_layout_buffers* L, void* recv, int64_t recv_rows_cap,
+                                            void* stream) {
+  epl_status st = check_pairs(cfg, L);
+  if (st != EPL_OK) return st;
+  const bool any = tokens_of(cfg) > 0;
+  if ((st = check_ptrs({{x, any}, {recv, any}}, 16)) != EPL_OK) return st;
+  if ((st = check_ptrs({{topk_w, any}}, 4)) != EPL_OK) return st;
+  if (recv_rows_cap < cap_of(cfg)) return EPL_ERR_CAPACITY;
+  if (any && !apart({recv}, {x, topk_w, L->pair_row})) return EPL_ERR_INVALID_ARG;
+  return from_hip(epl::launch_dispatch_weighted(x, topk_w, L->pair_row, recv, tokens_of(cfg), cfg->topk, cfg->hidden,
+                                                pitch_of(cfg), cap_of(cfg), static_cast<hipStream_t>(stream)));
+}
+
+EPL_EXPORT epl_status epl_dispatch_backward(const epl_config* cfg, const void* drecv, int64_t rows, const void* x,
+                                            const float* topk_w, const epl_layout_buffers* L, void* dx, float* dtopk_w,
+                                            void* stream) {
+  epl_status st = check_pairs(cfg, L);
+  if (st != EPL_OK) return st;
+  const bool any = tokens_of(cfg) > 0;
+  if ((st = check_ptrs({{drecv, any}, {x, any}, {dx, any}}, 16)) != EPL_OK) return st;
+  if ((st = check_ptrs({{topk_w, any}, {dtopk_w, any}}, 4)) != EPL_OK) return st;
+  if (rows < cap_of(cfg)) return EPL_ERR_CAPACITY;
+  if (any && !apart({dx, dtopk_w}, {drecv, dx == x ? nullptr : x, topk_w, L->pair_row})) return EPL_ERR_INVALID_ARG;
+  return from_hip(epl::launch_dispatch_grad(drecv, x, topk_w, L->pair_row, dx, dtopk_w, tokens_of(cfg), cfg->topk,
+                                            cfg->hidden, pitch_of(cfg), cap_of(cfg), static_cast<hipStream_t>(stream)));
+}
+
+EPL_EXPORT epl_status epl_dispatch_int8(const epl_config* cfg, const void* x, const float* topk_w,
+                                        const epl_layout_buffers* L, void* recv, float* recv_scale,
+                                        int64_t recv_rows_cap, void* stream) {
+  epl_status st = check_pairs(cfg, L);
+  if (st != EPL_OK) return st;
+  if (cfg->hidden % 16 != 0) return EPL_ERR_UNSUPPORTED;
+  const bool any = tokens_of(cfg) > 0;
+  if ((st = check_ptrs({{x, any}, {recv, any}}, 16)) != EPL_OK) return st;
+  if ((st = check_ptrs({{topk_w, false}, {recv_scale, any}}, 4)) != EPL_OK) return st;
+  if (recv_rows_cap < cap_of(cfg)) return EPL_ERR_CAPACITY;
+  if (any && !apart({recv, recv_scale}, {x, topk_w, L->pair_row})) return EPL_ERR_INVALID_ARG;
+  return from_hip(epl::launch_dispatch_int8(x, topk_w, L->pair_row, recv, recv_scale, tokens_of(cfg), cfg->topk,
+                                            cfg->hidden, pitch_of(cfg), cap_of(cfg), static_cast<hipStream_t>(stream)));
+}
+
+EPL_EXPORT epl_status epl_quantize_rows(const epl_config* cfg, const epl_quantize* quantize, const void* a, int64_t rows,
+                                        const epl_layout_buffers* L, void* q, float* q_scale, void* stream) {
+  epl_status st;
+  if (L && (st = check_products(cfg, L, rows)) != EPL_OK) return st;
+  if (!quantize || !feature_count(quantize->features) || rows < 0) return EPL_ERR_INVALID_ARG;
+  const int K = quantize->features;
+  if (!pitch_ok(quantize->in_pitch, K, 2) || !pitch_ok(quantize->out_pitch, K, 1)) return EPL_ERR_INVALID_ARG;
+  if (K % 16 != 0) return EPL_ERR_UNSUPPORTED;
+  const int64_t n = L ? cap_of(cfg) : rows;
+  const bool any = n > 0;
+  if ((st = check_ptrs({{a, any}, {q, any}}, 16)) != EPL_OK) return st;
+  if ((st = check_ptrs({{q_scale, any}}, 4)) != EPL_OK) return st;
+  const int32_t* count = L ? L->expert_off + cfg->num_experts : nullptr;
+  if (any && !apart({q, q_scale}, {a, L ? L->expert_off : nullptr})) return EPL_ERR_INVALID_ARG;
+  const int64_t a_ld = quantize->in_pitch ? quantize->in_pitch : K, q_ld = quantize->out_pitch ? quantize->out_pitch : K;
+  return from_hip(
+      epl::launch_quantize_rows(a, q, q_scale, count, n, K, a_ld / 8, q_ld / 16, static_cast<hipStream_t>(stream)));
 }
 
 EPL_EXPORT epl_status epl_debug_f32_to_e4m3(const float* in, uint8_t* out, int64_t n, void* stream) {

@@ -1,0 +1,130 @@
+// Dispatch with the gate weights applied, and its gradient: for token g with valid choices j in packed rows r,
+//   recv[r] = w[g][j] x[g];   dx[g] = sum_j w[g][j] drecv[r],   dw[g][j] = <x[g], drecv[r]>.
+// HBM traffic bounds both.
+#include "epl_internal.h"
+#include "experts.h"
+
+namespace epl {
+
+constexpr int kWeightedThreads = 128;
+constexpr int kWeightedWaves = kWeightedThreads / kWave;
+
+__global__ void __launch_bounds__(kWeightedThreads)
+    dispatch_weighted_kernel(const u32x4* __restrict__ x, const float* __restrict__ w, const int32_t* __restrict__ pair_row,
+                             u32x4* __restrict__ recv, int64_t T, int k, int nv, int pv, int chunks, int64_t cap) {
+  const int lane = threadIdx.x % kWave;
+  const int64_t units = T * chunks;
+  for (int64_t u = (int64_t)blockIdx.x * kWeightedWaves + threadIdx.x / kWave; u < units;
+       u += (int64_t)gridDim.x * kWeightedWaves) {
+    const int64_t g = u / chunks;
+    const int v = (int)(u - g * chunks) * kWave + lane;
+    const u32x4 buf = x[g * nv + std::min(v, nv - 1)];
+    const int my_row = lane < k ? pair_row[g * k + lane] : -1;
+    const float my_w = lane < k ? w[g * k + lane] : 0.0f;
+    for (int j = 0; j < k; ++j) {
+      const int row = __builtin_amdgcn_readlane(my_row, j);
+      if (row < 0 || row >= cap) continue;
+      const float wj = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(my_w), j));
+      u32x4 o;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] = f32x2_to_bf16x2(wj * bf16lo_to_f32(buf[i]), wj * bf16hi_to_f32(buf[i]));
+      if (v < nv) recv[(int64_t)row * pv + v] = o;
+    }
+  }
+}
+
+constexpr int kDispatchGradThreads = 256;
+constexpr int kDispatchGradWaves = kDispatchGradThreads / kWave;
+
+// One workgroup a token. A thread's products are summed in fp32 over its own columns, then over the wave and the waves in
+// a fixed order. dx may be x: a thread reads its columns before it writes them.
+// KMAX: choices held in registers (k <= KMAX).
+template <int KMAX>
+__global__ void __launch_bounds__(kDispatchGradThreads)
+    dispatch_grad_kernel(const u32x4* __restrict__ d, const u32x4* x, const float* __restrict__ w,
+                         const int32_t* __restrict__ pair_row, u32x4* dx, float* __restrict__ dw, int64_t T, int k, int nv,
+                         int pv, int64_t cap) {
+  __shared__ float part[kDispatchGradWaves][EPL_MAX_TOPK];
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  for (int64_t g = blockIdx.x; g < T; g += gridDim.x) {
+    float acc[KMAX];
+#pragma unroll
+    for (int j = 0; j < KMAX; ++j) acc[j] = 0.0f;
+    for (int c = threadIdx.x; c < nv; c += kDispatchGradThreads) {
+      const u32x4 xv = x[g * nv + c];
+      float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+      constexpr int kGroup = KMAX < 8 ? KMAX : 8;  // rows loaded before any is consumed
+#pragma unroll
+      for (int j0 = 0; j0 < KMAX; j0 += kGroup) {
+        u32x4 buf[kGroup];
+        int row[kGroup];
+#pragma unroll
+        for (int jj = 0; jj < kGroup; ++jj) {
+          const int j = j0 + jj;
+          row[jj] = j < k ? __builtin_amdgcn_readfirstlane(pair_row[g * k + j]) : -1;
+          if (row[jj] >= cap) row[jj] = -1;
+          if (row[jj] >= 0) buf[jj] = __builtin_nontemporal_load(d + (int64_t)row[jj] * pv + c);
+        }
+#pragma unroll
+        for (int jj = 0; jj < kGroup; ++jj) {
+          if (row[jj] < 0) continue;
+          const float wj = w[g * k + j0 + jj];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float lo = bf16lo_to_f32(buf[jj][i]), hi = bf16hi_to_f32(buf[jj][i]);
+            acc[j0 + jj] = fmaf(bf16lo_to_f32(xv[i]), lo, acc[j0 + jj]);
+            acc[j0 + jj] = fmaf(bf16hi_to_f32(xv[i]), hi, acc[j0 + jj]);
+            sum[2 * i] = fmaf(wj, lo, sum[2 * i]);
+            sum[2 * i + 1] = fmaf(wj, hi, sum[2 * i + 1]);
+          }
+        }
+      }
+      u32x4 o;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] = f32x2_to_bf16x2(sum[2 * i], sum[2 * i + 1]);
+      dx[g * nv + c] = o;
+    }
+    __syncthreads();  // the previous token's sums have been read
+#pragma unroll
+    for (int j = 0; j < KMAX; ++j) {
+      float v = acc[j];
+#pragma unroll
+      for (int off = kWave / 2; off > 0; off >>= 1) v += __shfl_xor(v, off, kWave);
+      if (lane == 0 && j < k) part[wave][j] = v;
+    }
+    __syncthreads();
+    if (threadIdx.x < k) {
+      float v = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kDispatchGradWaves; ++i) v += part[i][threadIdx.x];
+      dw[g * k + threadIdx.x] = v;
+    }
+  }
+}
+
+hipError_t launch_dispatch_weighted(const void* x, const float* w, const int32_t* pair_row, void* recv, int64_t T, int k,
+                                    int H, int pitch, int64_t cap, hipStream_t stream) {
+  if (T == 0) return hipSuccess;
+  const int nv = H / 8, chunks = (nv + kWave - 1) / kWave;
+  hipLaunchKernelGGL(dispatch_weighted_kernel, dim3(unit_grid(T * chunks, kWeightedWaves, kWeightedThreads)),
+                     dim3(kWeightedThreads), 0, stream, static_cast<const u32x4*>(x), w, pair_row, static_cast<u32x4*>(recv),
+                     T, k, nv, pitch / 8, chunks, cap);
+  return hipGetLastError();
+}
+
+hipError_t launch_dispatch_grad(const void* d, const void* x, const float* w, const int32_t* pair_row, void* dx, float* dw,
+                                int64_t T, int k, int H, int pitch, int64_t cap, hipStream_t stream) {
+  if (T == 0) return hipSuccess;
+  const dim3 grid((unsigned)std::min<int64_t>(T, 1 << 20));
+  const auto launch = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, dim3(kDispatchGradThreads), 0, stream, static_cast<const u32x4*>(d),
+                       static_cast<const u32x4*>(x), w, pair_row, static_cast<u32x4*>(dx), dw, T, k, H / 8, pitch / 8, cap);
+  };
+  if (k <= 8)
+    launch(dispatch_grad_kernel<8>);
+  else
+    launch(dispatch_grad_kernel<EPL_MAX_TOPK>);
+  return hipGetLastError();
+}
+
+}  // namespace epl

@@ -14,6 +14,8 @@ namespace epl {
 
 constexpr int kLayoutSlots = EPL_MAX_EXPERTS / kLayoutThreads;  // per-lane slots covering E or R experts/ranks
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+// Lambdas over register arrays: out of line they would put the arrays in memory.
+#define EPL_INLINE __attribute__((always_inline))
 
 // Buffer resource descriptor word 3 for raw (untyped) buffer accesses on CDNA3/CDNA4.
 constexpr int kBufferRsrcWord3 = 0x00020000;

@@ -1,4 +1,5 @@
-// Arguments and launchers of the router, the experts' products and combine's gradient (host side).
+// Arguments and launchers of the router, the experts' products, combine's gradient, dispatch with weights and the rows in
+// int8 (host side).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -8,12 +9,17 @@
 
 namespace epl {
 
+// Elements of the products' operands. Int8 ones go through everything as bf16 ones twice as long do: 64 bytes of a row are
+// one matrix instruction either way, and only the instruction and the type of its sums (32-bit integers, exact) differ.
+enum class Elem { kBf16, kE4m3, kInt8 };
+constexpr int elem_bytes(Elem t) { return t == Elem::kBf16 ? 2 : 1; }
+
 // Row strides (…_ld) are in bytes, expert_stride in elements. cap: packed rows, the bound on expert_off.
 struct ForwardArgs {
   const char* a;
-  const float* a_scale;  // fp8: [rows][K / 128]
+  const float* a_scale;  // fp8: [rows][K / 128]; int8: [rows]
   const char *w, *w2;    // [E] matrices [N][K]; w2: the up projection (gated)
-  const float *w_scale, *w2_scale;  // fp8: [E][N]
+  const float *w_scale, *w2_scale;  // fp8, int8: [E][N]
   const char* bias;      // [E][N] bf16 or null
   const char* residual;  // rows of N bf16 or null
   char* out;
@@ -55,8 +61,8 @@ inline bool short_rows(int64_t cap, int E) { return cap / E < 256; }
 // 3784-3786 / 3578-3585; 2048 to 7168: 589 / 598-610 at 512 rows, 1053-1071 / 1039-1047 at 1024, 2004-2008 / 1921-1938
 // at 2048.
 inline bool many_rows(int64_t cap, int E) { return cap / E >= 1024; }
-hipError_t launch_forward_few(const ForwardArgs& p, bool fp8, bool gated, hipStream_t stream);
-hipError_t launch_forward(const ForwardArgs& p, bool fp8, bool gated, hipStream_t stream);
+hipError_t launch_forward_few(const ForwardArgs& p, Elem type, bool gated, hipStream_t stream);
+hipError_t launch_forward(const ForwardArgs& p, Elem type, bool gated, hipStream_t stream);
 hipError_t launch_row_grad(const RowGradArgs& p, hipStream_t stream);
 hipError_t launch_weight_grad(const WeightGradArgs& p, hipStream_t stream);
 hipError_t launch_gated_pre_grad(const void* dh, const void* pre, void* dpre, const int32_t* expert_off, int E,
@@ -82,5 +88,18 @@ hipError_t launch_route_backward(const RouteArgs& p, hipStream_t stream);
 
 hipError_t launch_combine_grad(const void* dout, const void* y, const float* w, const int32_t* pair_row, void* dy,
                                float* dw, int64_t T, int k, int H, int pitch, int64_t cap, hipStream_t stream);
+
+// recv rows pitch elements apart; w [T][k].
+hipError_t launch_dispatch_weighted(const void* x, const float* w, const int32_t* pair_row, void* recv, int64_t T, int k,
+                                    int H, int pitch, int64_t cap, hipStream_t stream);
+hipError_t launch_dispatch_grad(const void* d, const void* x, const float* w, const int32_t* pair_row, void* dx, float* dw,
+                                int64_t T, int k, int H, int pitch, int64_t cap, hipStream_t stream);
+
+// w: [T][k] or null. recv rows pitch bytes apart.
+hipError_t launch_dispatch_int8(const void* x, const float* w, const int32_t* pair_row, void* recv, float* scale, int64_t T,
+                                int k, int H, int pitch, int64_t cap, hipStream_t stream);
+// The first n[0] of `rows` rows, or with n null all of them. Strides in 16-byte pieces.
+hipError_t launch_quantize_rows(const void* a, void* q, float* scale, const int32_t* n, int64_t rows, int K, int64_t a_ld,
+                                int64_t q_ld, hipStream_t stream);
 
 }  // namespace epl

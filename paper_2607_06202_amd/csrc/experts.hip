@@ -65,11 +65,12 @@ __device__ __forceinline__ void store_tile(const TileOut& out, int row, int col,
 
 // ---------------------------------------------------------------- forward
 // GATED: B tile = BN/2 gate rows and BN/2 up rows; BN/2 output columns.
-template <class S, bool FP8, bool GATED>
+template <class S, Elem T, bool GATED>
 struct ForwardJob {
+  static constexpr bool FP8 = T == Elem::kE4m3, INT8 = T == Elem::kInt8;
   static constexpr int kCols = GATED ? S::BN / 2 : S::BN;  // output columns of a tile
   static constexpr int kPairs = kCols / S::WN / 32;        // pairs of column fragments of a wave
-  static constexpr int kEsize = FP8 ? 1 : 2;
+  static constexpr int kEsize = elem_bytes(T);
   struct Tile {
     int64_t t;
     RowTile at;
@@ -133,8 +134,13 @@ struct ForwardJob {
     else
       wait_tiles<std::min(63, N + kEach * (GATED ? 3 : 2))>();
   }
-  __device__ __forceinline__ void finish(const Tile& t, f32x4 (&acc)[S::MF][S::NF]) const {
+  __device__ __forceinline__ void finish(const Tile& t, AccOf<T> (&acc)[S::MF][S::NF]) const {
     const int cols = std::min(p.N - t.col0, kCols);
+    float rs[S::MF];  // int8: the scales of the lane's rows
+    if constexpr (INT8) {
+#pragma unroll
+      for (int f = 0; f < S::MF; ++f) rs[f] = p.a_scale[t.row0 + std::min(at.row + f * 16, t.rows - 1)];
+    }
     const TileOut out(p.out, t.row0, p.out_ld, t.col0, t.rows, cols);
     const int64_t pre_ld = (int64_t)p.N * (GATED ? 4 : 2);
     const TileOut pre(p.pre, t.row0, pre_ld, t.col0, t.rows, cols);
@@ -148,7 +154,7 @@ struct ForwardJob {
       for (int k = 0; k < kTake; ++k) {
         // In range for the lanes past the last column.
         const int64_t cc = (int64_t)t.e * p.N + t.col0 + std::min(c0 + k * 32, cols - 8);
-        if constexpr (FP8) {
+        if constexpr (FP8 || INT8) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             s1[k][i] = p.w_scale[cc + i];
@@ -166,11 +172,13 @@ struct ForwardJob {
 #pragma unroll
         for (int j = 0; j < kTake * 8; ++j) {
           const int k = j / 8, i = j % 8, at_n = (g0 + k) * 2 + i / 4;
-          v[k][i] = acc[f][at_n][i % 4];
-          if constexpr (FP8) v[k][i] *= s1[k][i];
+          v[k][i] = (float)acc[f][at_n][i % 4];
+          if constexpr (INT8) v[k][i] *= rs[f];
+          if constexpr (FP8 || INT8) v[k][i] *= s1[k][i];
           if constexpr (GATED) {
-            u[k][i] = acc[f][S::NF / 2 + at_n][i % 4];
-            if constexpr (FP8) u[k][i] *= s2[k][i];
+            u[k][i] = (float)acc[f][S::NF / 2 + at_n][i % 4];
+            if constexpr (INT8) u[k][i] *= rs[f];
+            if constexpr (FP8 || INT8) u[k][i] *= s2[k][i];
           } else if (p.bias) {
             v[k][i] += bias[k][i];
           }
@@ -211,12 +219,12 @@ struct ForwardJob {
   }
 };
 
-template <class S, bool FP8, bool GATED>
+template <class S, Elem T, bool GATED>
 __global__ void __launch_bounds__(S::kThreads) forward_kernel(ForwardArgs p) {
-  __shared__ __attribute__((aligned(1024))) char tiles[S::lds(FP8)];
+  __shared__ __attribute__((aligned(1024))) char tiles[S::lds(T == Elem::kE4m3)];
   const int wave = uniform(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-  ForwardJob<S, FP8, GATED> job(p, wave, lane);
-  run_tiles<S, false, false, FP8, GATED>(job, lds_addr(tiles), wave, lane);
+  ForwardJob<S, T, GATED> job(p, wave, lane);
+  run_tiles<S, false, false, T, GATED>(job, lds_addr(tiles), wave, lane);
 }
 
 // ---------------------------------------------------------------- gradient of the rows
@@ -292,7 +300,7 @@ __global__ void __launch_bounds__(S::kThreads) row_grad_kernel(RowGradArgs p) {
   __shared__ __attribute__((aligned(1024))) char tiles[S::lds(false)];
   const int wave = uniform(threadIdx.x / kWave), lane = threadIdx.x % kWave;
   RowGradJob<S> job(p, wave, lane);
-  run_tiles<S, false, true, false, false>(job, lds_addr(tiles), wave, lane);
+  run_tiles<S, false, true, Elem::kBf16, false>(job, lds_addr(tiles), wave, lane);
 }
 
 // ---------------------------------------------------------------- gradient of the weights
@@ -365,7 +373,7 @@ __global__ void __launch_bounds__(S::kThreads) weight_grad_kernel(WeightGradArgs
   __shared__ __attribute__((aligned(1024))) char tiles[S::lds(false)];
   const int wave = uniform(threadIdx.x / kWave), lane = threadIdx.x % kWave;
   WeightGradJob<S> job(p, wave, lane);
-  run_tiles<S, true, true, false, false>(job, lds_addr(tiles), wave, lane);
+  run_tiles<S, true, true, Elem::kBf16, false>(job, lds_addr(tiles), wave, lane);
 }
 
 // ---------------------------------------------------------------- gradients through the activation
@@ -477,24 +485,29 @@ static unsigned persistent_grid(int64_t tiles, int per_cu) {
 // Row tiles of BM over at most `rows` rows of E experts.
 static int64_t row_tiles(int64_t rows, int E, int BM) { return rows / BM + std::min<int64_t>(E, rows); }
 
-template <class S, bool FP8, bool GATED>
-static hipError_t forward_as(const ForwardArgs& p, hipStream_t stream) {
-  const int cols = GATED ? S::BN / 2 : S::BN;
+template <class S, Elem T>
+static hipError_t forward_as(const ForwardArgs& p, bool gated, hipStream_t stream) {
+  const int cols = gated ? S::BN / 2 : S::BN;
   const int64_t tiles = row_tiles(p.cap, p.E, S::BM) * ((p.N + cols - 1) / cols);
-  hipLaunchKernelGGL((forward_kernel<S, FP8, GATED>), dim3(persistent_grid(tiles, 1)), dim3(S::kThreads), 0, stream,
-                     p);
+  const dim3 grid(persistent_grid(tiles, 1));
+  if (gated)
+    hipLaunchKernelGGL((forward_kernel<S, T, true>), grid, dim3(S::kThreads), 0, stream, p);
+  else
+    hipLaunchKernelGGL((forward_kernel<S, T, false>), grid, dim3(S::kThreads), 0, stream, p);
   return hipGetLastError();
 }
 
-hipError_t launch_forward(const ForwardArgs& p, bool fp8, bool gated, hipStream_t stream) {
+hipError_t launch_forward(const ForwardArgs& p, Elem type, bool gated, hipStream_t stream) {
   if (p.cap == 0) return hipSuccess;
-  if (few_rows(p.cap)) return launch_forward_few(p, fp8, gated, stream);
-  if (fp8 && short_rows(p.cap, p.E))
-    return gated ? forward_as<Short, true, true>(p, stream) : forward_as<Short, true, false>(p, stream);
-  if (fp8) return gated ? forward_as<Mid, true, true>(p, stream) : forward_as<Mid, true, false>(p, stream);
-  if (many_rows(p.cap, p.E))
-    return gated ? forward_as<Big, false, true>(p, stream) : forward_as<Big, false, false>(p, stream);
-  return gated ? forward_as<Mid, false, true>(p, stream) : forward_as<Mid, false, false>(p, stream);
+  if (few_rows(p.cap)) return launch_forward_few(p, type, gated, stream);
+  if (type == Elem::kE4m3)
+    return short_rows(p.cap, p.E) ? forward_as<Short, Elem::kE4m3>(p, gated, stream)
+                                  : forward_as<Mid, Elem::kE4m3>(p, gated, stream);
+  if (type == Elem::kInt8)
+    return many_rows(p.cap, p.E) ? forward_as<Big, Elem::kInt8>(p, gated, stream)
+                                 : forward_as<Mid, Elem::kInt8>(p, gated, stream);
+  return many_rows(p.cap, p.E) ? forward_as<Big, Elem::kBf16>(p, gated, stream)
+                               : forward_as<Mid, Elem::kBf16>(p, gated, stream);
 }
 
 hipError_t launch_row_grad(const RowGradArgs& p, hipStream_t stream) {

@@ -37,11 +37,13 @@ __device__ __forceinline__ int nth_expert(const int32_t* expert_off, int E, int 
   return E;
 }
 
-template <int NF, bool FP8, bool GATED>
+template <int NF, Elem T, bool GATED>
 __global__ void __launch_bounds__(kFewWaves* kWave, 2) few_rows_kernel(ForwardArgs p) {
-  constexpr int kCols = 16 * NF / (GATED ? 2 : 1), kEsize = FP8 ? 1 : 2;
+  constexpr bool FP8 = T == Elem::kE4m3, INT8 = T == Elem::kInt8;
+  constexpr int kCols = 16 * NF / (GATED ? 2 : 1), kEsize = elem_bytes(T);
   constexpr int kUnits = kCols / 32;  // groups of 32 output columns
-  __shared__ f32x4 part[kFewWaves][NF][kWave];
+  using Acc = AccOf<T>;
+  __shared__ Acc part[kFewWaves][NF][kWave];
   const int wave = uniform(threadIdx.x / kWave), lane = threadIdx.x % kWave;
   const int rho = lane & 15, q = lane >> 4;
   const int nt = (p.N + kCols - 1) / kCols;
@@ -88,9 +90,9 @@ __global__ void __launch_bounds__(kFewWaves* kWave, 2) few_rows_kernel(ForwardAr
     }
     if constexpr (FP8) sc[d] = sp[std::min(s, nb - 1)];
   };
-  f32x4 acc[NF];
+  Acc acc[NF];
 #pragma unroll
-  for (int n = 0; n < NF; ++n) acc[n] = f32x4{0, 0, 0, 0};
+  for (int n = 0; n < NF; ++n) acc[n] = Acc{0, 0, 0, 0};
 #pragma unroll
   for (int d = 0; d < kDepth; ++d) load(d, wave + d * kFewWaves);
   for (int s = wave; s < steps; s += kDepth * kFewWaves) {
@@ -101,9 +103,14 @@ __global__ void __launch_bounds__(kFewWaves* kWave, 2) few_rows_kernel(ForwardAr
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int n = 0; n < NF; ++n)
-            acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b[d][n][h]),
-                                                             __builtin_bit_cast(bf16x8, a[d][h]), acc[n], 0, 0, 0);
+          for (int n = 0; n < NF; ++n) {
+            if constexpr (INT8)
+              acc[n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, b[d][n][h]),
+                                                             __builtin_bit_cast(i32x4, a[d][h]), acc[n], 0, 0, 0);
+            else
+              acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b[d][n][h]),
+                                                               __builtin_bit_cast(bf16x8, a[d][h]), acc[n], 0, 0, 0);
+          }
       } else {
         // As in run_tiles: a block's product joins the sum scaled, the instruction's own scales are one.
         const auto join = [](const u32x4(&h)[2]) EPL_INLINE {
@@ -130,17 +137,21 @@ __global__ void __launch_bounds__(kFewWaves* kWave, 2) few_rows_kernel(ForwardAr
     float v[8], u[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      v[i] = u[i] = 0.0f;
+      std::conditional_t<INT8, int, float> sv = 0, su = 0;
 #pragma unroll
       for (int w = 0; w < kFewWaves; ++w) {
-        v[i] += part[w][wave * 2 + i / 4][lane][i % 4];
-        if constexpr (GATED) u[i] += part[w][NF / 2 + wave * 2 + i / 4][lane][i % 4];
+        sv += part[w][wave * 2 + i / 4][lane][i % 4];
+        if constexpr (GATED) su += part[w][NF / 2 + wave * 2 + i / 4][lane][i % 4];
       }
+      v[i] = (float)sv;
+      u[i] = (float)su;
     }
     const int64_t cc = (int64_t)e * p.N + c, row = beg + rho;
-    if constexpr (FP8) {
+    if constexpr (FP8 || INT8) {
+      const float rs = INT8 ? p.a_scale[row] : 1.0f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
+        if constexpr (INT8) v[i] *= rs, u[i] *= rs;
         v[i] *= p.w_scale[cc + i];
         if constexpr (GATED) u[i] *= p.w2_scale[cc + i];
       }
@@ -180,18 +191,23 @@ __global__ void __launch_bounds__(kFewWaves* kWave, 2) few_rows_kernel(ForwardAr
   }
 }
 
-template <int NF, bool FP8, bool GATED>
+template <int NF, Elem T, bool GATED>
 static hipError_t launch_as(const ForwardArgs& p, hipStream_t stream) {
   constexpr int kCols = 16 * NF / (GATED ? 2 : 1);
   const int64_t grid = (int64_t)((p.N + kCols - 1) / kCols) * std::min(p.E, p.cap);
-  hipLaunchKernelGGL((few_rows_kernel<NF, FP8, GATED>), dim3((unsigned)grid), dim3(kFewWaves * kWave), 0,
+  hipLaunchKernelGGL((few_rows_kernel<NF, T, GATED>), dim3((unsigned)grid), dim3(kFewWaves * kWave), 0,
                      stream, p);
   return hipGetLastError();
 }
 
-hipError_t launch_forward_few(const ForwardArgs& p, bool fp8, bool gated, hipStream_t stream) {
-  if (gated) return fp8 ? launch_as<4, true, true>(p, stream) : launch_as<4, false, true>(p, stream);
-  return fp8 ? launch_as<2, true, false>(p, stream) : launch_as<2, false, false>(p, stream);
+template <Elem T>
+static hipError_t launch_type(const ForwardArgs& p, bool gated, hipStream_t stream) {
+  return gated ? launch_as<4, T, true>(p, stream) : launch_as<2, T, false>(p, stream);
+}
+
+hipError_t launch_forward_few(const ForwardArgs& p, Elem type, bool gated, hipStream_t stream) {
+  if (type == Elem::kInt8) return launch_type<Elem::kInt8>(p, gated, stream);
+  return type == Elem::kE4m3 ? launch_type<Elem::kE4m3>(p, gated, stream) : launch_type<Elem::kBf16>(p, gated, stream);
 }
 
 }  // namespace epl

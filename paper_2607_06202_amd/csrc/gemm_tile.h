@@ -1,7 +1,7 @@
 // Matrix-instruction tile shared by the experts' products (device only).
 //
 // A workgroup computes a BM x BN tile of D = A * B^T with 64-wide waves in a WM x WN arrangement. Both
-// operands pass through LDS in steps of 128 bytes of the reduction (64 bf16 or 128 E4M3 elements), and each may be
+// operands pass through LDS in steps of 128 bytes of the reduction (64 bf16 or 128 E4M3 or int8 elements), and each may be
 // stored either way round in memory:
 //   * reduction-contiguous ("rows"): LDS holds [rows][128 bytes]; a lane reads 16 bytes of its row;
 //   * reduction-major ("columns"):   LDS holds [64 reduction rows][columns]; a lane reads two 4x16 blocks that
@@ -22,6 +22,7 @@
 #include <type_traits>
 
 #include "epl_internal.h"
+#include "experts.h"
 
 namespace epl {
 
@@ -31,10 +32,11 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
-// Lambdas over register arrays: out of line they would put the arrays in memory.
-#define EPL_INLINE __attribute__((always_inline))
+// A lane's four sums.
+template <Elem T>
+using AccOf = std::conditional_t<T == Elem::kInt8, i32x4, f32x4>;
 
-constexpr int kStepBytes = 128;       // reduction bytes of a row per step: 64 bf16 or 128 E4M3 elements
+constexpr int kStepBytes = 128;       // reduction bytes of a row per step: 64 bf16 or 128 E4M3 or int8 elements
 constexpr int kOutOfRange = INT_MIN;  // as an unsigned offset, past every descriptor below 2 GiB
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
@@ -281,7 +283,7 @@ __device__ __forceinline__ void arrived(T& v) {
 //   finish(t, acc)                the end of a tile: a known number of buffer stores per wave, whatever is masked;
 //   wait<N>(stored)               wait_tiles<N>, or with the number of stores added.
 //
-// A step is a group of NF products for each row fragment and (bf16) 64 bytes of the reduction. The row fragment of a
+// A step is a group of NF products for each row fragment and (bf16, int8) 64 bytes of the reduction. The row fragment of a
 // group is read kAhead groups before it, into a ring of four, across the end of the step too: the barrier between
 // steps comes when the last kAhead groups' operands are in registers, so the matrix unit has their work while the
 // waves meet and the first reads of the next stage return. At that point every wave has read this stage, and the
@@ -299,8 +301,10 @@ __device__ __forceinline__ void arrived(T& v) {
 //
 // The next tile's first steps are loaded before this one's results are worked out and stored. Loads and stores leave
 // one in-order counter, so the first steps of a tile wait for all but the stores behind their loads.
-template <class S, bool ACOLS, bool BCOLS, bool FP8, bool SPLIT, class Job>
+template <class S, bool ACOLS, bool BCOLS, Elem T, bool SPLIT, class Job>
 __device__ __forceinline__ void run_tiles(Job& job, uint32_t lds, int wave, int lane) {
+  constexpr bool FP8 = T == Elem::kE4m3;
+  using Acc = AccOf<T>;
   constexpr int kStage = S::stage(FP8);
   using A = Operand<ACOLS, S::BM, S::kWaves, false>;
   using B = Operand<BCOLS, S::BN, S::kWaves, true, SPLIT>;
@@ -310,9 +314,9 @@ __device__ __forceinline__ void run_tiles(Job& job, uint32_t lds, int wave, int 
   constexpr int kLoads = A::kLoads + B::kLoads + (FP8 ? 1 : 0);
   constexpr int kLater = S::STAGES - 2;  // steps loading behind the one that a step waits for
   static_assert(kGroups % kRing == 0, "ring of row fragments");
-  static_assert(!FP8 || (!ACOLS && !BCOLS), "fp8 operands are rows of 128-element blocks");
+  static_assert(T == Elem::kBf16 || (!ACOLS && !BCOLS), "8-bit operands are rows");
   static_assert(kHalves == 2 || S::STAGES == 3, "steps() gives an fp8 tile one step more than the written-out three");
-  static_assert(!S::RING || kHalves == 2, "a ring holds bf16 steps of 128 bytes");
+  static_assert(!S::RING || kHalves == 2, "a ring holds steps of two halves");
   Fragments<S, ACOLS, BCOLS, SPLIT> fr;
   fr.init(wave, lane);
   const uint32_t scale_at = A::kBytes + B::kBytes + ((wave / S::WN) * S::MF * 16 + (lane & 15)) * 4;
@@ -320,7 +324,7 @@ __device__ __forceinline__ void run_tiles(Job& job, uint32_t lds, int wave, int 
   B b;
   Frag fa[kRing], fb[2][S::NF];  // fb: by half, or by the parity of the step where it has one
   float sc[2][S::MF];
-  f32x4 acc[S::MF][S::NF];
+  Acc acc[S::MF][S::NF];
   int at = 0;  // steps of the tile being loaded
   typename Job::Tile tile;
   // Load i of a step, B's first, into the tiles at to_a and to_b (fp8: the scales behind them).
@@ -404,7 +408,9 @@ __device__ __forceinline__ void run_tiles(Job& job, uint32_t lds, int wave, int 
       }
       static_for<0, S::NF>([&](auto n) EPL_INLINE {
         __builtin_amdgcn_sched_barrier(0);
-        if constexpr (!FP8) {
+        if constexpr (T == Elem::kInt8) {
+          acc[m][n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[bi][n], fa[g % kRing], acc[m][n], 0, 0, 0);
+        } else if constexpr (!FP8) {
           acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fb[bi][n]),
                                                               __builtin_bit_cast(bf16x8, fa[g % kRing]), acc[m][n], 0,
                                                               0, 0);
@@ -458,7 +464,7 @@ __device__ __forceinline__ void run_tiles(Job& job, uint32_t lds, int wave, int 
 #pragma unroll
     for (int m = 0; m < S::MF; ++m)
 #pragma unroll
-      for (int n = 0; n < S::NF; ++n) acc[m][n] = f32x4{0, 0, 0, 0};
+      for (int n = 0; n < S::NF; ++n) acc[m][n] = Acc{0, 0, 0, 0};
     job.template wait<S::RING ? 2 * A::kLoads + B::kLoads : kLoads*(S::STAGES - 1)>(stored > 0);
     cur = lds;
     fr.point(cur, b_of(cur));

@@ -1,0 +1,170 @@
+// Rows of bf16 to int8 with one scale a row: in dispatch (into the packed receive rows) and of rows where they are.
+//
+//   A = max|x|,  s = A / 127,  q = the integer nearest to 127 x / A, halves to even.
+//
+// The nearest integer is decided on the exact quotient, at the price of a multiplication. x and A have 8-bit mantissas, so
+// a quotient that is no half (n + 1/2) is at least 1.5e-5 of itself away from one: 254 X 2^a - (2 n + 1) A' 2^b is a whole
+// multiple of the smaller power of two, over 2 A'. x * (127 / A) in fp32 is off by 2^-23 of itself at most; rounded to
+// 20 bits (another 2^-20 = 9.5e-7 at most) a half comes out as that half and nothing else does. Adding 1.5 * 2^23 then
+// rounds to the nearest even integer and leaves it in the low byte. 127 / A is finite for every bf16 A but those below
+// 2^-121; x and A are taken times 2^100 where A is below 2^-100.
+//
+// A row is read once: it stays in registers between the maximum and the conversion.
+#include "epl_internal.h"
+#include "experts.h"
+
+namespace epl {
+
+constexpr int kInt8Threads = 256;
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+
+// A row of n pieces of 16 elements in the registers of GROUP threads, UNITS pieces each; longer rows in passes.
+template <int GROUP, int UNITS>
+struct Int8Row {
+  u32x4 v[UNITS][2];
+  const u32x4* row;
+  int n, t;
+  // Pieces past the last one are the last one again.
+  __device__ __forceinline__ void load(int first) {
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) {
+      const int u = std::min(first + i * GROUP + t, n - 1);
+      v[i][0] = row[2 * u];
+      v[i][1] = row[2 * u + 1];
+    }
+  }
+  // The larger of m and the magnitudes' bits, by halves.
+  __device__ __forceinline__ u16x2 top(u16x2 m) const {
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, v[i][j / 4][j % 4] & 0x7FFF7FFFu));
+    return m;
+  }
+};
+
+// What a row's largest magnitude (bf16 bits) makes of it.
+struct Int8Scale {
+  float s, pre, mul;  // the row's scale; x * pre * mul is the quotient
+  bool zero;          // q is 0 whatever x is
+  __device__ __forceinline__ explicit Int8Scale(uint32_t bits) {
+    const float a = __uint_as_float(bits << 16);
+    zero = bits == 0 || bits >= 0x7F80u;
+    s = bits >= 0x7F80u ? __uint_as_float(0x7FC00000u) : a / 127.0f;
+    pre = a < 0x1p-100f ? 0x1p100f : 1.0f;
+    mul = 127.0f / (a * pre);
+  }
+  // The low byte is q.
+  __device__ __forceinline__ uint32_t one(float x) const {
+    const uint32_t t = __float_as_uint(x * pre * mul);
+    return __float_as_uint(__uint_as_float((t + 8u) & ~15u) + 12582912.0f);
+  }
+  __device__ __forceinline__ uint32_t four(uint32_t lo, uint32_t hi) const {
+    const uint32_t a = one(bf16lo_to_f32(lo)), b = one(bf16hi_to_f32(lo)), c = one(bf16lo_to_f32(hi)), d = one(bf16hi_to_f32(hi));
+    return __builtin_amdgcn_perm(b, a, 0x0C0C0400u) | __builtin_amdgcn_perm(d, c, 0x04000C0Cu);
+  }
+  __device__ __forceinline__ u32x4 sixteen(const u32x4 (&v)[2]) const {
+    if (zero) return u32x4{0, 0, 0, 0};
+    return u32x4{four(v[0][0], v[0][1]), four(v[0][2], v[0][3]), four(v[1][0], v[1][1]), four(v[1][2], v[1][3])};
+  }
+};
+
+// The largest over the group's threads; every thread of the workgroup is here if the group is one.
+template <int GROUP>
+__device__ __forceinline__ uint32_t group_max(u16x2 m) {
+  uint32_t v = std::max<uint32_t>(m[0], m[1]);
+#pragma unroll
+  for (int off = kWave / 2; off > 0; off >>= 1) v = std::max(v, (uint32_t)__shfl_xor((int)v, off, kWave));
+  if constexpr (GROUP > kWave) {
+    __shared__ uint32_t part[GROUP / kWave];
+    __syncthreads();  // the last row's have been read
+    if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = v;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < GROUP / kWave; ++i) v = std::max(v, part[i]);
+  }
+  return (uint32_t)__builtin_amdgcn_readfirstlane((int)v);
+}
+
+// One row: put(piece, its 16 values) of every piece and put_scale(s) once.
+template <int GROUP, int UNITS, class Put, class PutScale>
+__device__ __forceinline__ void quantise_row(const u32x4* row, int n, int t, Put&& put, PutScale&& put_scale) {
+  constexpr int kPass = GROUP * UNITS;
+  Int8Row<GROUP, UNITS> r;
+  r.row = row;
+  r.n = n;
+  r.t = t;
+  u16x2 m = {0, 0};
+  for (int first = 0; first < n; first += kPass) {
+    r.load(first);
+    m = r.top(m);
+  }
+  const Int8Scale scale(group_max<GROUP>(m));
+  put_scale(scale.s);
+  for (int first = 0; first < n; first += kPass) {
+    if (n > kPass) r.load(first);
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) {
+      const int u = first + i * GROUP + t;
+      if (u < n) put(u, scale.sixteen(r.v[i]));
+    }
+  }
+}
+
+template <int GROUP, int UNITS>
+__global__ void __launch_bounds__(kInt8Threads)
+    quantize_rows_kernel(const u32x4* a, u32x4* q, float* scale, const int32_t* count, int64_t rows, int n, int64_t a_ld,
+                         int64_t q_ld) {
+  constexpr int kPer = kInt8Threads / GROUP;
+  const int t = threadIdx.x % GROUP;
+  if (count) rows = std::min<int64_t>(std::max(*count, 0), rows);
+  for (int64_t r = (int64_t)blockIdx.x * kPer + threadIdx.x / GROUP; r < rows; r += (int64_t)gridDim.x * kPer)
+    quantise_row<GROUP, UNITS>(
+        a + r * a_ld, n, t, [&](int u, u32x4 v) EPL_INLINE { q[r * q_ld + u] = v; },
+        [&](float s) EPL_INLINE {
+          if (t == 0) scale[r] = s;
+        });
+}
+
+template <int GROUP, int UNITS>
+__global__ void __launch_bounds__(kInt8Threads)
+    dispatch_int8_kernel(const u32x4* x, const float* w, const int32_t* pair_row, u32x4* recv, float* scale, int64_t T,
+                         int k, int n, int64_t ld, int64_t cap) {
+  constexpr int kPer = kInt8Threads / GROUP;
+  const int t = threadIdx.x % GROUP, lane = threadIdx.x % kWave;
+  for (int64_t g = (int64_t)blockIdx.x * kPer + threadIdx.x / GROUP; g < T; g += (int64_t)gridDim.x * kPer) {
+    int mine = lane < k ? pair_row[g * k + lane] : -1;
+    if (mine >= cap) mine = -1;
+    quantise_row<GROUP, UNITS>(
+        x + g * 2 * n, n, t,
+        [&](int u, u32x4 v) EPL_INLINE {
+          for (int j = 0; j < k; ++j) {
+            const int row = __builtin_amdgcn_readlane(mine, j);
+            if (row >= 0) recv[row * ld + u] = v;
+          }
+        },
+        [&](float s) EPL_INLINE {
+          if (t < kWave && mine >= 0) scale[mine] = w ? s * w[g * k + lane] : s;
+        });
+  }
+}
+
+hipError_t launch_quantize_rows(const void* a, void* q, float* scale, const int32_t* n, int64_t rows, int K, int64_t a_ld,
+                                int64_t q_ld, hipStream_t stream) {
+  if (rows == 0) return hipSuccess;
+  hipLaunchKernelGGL((quantize_rows_kernel<kInt8Threads, 8>), dim3(unit_grid(rows, 1, kInt8Threads)), dim3(kInt8Threads), 0,
+                     stream, static_cast<const u32x4*>(a), static_cast<u32x4*>(q), scale, n, rows, K / 16, a_ld, q_ld);
+  return hipGetLastError();
+}
+
+hipError_t launch_dispatch_int8(const void* x, const float* w, const int32_t* pair_row, void* recv, float* scale, int64_t T,
+                                int k, int H, int pitch, int64_t cap, hipStream_t stream) {
+  if (T == 0) return hipSuccess;
+  hipLaunchKernelGGL((dispatch_int8_kernel<kInt8Threads, 8>), dim3(unit_grid(T, 1, kInt8Threads)), dim3(kInt8Threads), 0,
+                     stream, static_cast<const u32x4*>(x), w, pair_row, static_cast<u32x4*>(recv), scale, T, k, H / 16,
+                     (int64_t)pitch / 16, cap);
+  return hipGetLastError();
+}
+
+}  // namespace epl

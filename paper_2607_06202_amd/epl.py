@@ -24,6 +24,7 @@ PAYLOAD_FP8_E4M3 = 1
 MAX_EXPERTS = 1024
 MAX_TOPK = 32
 MAX_HOP_CLASSES = 8  # EPL_MAX_HOP_CLASSES
+MAX_INT8_FEATURES = 131056  # EPL_MAX_INT8_FEATURES: features in of an int8 product
 STATIC_SCRATCH_BYTES = 8 << 20  # EPL_STATIC_SCRATCH_BYTES: the library's own workspace per GPU
 
 STATUS = {0: "EPL_OK", 1: "EPL_ERR_INVALID_ARG", 2: "EPL_ERR_ALIGN", 3: "EPL_ERR_CAPACITY",
@@ -116,6 +117,10 @@ class Linear(ctypes.Structure):
     _fields_ += [("expert_stride", ctypes.c_int64)]
 
 
+class Quantize(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("features", "in_pitch", "out_pitch")]
+
+
 class LayoutBuffers(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("send_cnt", "rank_cnt", "expert_off", "rank_off", "seg_off",
                                                "tok_nranks", "pair_row", "pair_rslot", "recv_src", "recv_j",
@@ -186,6 +191,7 @@ def lib() -> ctypes.CDLL:
         L.epl_dispatch_scheduled.restype = ctypes.c_int
         L.epl_dispatch_scheduled.argtypes = [CP, P, LP, P, P, I64, I32, I32, P]
         RP, GP, NP = ctypes.POINTER(RouteOpts), ctypes.POINTER(Gated), ctypes.POINTER(Linear)
+        QP = ctypes.POINTER(Quantize)
         for name, args in [
                 ("epl_route", [CP, RP, P, P, P, P, P]),
                 ("epl_route_backward", [CP, RP, P, P, P, P, P]),
@@ -193,7 +199,13 @@ def lib() -> ctypes.CDLL:
                 ("epl_experts_gated_backward", [CP, GP, P, P, P, I64, LP, P, P, P, P, P, P, P]),
                 ("epl_experts_linear", [CP, NP, P, P, I64, LP, P, P, P, P, P, P, P]),
                 ("epl_experts_linear_backward", [CP, NP, P, P, P, I64, LP, P, P, P, P, P, P]),
-                ("epl_combine_backward", [CP, P, P, P, LP, P, I64, P, P])]:
+                ("epl_combine_backward", [CP, P, P, P, LP, P, I64, P, P]),
+                ("epl_dispatch_weighted", [CP, P, P, LP, P, I64, P]),
+                ("epl_dispatch_backward", [CP, P, I64, P, P, LP, P, P, P]),
+                ("epl_dispatch_int8", [CP, P, P, LP, P, P, I64, P]),
+                ("epl_quantize_rows", [CP, QP, P, I64, LP, P, P, P]),
+                ("epl_experts_gated_int8", [CP, GP, P, P, I64, LP, P, P, P, P, P, P]),
+                ("epl_experts_linear_int8", [CP, NP, P, P, I64, LP, P, P, P, P, P, P])]:
             getattr(L, name).restype = ctypes.c_int
             getattr(L, name).argtypes = args
         _lib = L
@@ -902,11 +914,11 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _rows_out(t, cfg: Config, width: int, dev, pitch: int = 0) -> torch.Tensor:
-    """t, or a new [T*k, width] bf16 buffer of packed rows pitch (0: width) elements apart."""
+def _rows_out(t, cfg: Config, width: int, dev, pitch: int = 0, dtype=torch.bfloat16) -> torch.Tensor:
+    """t, or a new [T*k, width] buffer of packed rows pitch (0: width) elements apart."""
     if t is not None:
         return t
-    return torch.empty(max(recv_rows_cap(cfg), 1), pitch or width, dtype=torch.bfloat16, device=dev)[:, :width]
+    return torch.empty(max(recv_rows_cap(cfg), 1), pitch or width, dtype=dtype, device=dev)[:, :width]
 
 
 def experts_gated(cfg: Config, recv: torch.Tensor, L: Layout, w_gate: torch.Tensor, w_up: torch.Tensor,
@@ -1095,6 +1107,173 @@ def combine_backward(cfg: Config, dout: torch.Tensor, y: torch.Tensor, topk_w: t
     _call(dev, "epl_combine_backward", ctypes.byref(cfg), dout.data_ptr(), y.data_ptr(), topk_w.data_ptr(),
           ctypes.byref(bufs), dy.data_ptr(), dy.shape[0], dtopk_w.data_ptr())
     return dy, dtopk_w
+
+
+def _tokens(t, name: str, cfg: Config) -> None:
+    _dev(t, name, torch.bfloat16)
+    if _rows_of(t, name, cfg.hidden) < cfg.T:
+        raise ValueError("%s has %d rows, needs T = %d" % (name, t.shape[0], cfg.T))
+
+
+def _row_scales(t, name: str, rows: int) -> int:
+    """One fp32 scale a row: 1-D [>= rows]."""
+    p = _dev(t, name, torch.float32)
+    if t.dim() != 1 or t.shape[0] < rows:
+        raise ValueError("%s must be 1-D with at least %d values, got shape %s" % (name, rows, tuple(t.shape)))
+    return p
+
+
+def dispatch_weighted(cfg: Config, x: torch.Tensor, topk_w: torch.Tensor, L: Layout,
+                      recv: torch.Tensor | None = None) -> torch.Tensor:
+    """epl_dispatch_weighted: x [T, H] bf16 and topk_w [T, k] fp32 -> recv [T*k, H] bf16 at cfg's pitch, the rows of
+    dispatch each times its gate weight (for experts that take weighted inputs; combine then adds their outputs with
+    weights of one)."""
+    dev = x.device
+    _tokens(x, "x", cfg)
+    _per_choice(cfg, topk_w, "topk_w", torch.float32)
+    _check_layout(cfg, L, dev)
+    recv = _rows_out(recv, cfg, cfg.hidden, dev, cfg.pitch)
+    _packed(recv, "recv", torch.bfloat16, cfg.hidden, cfg, cfg.pitch)
+    _same_device(dev, topk_w=topk_w, recv=recv)
+    bufs = L.buffers()
+    _call(dev, "epl_dispatch_weighted", ctypes.byref(cfg), x.data_ptr(), topk_w.data_ptr(), ctypes.byref(bufs),
+          recv.data_ptr(), recv.shape[0])
+    return recv
+
+
+def dispatch_backward(cfg: Config, drecv: torch.Tensor, x: torch.Tensor, topk_w: torch.Tensor, L: Layout,
+                      dx: torch.Tensor | None = None, dtopk_w: torch.Tensor | None = None):
+    """epl_dispatch_backward: the gradients of dispatch_weighted from drecv [T*k, H] bf16 (at cfg's pitch) and the x and
+    topk_w of the forward call -> (dx [T, H] bf16, dtopk_w [T, k] fp32). dx may be x itself."""
+    dev = drecv.device
+    _packed(drecv, "drecv", torch.bfloat16, cfg.hidden, cfg, cfg.pitch)
+    _tokens(x, "x", cfg)
+    _per_choice(cfg, topk_w, "topk_w", torch.float32)
+    _check_layout(cfg, L, dev)
+    if dx is None:
+        dx = torch.empty(max(cfg.T, 1), cfg.hidden, dtype=torch.bfloat16, device=dev)
+    _tokens(dx, "dx", cfg)
+    if dtopk_w is None:
+        dtopk_w = torch.empty(max(cfg.T, 1), cfg.topk, dtype=torch.float32, device=dev)
+    _per_choice(cfg, dtopk_w, "dtopk_w", torch.float32)
+    _same_device(dev, x=x, topk_w=topk_w, dx=dx, dtopk_w=dtopk_w)
+    bufs = L.buffers()
+    _call(dev, "epl_dispatch_backward", ctypes.byref(cfg), drecv.data_ptr(), drecv.shape[0], x.data_ptr(),
+          topk_w.data_ptr(), ctypes.byref(bufs), dx.data_ptr(), dtopk_w.data_ptr())
+    return dx, dtopk_w
+
+
+def dispatch_int8(cfg: Config, x: torch.Tensor, L: Layout, topk_w: torch.Tensor | None = None,
+                  recv: torch.Tensor | None = None, recv_scale: torch.Tensor | None = None):
+    """epl_dispatch_int8: x [T, H] bf16 (H a multiple of 16) -> (recv [T*k, H] int8 at cfg's pitch, recv_scale [T*k]
+    fp32), the rows of dispatch in int8 with one scale each; with topk_w [T, k] fp32 each scale is times the row's gate
+    weight. cfg's payload is not used."""
+    dev = x.device
+    _tokens(x, "x", cfg)
+    if topk_w is not None:
+        _per_choice(cfg, topk_w, "topk_w", torch.float32)
+    _check_layout(cfg, L, dev)
+    recv = _rows_out(recv, cfg, cfg.hidden, dev, cfg.pitch, torch.int8)
+    _packed(recv, "recv", torch.int8, cfg.hidden, cfg, cfg.pitch)
+    rows = recv_rows_cap(cfg)
+    if recv_scale is None:
+        recv_scale = torch.empty(max(rows, 1), dtype=torch.float32, device=dev)
+    sp = _row_scales(recv_scale, "recv_scale", rows)
+    _same_device(dev, topk_w=topk_w, recv=recv, recv_scale=recv_scale)
+    bufs = L.buffers()
+    _call(dev, "epl_dispatch_int8", ctypes.byref(cfg), x.data_ptr(), _ptr(topk_w), ctypes.byref(bufs), recv.data_ptr(), sp,
+          rows)
+    return recv, recv_scale
+
+
+def quantize_rows(cfg: Config, a: torch.Tensor, L: Layout, q: torch.Tensor | None = None,
+                  q_scale: torch.Tensor | None = None):
+    """epl_quantize_rows on packed rows: a [T*k, K] bf16 (rows any pitch apart, K a multiple of 16) -> (q [T*k, K] int8,
+    q_scale [T*k] fp32), as dispatch_int8 makes them; rows behind the last one are left as they are."""
+    dev = a.device
+    rows = recv_rows_cap(cfg)
+    if a.dim() != 2:
+        raise ValueError("a must be 2-D, got shape %s" % (tuple(a.shape),))
+    K = a.shape[1]
+    lda = _packed(a, "a", torch.bfloat16, K, cfg)
+    q = _rows_out(q, cfg, K, dev, 0, torch.int8)
+    ldq = _packed(q, "q", torch.int8, K, cfg)
+    if q_scale is None:
+        q_scale = torch.empty(max(rows, 1), dtype=torch.float32, device=dev)
+    sp = _row_scales(q_scale, "q_scale", rows)
+    _check_layout(cfg, L, dev)
+    _same_device(dev, q=q, q_scale=q_scale)
+    z = Quantize(_int32(K, "features"), _int32(lda, "a's pitch"), _int32(ldq, "q's pitch"))
+    bufs = L.buffers()
+    _call(dev, "epl_quantize_rows", ctypes.byref(cfg), ctypes.byref(z), a.data_ptr(), rows, ctypes.byref(bufs),
+          q.data_ptr(), sp)
+    return q, q_scale
+
+
+def quantize_weights(w: torch.Tensor):
+    """epl_quantize_rows on a layer's matrices: w [E, N, K] bf16, contiguous, K a multiple of 16 -> (q [E, N, K] int8,
+    scale [E, N] fp32), as experts_gated_int8 and experts_linear_int8 take them."""
+    _dev(w, "w", torch.bfloat16)
+    if w.dim() != 3:
+        raise ValueError("w must be [E, out, in], got %s" % (tuple(w.shape),))
+    E, N, K = w.shape
+    q = torch.empty(E, N, K, dtype=torch.int8, device=w.device)
+    scale = torch.empty(E, N, dtype=torch.float32, device=w.device)
+    z = Quantize(_int32(K, "features"), 0, 0)
+    _call(w.device, "epl_quantize_rows", None, ctypes.byref(z), w.data_ptr(), E * N, None, q.data_ptr(), scale.data_ptr())
+    return q, scale
+
+
+def experts_gated_int8(cfg: Config, recv: torch.Tensor, recv_scale: torch.Tensor, L: Layout, w_gate: torch.Tensor,
+                       gate_scale: torch.Tensor, w_up: torch.Tensor, up_scale: torch.Tensor, activation: str = "silu",
+                       h: torch.Tensor | None = None) -> torch.Tensor:
+    """epl_experts_gated_int8: experts_gated on int8 rows and weights. recv [T*k, H] int8 and recv_scale [T*k] as
+    dispatch_int8 makes them; w_gate, w_up [E, I, H] int8 and gate_scale, up_scale [E, I] fp32 as quantize_weights makes
+    them -> h [T*k, I] bf16 (quantize_rows makes the down projection's rows of it)."""
+    dev = recv.device
+    _packed(recv, "recv", torch.int8, cfg.hidden, cfg, cfg.pitch)
+    stride = _matrices(w_gate, "w_gate", torch.int8, cfg)
+    inner = w_gate.shape[1]
+    if w_gate.shape[2] != cfg.hidden or _matrices(w_up, "w_up", torch.int8, cfg, (inner, cfg.hidden)) != stride:
+        raise ValueError("w_gate and w_up must be [E, I, %d] with one stride between experts" % cfg.hidden)
+    rows = recv_rows_cap(cfg)
+    sp = [_row_scales(recv_scale, "recv_scale", rows), _scales(gate_scale, "gate_scale", cfg.num_experts, inner),
+          _scales(up_scale, "up_scale", cfg.num_experts, inner)]
+    h = _rows_out(h, cfg, inner, dev)
+    _packed(h, "h", torch.bfloat16, inner, cfg, inner)
+    _check_layout(cfg, L, dev)
+    _same_device(dev, recv_scale=recv_scale, gate_scale=gate_scale, up_scale=up_scale, w_gate=w_gate, w_up=w_up, h=h)
+    g = Gated(_int32(inner, "inner features"), _one_of(ACTIVATION, activation, "activation"), stride)
+    bufs = L.buffers()
+    _call(dev, "epl_experts_gated_int8", ctypes.byref(cfg), ctypes.byref(g), recv.data_ptr(), sp[0], rows,
+          ctypes.byref(bufs), w_gate.data_ptr(), w_up.data_ptr(), sp[1], sp[2], h.data_ptr())
+    return h
+
+
+def experts_linear_int8(cfg: Config, a: torch.Tensor, a_scale: torch.Tensor, L: Layout, w: torch.Tensor,
+                        w_scale: torch.Tensor, bias: torch.Tensor | None = None, residual: torch.Tensor | None = None,
+                        activation: str = "none", out: torch.Tensor | None = None) -> torch.Tensor:
+    """epl_experts_linear_int8: experts_linear on int8 rows and weights. a [T*k, K] int8 (rows any pitch apart) and
+    a_scale [T*k]; w [E, N, K] int8 and w_scale [E, N] fp32; bias [E, N], residual [T*k, N] bf16 -> out [T*k, N] bf16.
+    A new out of cfg.hidden columns has cfg's pitch, as combine reads it."""
+    dev = a.device
+    stride = _matrices(w, "w", torch.int8, cfg)
+    N, K = w.shape[1], w.shape[2]
+    lda = _packed(a, "a", torch.int8, K, cfg)
+    rows = recv_rows_cap(cfg)
+    sp = [_row_scales(a_scale, "a_scale", rows), _scales(w_scale, "w_scale", cfg.num_experts, N)]
+    bp = _biases(bias, "bias", cfg, N)
+    out = _rows_out(out, cfg, N, dev, cfg.pitch if N == cfg.hidden else 0)
+    ldo = _packed(out, "out", torch.bfloat16, N, cfg)
+    ldr = 0 if residual is None else _packed(residual, "residual", torch.bfloat16, N, cfg)
+    _check_layout(cfg, L, dev)
+    _same_device(dev, a_scale=a_scale, w=w, w_scale=w_scale, bias=bias, residual=residual, out=out)
+    lin = Linear(_int32(K, "in_features"), _int32(N, "out_features"), _int32(lda, "a's pitch"), _int32(ldo, "out's pitch"),
+                 _int32(ldr, "residual's pitch"), _one_of(ACTIVATION, activation, "activation"), 0, stride)
+    bufs = L.buffers()
+    _call(dev, "epl_experts_linear_int8", ctypes.byref(cfg), ctypes.byref(lin), a.data_ptr(), sp[0], rows,
+          ctypes.byref(bufs), w.data_ptr(), sp[1], bp, _ptr(residual), out.data_ptr())
+    return out
 
 
 class PreparedLayer:
