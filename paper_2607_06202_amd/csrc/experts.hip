@@ -79,6 +79,9 @@ struct ForwardJob {
   const ForwardArgs& p;
   int wave, lane, nt, steps;
   LanePlace<S, GATED> at;
+  // int8: the scales of the lane's rows and columns and its columns' bias (see gather).
+  float rs[INT8 ? S::MF : 1], cs[INT8 ? kPairs : 1][8], cs2[INT8 && GATED ? kPairs : 1][8];
+  u32x4 cb[INT8 && !GATED ? kPairs : 1];
   __device__ __forceinline__ ForwardJob(const ForwardArgs& p_, int wave_, int lane_)
       : p(p_), wave(wave_), lane(lane_), at(wave_, lane_) {
     nt = (p.N + kCols - 1) / kCols;
@@ -134,13 +137,47 @@ struct ForwardJob {
     else
       wait_tiles<std::min(63, N + kEach * (GATED ? 3 : 2))>();
   }
-  __device__ __forceinline__ void finish(const Tile& t, AccOf<T> (&acc)[S::MF][S::NF]) const {
-    const int cols = std::min(p.N - t.col0, kCols);
-    float rs[S::MF];  // int8: the scales of the lane's rows
+  // Before the last step of a tile: what its end reads besides the sums. Loaded later, it would come behind the next
+  // tile's first steps, and the end could not begin until they are there.
+  __device__ __forceinline__ void gather(const Tile& t) {
     if constexpr (INT8) {
+      const int cols = std::min(p.N - t.col0, kCols);
 #pragma unroll
       for (int f = 0; f < S::MF; ++f) rs[f] = p.a_scale[t.row0 + std::min(at.row + f * 16, t.rows - 1)];
+#pragma unroll
+      for (int g = 0; g < kPairs; ++g) {
+        const int64_t cc = (int64_t)t.e * p.N + t.col0 + std::min(at.col + g * 32, cols - 8);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          cs[g][i] = p.w_scale[cc + i];
+          if constexpr (GATED) cs2[g][i] = p.w2_scale[cc + i];
+        }
+        if constexpr (!GATED) {
+          cb[g] = p.bias ? *(const u32x4*)(p.bias + cc * 2) : u32x4{0, 0, 0, 0};
+        }
+      }
     }
+  }
+  __device__ __forceinline__ void gathered() {
+    if constexpr (INT8) {
+#pragma unroll
+      for (int f = 0; f < S::MF; ++f) arrived(rs[f]);
+#pragma unroll
+      for (int g = 0; g < kPairs; ++g) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          arrived(cs[g][i]);
+          if constexpr (GATED) arrived(cs2[g][i]);
+        }
+        if constexpr (!GATED) arrived(cb[g]);
+      }
+    }
+  }
+  __device__ __forceinline__ void finish(const Tile& t, AccOf<T> (&acc)[S::MF][S::NF]) const {
+    const int cols = std::min(p.N - t.col0, kCols);
+    int row0 = at.row, col = at.col;
+    // Not to be worked out once for all tiles: the offsets of all stores are more than the registers that the steps leave.
+    if constexpr (INT8) asm volatile("" : "+v"(row0), "+v"(col));
     const TileOut out(p.out, t.row0, p.out_ld, t.col0, t.rows, cols);
     const int64_t pre_ld = (int64_t)p.N * (GATED ? 4 : 2);
     const TileOut pre(p.pre, t.row0, pre_ld, t.col0, t.rows, cols);
@@ -148,26 +185,33 @@ struct ForwardJob {
     constexpr int kTake = kPairs % 2 ? 1 : 2;  // groups of 32 columns stored together
 #pragma unroll
     for (int g0 = 0; g0 < kPairs; g0 += kTake) {
-      const int c0 = at.col + g0 * 32;
+      const int c0 = col + g0 * 32;
       float s1[kTake][8], s2[kTake][8], bias[kTake][8];
 #pragma unroll
       for (int k = 0; k < kTake; ++k) {
         // In range for the lanes past the last column.
         const int64_t cc = (int64_t)t.e * p.N + t.col0 + std::min(c0 + k * 32, cols - 8);
-        if constexpr (FP8 || INT8) {
+        if constexpr (FP8) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             s1[k][i] = p.w_scale[cc + i];
             if constexpr (GATED) s2[k][i] = p.w2_scale[cc + i];
           }
         }
-        if constexpr (!GATED) {
+        if constexpr (INT8) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            s1[k][i] = cs[g0 + k][i];
+            if constexpr (GATED) s2[k][i] = cs2[g0 + k][i];
+          }
+          if constexpr (!GATED) unpack8(cb[g0 + k], bias[k]);
+        } else if constexpr (!GATED) {
           if (p.bias) unpack8(*(const u32x4*)(p.bias + cc * 2), bias[k]);
         }
       }
 #pragma unroll
       for (int f = 0; f < S::MF; ++f) {
-        const int r = at.row + f * 16;
+        const int r = row0 + f * 16;
         float v[kTake][8], u[kTake][8];
 #pragma unroll
         for (int j = 0; j < kTake * 8; ++j) {
@@ -190,7 +234,7 @@ struct ForwardJob {
         with_activation(p.act, [&](auto act) EPL_INLINE {
 #pragma unroll
           for (int j = 0; j < kTake * 8; ++j) {
-            v[j / 8][j % 8] = activate<act>(v[j / 8][j % 8]);
+            v[j / 8][j % 8] = activate<act, INT8>(v[j / 8][j % 8]);
             if constexpr (GATED) v[j / 8][j % 8] *= u[j / 8][j % 8];
           }
         });
@@ -278,6 +322,8 @@ struct RowGradJob {
     b.start_cols(w + (t.e * p.expert_stride + t.col0) * 2, p.N, std::min(p.K - t.col0, S::BN), ldb);
   }
   // The second part's first step. (An only part's padded step may have that number too.)
+  __device__ __forceinline__ void gather(const Tile&) const {}
+  __device__ __forceinline__ void gathered() const {}
   template <class A, class B>
   __device__ __forceinline__ void turn(const Tile& t, int step, A& a, B& b) const {
     if (p.parts == 2 && step == part_steps) start(t, 1, p.w2, a, b);
@@ -344,6 +390,8 @@ struct WeightGradJob {
     t.t += gridDim.x;
     return place(t);
   }
+  __device__ __forceinline__ void gather(const Tile&) const {}
+  __device__ __forceinline__ void gathered() const {}
   template <class A, class B>
   __device__ __forceinline__ void turn(const Tile&, int, A&, B&) const {}
   template <class A, class B>

@@ -175,7 +175,7 @@ __global__ void __launch_bounds__(kFewWaves* kWave, 2) few_rows_kernel(ForwardAr
     with_activation(p.act, [&](auto act) EPL_INLINE {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        v[i] = activate<act>(v[i]);
+        v[i] = activate<act, INT8>(v[i]);
         if constexpr (GATED) v[i] *= u[i];
       }
     });

@@ -280,6 +280,7 @@ __device__ __forceinline__ void arrived(T& v) {
 //   begin(t, a, b)                sets the operands up for step 0 of tile t;
 //   turn(t, step, a, b)           the same for a later step at which a source changes;
 //   load_scales(t, step, lds)     fp8: one load per wave that brings the step's row scales to lds;
+//   gather(t), gathered()         before a tile's last step, and before the next tile's first loads: reads for its end;
 //   finish(t, acc)                the end of a tile: a known number of buffer stores per wave, whatever is masked;
 //   wait<N>(stored)               wait_tiles<N>, or with the number of stores added.
 //
@@ -478,12 +479,14 @@ __device__ __forceinline__ void run_tiles(Job& job, uint32_t lds, int wave, int 
       if constexpr (kHalves == 1) step(std::integral_constant<int, 1 - kOdd>{}, Middle{});
     }
     static_for<0, S::kFinal>([&](auto i) EPL_INLINE {
+      if constexpr (i == S::kFinal - 1) job.gather(tile);
       step(std::integral_constant<int, kHalves == 2 ? 0 : (kOdd + i) % 2>{},
            std::integral_constant<int, S::kFinal - 1 - i>{});
     });
     const typename Job::Tile done = tile;
     const bool more = job.next(tile);
     wait_tiles<0>();  // every wave has read the last stages
+    job.gathered();
     if (more) begin_tile();
     job.finish(done, acc);
     if (!more) return;
@@ -573,8 +576,18 @@ __device__ __forceinline__ float tail_ratio(float a) {
 // exp(-v^2 / 4): twice as a factor, so that products with exp(-v^2 / 2) below fp32's normal range still come out.
 __device__ __forceinline__ float bell_root(float v) { return __builtin_amdgcn_exp2f(v * v * -0.36067376022224085f); }
 
-template <int ACT>
+// QUICK: SiLU without the library's exponential and without a division.
+template <int ACT, bool QUICK = false>
 __device__ __forceinline__ float activate(float v) {
+  if constexpr (ACT == EPL_ACT_SILU && QUICK) {
+    // 2^t from t = -|v| / (2 ln 2), in two parts, so that it is right relative to its value; twice as a factor, so that the
+    // product comes out where exp(-|v|) is below fp32's normal range. From |v| = 200 on that is 0 either way (and rest
+    // would be a NaN for an infinity).
+    const float a = fminf(fabsf(v), 200.0f), t = a * -0.72134752f;
+    const float rest = fmaf(a, -9.6298151e-9f, fmaf(a, -0.72134752f, -t)) * 0.69314718f;
+    const float p = __builtin_amdgcn_exp2f(t), e = fmaf(p, rest, p);
+    return (v < 0.0f ? v * e * e : v) * __builtin_amdgcn_rcpf(fmaf(e, e, 1.0f));
+  }
   if constexpr (ACT == EPL_ACT_SILU) {
     // From exp(-|v|), which cannot overflow: v / (1 + exp(-v)) is 0 below -88.7, where the value is -2.6e-37.
     const float e = expf(-fabsf(v));
