@@ -78,17 +78,24 @@ struct ForwardJob {
   };
   const ForwardArgs& p;
   int wave, lane, nt, steps;
-  LanePlace<S, GATED> at;
-  // int8: the scales of the lane's rows and columns and its columns' bias (see gather).
-  float rs[INT8 ? S::MF : 1], cs[INT8 ? kPairs : 1][8], cs2[INT8 && GATED ? kPairs : 1][8];
-  u32x4 cb[INT8 && !GATED ? kPairs : 1];
+  // The lane, for int8 not to be seen through: what follows from it is worked out for each tile. Once for all tiles would
+  // be cheaper but for the registers (all offsets of a tile's loads and stores), of which the steps leave too few.
+  __device__ __forceinline__ int my_lane() const {
+    int l = lane;
+    if constexpr (INT8) asm volatile("" : "+v"(l));
+    return l;
+  }
+  // int8: what the tile's end takes besides the sums, one value a lane (see gather), and the experts' offsets (see find).
+  float row_scale[S::MF / 4], col_scale, col_bias;
+  Offsets offsets;
   __device__ __forceinline__ ForwardJob(const ForwardArgs& p_, int wave_, int lane_)
-      : p(p_), wave(wave_), lane(lane_), at(wave_, lane_) {
+      : p(p_), wave(wave_), lane(lane_) {
     nt = (p.N + kCols - 1) / kCols;
     steps = S::steps(p.K * kEsize, FP8);
   }
-  __device__ __forceinline__ bool place(Tile& t) const {
-    if (!t.at.template find<S::BM>(p.expert_off, p.E, p.cap, t.t / nt, lane)) return false;
+  __device__ __forceinline__ bool place(Tile& t) {
+    Offsets fresh;
+    if (!t.at.template find<S::BM>(p.expert_off, p.E, p.cap, t.t / nt, lane, INT8 ? offsets : fresh)) return false;
     int m, n;
     t.e = t.at.e;
     band_tile(t.t - t.at.before * nt, t.at.count, nt, 8, m, n);
@@ -98,24 +105,37 @@ struct ForwardJob {
     t.steps = steps;
     return true;
   }
-  __device__ __forceinline__ bool first(Tile& t) const {
+  __device__ __forceinline__ bool first(Tile& t) {
     t = Tile{};
     t.t = xcd_slot(blockIdx.x, gridDim.x);
     return place(t);
   }
-  __device__ __forceinline__ bool next(Tile& t) const {
+  __device__ __forceinline__ bool next(Tile& t) {
     t.t += gridDim.x;
     return place(t);
   }
-  template <class A, class B>
-  __device__ __forceinline__ void begin(const Tile& t, A& a, B& b) const {
+  template <class A>
+  __device__ __forceinline__ void begin_a(const Tile& t, A& a) const {
+    a.lanes(t.rows, p.a_ld, wave, my_lane());
+    a.start_rows(p.a + t.row0 * p.a_ld, nullptr, t.rows, p.a_ld, p.K * kEsize);
+  }
+  template <class B>
+  __device__ __forceinline__ void begin_b(const Tile& t, B& b) const {
     const int64_t ldb = (int64_t)p.K * kEsize;
     const int64_t boff = t.e * p.expert_stride * kEsize + t.col0 * ldb;
     const int cols = std::min(p.N - t.col0, kCols);
-    a.lanes(t.rows, p.a_ld, wave, lane);
-    b.lanes(cols, ldb, wave, lane);
-    a.start_rows(p.a + t.row0 * p.a_ld, nullptr, t.rows, p.a_ld, p.K * kEsize);
+    b.lanes(cols, ldb, wave, my_lane());
     b.start_rows(p.w + boff, p.w2 + boff, cols, ldb, p.K * kEsize);
+  }
+  template <class A, class B>
+  __device__ __forceinline__ void begin(const Tile& t, A& a, B& b) const {
+    begin_a(t, a);
+    begin_b(t, b);
+  }
+  // A tile of nothing: every load is out of range.
+  __device__ __forceinline__ void none(Tile& t) const {
+    t.e = t.row0 = t.rows = 0;
+    t.col0 = p.N;
   }
   template <class A, class B>
   __device__ __forceinline__ void turn(const Tile&, int, A&, B&) const {}
@@ -137,47 +157,31 @@ struct ForwardJob {
     else
       wait_tiles<std::min(63, N + kEach * (GATED ? 3 : 2))>();
   }
-  // Before the last step of a tile: what its end reads besides the sums. Loaded later, it would come behind the next
-  // tile's first steps, and the end could not begin until they are there.
+  // Before the last step of a tile: the scales of the wave's rows and columns and its columns' bias, for its end. Each lane
+  // has one value of each and gets at the others' by shuffles: the steps leave few registers, and one that is spilled
+  // comes back behind the loads of the next tile. (Gated: the gate's scales in the lower lanes, the up ones in the others.)
   __device__ __forceinline__ void gather(const Tile& t) {
-    if constexpr (INT8) {
-      const int cols = std::min(p.N - t.col0, kCols);
+    constexpr int kWide = kPairs * 32;
+    static_assert(kWide <= (GATED ? 32 : kWave) && S::MF % 4 == 0, "a value a lane");
+    const int cols = std::min(p.N - t.col0, kCols), lane = my_lane();
 #pragma unroll
-      for (int f = 0; f < S::MF; ++f) rs[f] = p.a_scale[t.row0 + std::min(at.row + f * 16, t.rows - 1)];
-#pragma unroll
-      for (int g = 0; g < kPairs; ++g) {
-        const int64_t cc = (int64_t)t.e * p.N + t.col0 + std::min(at.col + g * 32, cols - 8);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          cs[g][i] = p.w_scale[cc + i];
-          if constexpr (GATED) cs2[g][i] = p.w2_scale[cc + i];
-        }
-        if constexpr (!GATED) {
-          cb[g] = p.bias ? *(const u32x4*)(p.bias + cc * 2) : u32x4{0, 0, 0, 0};
-        }
-      }
-    }
+    for (int i = 0; i < S::MF / 4; ++i)
+      row_scale[i] = p.a_scale[t.row0 + std::min((wave / S::WN) * S::MF * 16 + i * kWave + lane, t.rows - 1)];
+    const int c = std::min((wave % S::WN) * kWide + lane % kWide, cols - 1);
+    const int64_t cc = (int64_t)t.e * p.N + t.col0 + c;
+    col_scale = (GATED && lane >= 32 ? p.w2_scale : p.w_scale)[cc];
+    if constexpr (!GATED) col_bias = p.bias ? bf16lo_to_f32(((const uint16_t*)p.bias)[cc]) : 0.0f;
   }
   __device__ __forceinline__ void gathered() {
-    if constexpr (INT8) {
 #pragma unroll
-      for (int f = 0; f < S::MF; ++f) arrived(rs[f]);
-#pragma unroll
-      for (int g = 0; g < kPairs; ++g) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          arrived(cs[g][i]);
-          if constexpr (GATED) arrived(cs2[g][i]);
-        }
-        if constexpr (!GATED) arrived(cb[g]);
-      }
-    }
+    for (int i = 0; i < S::MF / 4; ++i) arrived(row_scale[i]);
+    arrived(col_scale);
+    if constexpr (!GATED) arrived(col_bias);
   }
   __device__ __forceinline__ void finish(const Tile& t, AccOf<T> (&acc)[S::MF][S::NF]) const {
     const int cols = std::min(p.N - t.col0, kCols);
-    int row0 = at.row, col = at.col;
-    // Not to be worked out once for all tiles: the offsets of all stores are more than the registers that the steps leave.
-    if constexpr (INT8) asm volatile("" : "+v"(row0), "+v"(col));
+    const int lane = my_lane();
+    const LanePlace<S, GATED> at(wave, lane);
     const TileOut out(p.out, t.row0, p.out_ld, t.col0, t.rows, cols);
     const int64_t pre_ld = (int64_t)p.N * (GATED ? 4 : 2);
     const TileOut pre(p.pre, t.row0, pre_ld, t.col0, t.rows, cols);
@@ -185,7 +189,7 @@ struct ForwardJob {
     constexpr int kTake = kPairs % 2 ? 1 : 2;  // groups of 32 columns stored together
 #pragma unroll
     for (int g0 = 0; g0 < kPairs; g0 += kTake) {
-      const int c0 = col + g0 * 32;
+      const int c0 = at.col + g0 * 32;
       float s1[kTake][8], s2[kTake][8], bias[kTake][8];
 #pragma unroll
       for (int k = 0; k < kTake; ++k) {
@@ -201,27 +205,33 @@ struct ForwardJob {
         if constexpr (INT8) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            s1[k][i] = cs[g0 + k][i];
-            if constexpr (GATED) s2[k][i] = cs2[g0 + k][i];
+            const int from = (g0 + k) * 32 + (lane >> 4) * 8 + i;
+            s1[k][i] = __shfl(col_scale, from, kWave);
+            if constexpr (GATED) s2[k][i] = __shfl(col_scale, 32 + from, kWave);
+            if constexpr (!GATED) bias[k][i] = __shfl(col_bias, from, kWave);
           }
-          if constexpr (!GATED) unpack8(cb[g0 + k], bias[k]);
         } else if constexpr (!GATED) {
           if (p.bias) unpack8(*(const u32x4*)(p.bias + cc * 2), bias[k]);
         }
       }
 #pragma unroll
       for (int f = 0; f < S::MF; ++f) {
-        const int r = row0 + f * 16;
+        const int r = at.row + f * 16;
         float v[kTake][8], u[kTake][8];
+        float rs;
+        if constexpr (INT8) {
+          __builtin_amdgcn_sched_barrier(0);  // one fragment's values at a time
+          rs = __shfl(row_scale[f / 4], f % 4 * 16 + (lane & 15), kWave);
+        }
 #pragma unroll
         for (int j = 0; j < kTake * 8; ++j) {
           const int k = j / 8, i = j % 8, at_n = (g0 + k) * 2 + i / 4;
           v[k][i] = (float)acc[f][at_n][i % 4];
-          if constexpr (INT8) v[k][i] *= rs[f];
+          if constexpr (INT8) v[k][i] *= rs;
           if constexpr (FP8 || INT8) v[k][i] *= s1[k][i];
           if constexpr (GATED) {
             u[k][i] = (float)acc[f][S::NF / 2 + at_n][i % 4];
-            if constexpr (INT8) u[k][i] *= rs[f];
+            if constexpr (INT8) u[k][i] *= rs;
             if constexpr (FP8 || INT8) u[k][i] *= s2[k][i];
           } else if (p.bias) {
             v[k][i] += bias[k][i];
@@ -290,7 +300,8 @@ struct RowGradJob {
     part_steps = (p.N * 2 + kStepBytes - 1) / kStepBytes;
   }
   __device__ __forceinline__ bool place(Tile& t) const {
-    if (!t.at.template find<S::BM>(p.expert_off, p.E, p.cap, t.t / nt, lane)) return false;
+    Offsets fresh;
+    if (!t.at.template find<S::BM>(p.expert_off, p.E, p.cap, t.t / nt, lane, fresh)) return false;
     int m, n;
     t.e = t.at.e;
     band_tile(t.t - t.at.before * nt, t.at.count, nt, 8, m, n);
@@ -322,8 +333,6 @@ struct RowGradJob {
     b.start_cols(w + (t.e * p.expert_stride + t.col0) * 2, p.N, std::min(p.K - t.col0, S::BN), ldb);
   }
   // The second part's first step. (An only part's padded step may have that number too.)
-  __device__ __forceinline__ void gather(const Tile&) const {}
-  __device__ __forceinline__ void gathered() const {}
   template <class A, class B>
   __device__ __forceinline__ void turn(const Tile& t, int step, A& a, B& b) const {
     if (p.parts == 2 && step == part_steps) start(t, 1, p.w2, a, b);
@@ -390,8 +399,6 @@ struct WeightGradJob {
     t.t += gridDim.x;
     return place(t);
   }
-  __device__ __forceinline__ void gather(const Tile&) const {}
-  __device__ __forceinline__ void gathered() const {}
   template <class A, class B>
   __device__ __forceinline__ void turn(const Tile&, int, A&, B&) const {}
   template <class A, class B>

@@ -280,7 +280,6 @@ __device__ __forceinline__ void arrived(T& v) {
 //   begin(t, a, b)                sets the operands up for step 0 of tile t;
 //   turn(t, step, a, b)           the same for a later step at which a source changes;
 //   load_scales(t, step, lds)     fp8: one load per wave that brings the step's row scales to lds;
-//   gather(t), gathered()         before a tile's last step, and before the next tile's first loads: reads for its end;
 //   finish(t, acc)                the end of a tile: a known number of buffer stores per wave, whatever is masked;
 //   wait<N>(stored)               wait_tiles<N>, or with the number of stores added.
 //
@@ -314,6 +313,7 @@ __device__ __forceinline__ void run_tiles(Job& job, uint32_t lds, int wave, int 
   constexpr int kGroups = kHalves * S::MF, kRing = 4, kAhead = 3, kTail = kGroups - kAhead;
   constexpr int kLoads = A::kLoads + B::kLoads + (FP8 ? 1 : 0);
   constexpr int kLater = S::STAGES - 2;  // steps loading behind the one that a step waits for
+  constexpr bool kStream = T == Elem::kInt8;  // loads run on into the next tile
   static_assert(kGroups % kRing == 0, "ring of row fragments");
   static_assert(T == Elem::kBf16 || (!ACOLS && !BCOLS), "8-bit operands are rows");
   static_assert(kHalves == 2 || S::STAGES == 3, "steps() gives an fp8 tile one step more than the written-out three");
@@ -401,11 +401,14 @@ __device__ __forceinline__ void run_tiles(Job& job, uint32_t lds, int wave, int 
         // groups' products wait for the reads that follow the barrier.
         static_for<0, kAhead>([&](auto i) EPL_INLINE { arrived(fa[(g + i) % kRing]); });
         if constexpr (kHalves == 2) static_for<0, S::NF>([&](auto n) EPL_INLINE { arrived(fb[1][n]); });
-        if constexpr (left > 0) {
+        if constexpr (kStream) {
+          job.template wait<S::RING ? A::kLoads : kLoads * kLater>(stored > 0);
+          if constexpr (left == 0) job.gathered();
+        } else if constexpr (left > 0) {
           constexpr int behind = S::RING ? (left > 1 ? A::kLoads : 0) : kLoads * std::min(kLater, left - 1);
           job.template wait<behind>(stored > 0);
-          fr.point(cur, b_of(cur));
         }
+        if constexpr (left > 0) fr.point(cur, b_of(cur));
       }
       static_for<0, S::NF>([&](auto n) EPL_INLINE {
         __builtin_amdgcn_sched_barrier(0);
@@ -430,17 +433,17 @@ __device__ __forceinline__ void run_tiles(Job& job, uint32_t lds, int wave, int 
           constexpr int kSpread = std::min(S::MF, kTail), per = (S::NF + kSpread - 1) / kSpread;
           if constexpr (kHalves == 2 && g < kSpread && n == S::NF / 2)
             static_for<g * per, std::min((g + 1) * per, S::NF)>([&](auto i) EPL_INLINE { read_b(One{}, i, One{}); });
-        } else if constexpr (left > 0) {
+        } else if constexpr (left > 0 || kStream) {
           constexpr int slot = (g - kTail) * S::NF + n, kSlots = kAhead * S::NF;
           constexpr int to = kHalves == 2 ? 0 : 1 - par;
-          if constexpr (slot < S::NF) read_b(std::integral_constant<int, to>{}, n, Zero{});
+          if constexpr (left > 0 && slot < S::NF) read_b(std::integral_constant<int, to>{}, n, Zero{});
           // A ring entry is free once its own group is done.
-          if constexpr (g == kTail + 1 && n < 2) read_a(n);
-          if constexpr (g == kTail + 2 && n == 0) read_a(std::integral_constant<int, 2>{});
+          if constexpr (left > 0 && g == kTail + 1 && n < 2) read_a(n);
+          if constexpr (left > 0 && g == kTail + 2 && n == 0) read_a(std::integral_constant<int, 2>{});
           if constexpr (FP8 && slot == S::NF)
             static_for<0, S::MF>([&](auto f) EPL_INLINE { read_scale(std::integral_constant<int, to>{}, f, cur); });
           // The freed tiles: in a ring they take B of the step after the next and then A of the one behind it.
-          constexpr int issue = left == S::kFinal ? kLoads : S::RING && left == 2 ? B::kLoads : 0;
+          constexpr int issue = left == S::kFinal || kStream ? kLoads : S::RING && left == 2 ? B::kLoads : 0;
           if constexpr (issue > 0) {
             constexpr int per = (issue + kSlots - 1) / kSlots, begin = kSlots - (issue + per - 1) / per;
             if constexpr (slot >= begin)
@@ -461,13 +464,17 @@ __device__ __forceinline__ void run_tiles(Job& job, uint32_t lds, int wave, int 
 
   if (!job.first(tile)) return;
   begin_tile();
+  constexpr int kFirst = S::RING ? 2 * A::kLoads + B::kLoads : kLoads * (S::STAGES - 1);  // loads behind the first step's
+  if constexpr (kStream) job.template wait<kFirst>(false);
   while (true) {
 #pragma unroll
     for (int m = 0; m < S::MF; ++m)
 #pragma unroll
       for (int n = 0; n < S::NF; ++n) acc[m][n] = Acc{0, 0, 0, 0};
-    job.template wait<S::RING ? 2 * A::kLoads + B::kLoads : kLoads*(S::STAGES - 1)>(stored > 0);
-    cur = lds;
+    if constexpr (!kStream) {
+      job.template wait<kFirst>(stored > 0);
+      cur = lds;
+    }
     fr.point(cur, b_of(cur));
     static_for<0, S::NF>([&](auto n) EPL_INLINE { read_b(Zero{}, n, Zero{}); });
     if constexpr (FP8) static_for<0, S::MF>([&](auto f) EPL_INLINE { read_scale(Zero{}, f, cur); });
@@ -478,23 +485,48 @@ __device__ __forceinline__ void run_tiles(Job& job, uint32_t lds, int wave, int 
       step(std::integral_constant<int, kHalves == 2 ? 0 : kOdd>{}, Middle{});
       if constexpr (kHalves == 1) step(std::integral_constant<int, 1 - kOdd>{}, Middle{});
     }
+    typename Job::Tile other = tile;  // the next tile; where loads run on into it, known before this one's last steps
+    bool more = false;
     static_for<0, S::kFinal>([&](auto i) EPL_INLINE {
-      if constexpr (i == S::kFinal - 1) job.gather(tile);
+      if constexpr (kStream) {
+        // A step loads B of the second and, in a ring, A of the third step after it, else both of the third.
+        if constexpr (i == 0) {
+          more = job.next(other);
+          if (!more) job.none(other);
+          job.begin_a(other, a);
+        }
+        if constexpr (i == (S::RING ? 1 : 0)) job.begin_b(other, b);
+        if constexpr (i == S::kFinal - 1) job.gather(tile);
+      }
       step(std::integral_constant<int, kHalves == 2 ? 0 : (kOdd + i) % 2>{},
            std::integral_constant<int, S::kFinal - 1 - i>{});
     });
-    const typename Job::Tile done = tile;
-    const bool more = job.next(tile);
-    wait_tiles<0>();  // every wave has read the last stages
-    job.gathered();
-    if (more) begin_tile();
-    job.finish(done, acc);
-    if (!more) return;
+    if constexpr (kStream) {
+      job.finish(tile, acc);
+      if (!more) {
+        wait_tiles<0>();  // no load to LDS outlives the workgroup
+        return;
+      }
+      tile = other;
+    } else {
+      other = tile;
+      more = job.next(tile);
+      wait_tiles<0>();  // every wave has read the last stages
+      if (more) begin_tile();
+      job.finish(other, acc);
+      if (!more) return;
+    }
     stored = S::STAGES - 1;
   }
 }
 
 // ---------------------------------------------------------------- tiles over the experts' rows
+// The rows [b0, b1) of an expert a lane, of a group of 64, its row tiles and those up to it.
+struct Offsets {
+  int group = -1, b0, b1;
+  uint32_t n, sum;
+};
+
 // Where a row tile lies: expert e, its rows [beg, end), the row tiles before it and its own.
 struct RowTile {
   int e = 0, beg = 0, end = 0;
@@ -505,24 +537,29 @@ struct RowTile {
   // Finds row tile m (BM rows a tile), not before the one found last; false past the last one. A wave works it out from
   // the offsets, 64 experts at a time, from the group where it last was: a table in LDS would cost the room of the
   // ring. Offsets are clipped to the buffer, so that whatever they hold, no access leaves it.
+  // o: a group's offsets, kept by the caller from one call to the next or fresh.
   template <int BM>
-  __device__ __forceinline__ bool find(const int32_t* expert_off, int E, int cap, int64_t m, int lane) {
+  __device__ __forceinline__ bool find(const int32_t* expert_off, int E, int cap, int64_t m, int lane, Offsets& o) {
     for (int e0 = e & ~(kWave - 1); e0 < E; e0 += kWave) {
-      const int mine = std::min(e0 + lane, E - 1);
-      const int b0 = std::min(std::max(expert_off[mine], 0), cap), b1 = std::min(std::max(expert_off[mine + 1], b0), cap);
-      const uint32_t n = e0 + lane < E ? (uint32_t)(b1 - b0 + BM - 1) / BM : 0u;
-      const uint32_t sum = (uint32_t)wave_inclusive_sum((int)n);
-      const uint64_t past = __ballot(chunk_before + sum > m);
+      if (e0 != o.group) {
+        const int mine = std::min(e0 + lane, E - 1);
+        o.b0 = std::min(std::max(expert_off[mine], 0), cap);
+        o.b1 = std::min(std::max(expert_off[mine + 1], o.b0), cap);
+        o.n = e0 + lane < E ? (uint32_t)(o.b1 - o.b0 + BM - 1) / BM : 0u;
+        o.sum = (uint32_t)wave_inclusive_sum((int)o.n);
+        o.group = e0;
+      }
+      const uint64_t past = __ballot(chunk_before + o.sum > m);
       if (past) {
         const int l = __builtin_ctzll(past);
         e = e0 + l;
-        beg = __builtin_amdgcn_readlane(b0, l);
-        end = __builtin_amdgcn_readlane(b1, l);
-        count = __builtin_amdgcn_readlane((int)n, l);
-        before = chunk_before + (uint32_t)__builtin_amdgcn_readlane((int)sum, l) - (uint32_t)count;
+        beg = __builtin_amdgcn_readlane(o.b0, l);
+        end = __builtin_amdgcn_readlane(o.b1, l);
+        count = __builtin_amdgcn_readlane((int)o.n, l);
+        before = chunk_before + (uint32_t)__builtin_amdgcn_readlane((int)o.sum, l) - (uint32_t)count;
         return true;
       }
-      chunk_before += (uint32_t)__builtin_amdgcn_readlane((int)sum, kWave - 1);
+      chunk_before += (uint32_t)__builtin_amdgcn_readlane((int)o.sum, kWave - 1);
     }
     return false;
   }
