@@ -1,21 +1,22 @@
 // Dispatch with the gate weights applied, and its gradient: for token g with valid choices j in packed rows r,
 //   recv[r] = w[g][j] x[g];   dx[g] = sum_j w[g][j] drecv[r],   dw[g][j] = <x[g], drecv[r]>.
 // HBM traffic bounds both.
-#include "epl_internal.h"
 #include "experts.h"
+#include "rows_body.h"
 
 namespace epl {
 
-constexpr int kWeightedThreads = 128;
-constexpr int kWeightedWaves = kWeightedThreads / kWave;
-
-__global__ void __launch_bounds__(kWeightedThreads)
+// As the plain bf16 dispatch: one (token, 1 KiB column chunk) a wave, two waves a workgroup, held at 4 waves per SIMD (6 with
+// one or two choices). 8192 tokens of 7168 columns to 8 rows each: 191 us, as without the weights; not held 198, held at 2 / 3
+// / 5 / 6 228 / 193 / 192 / 195; with default stores 214, with streaming ones 194.
+template <bool FEW>
+__global__ void __launch_bounds__(kPlainThreads) __attribute__((amdgpu_waves_per_eu(FEW ? 6 : 4, FEW ? 6 : 4)))
     dispatch_weighted_kernel(const u32x4* __restrict__ x, const float* __restrict__ w, const int32_t* __restrict__ pair_row,
                              u32x4* __restrict__ recv, int64_t T, int k, int nv, int pv, int chunks, int64_t cap) {
   const int lane = threadIdx.x % kWave;
   const int64_t units = T * chunks;
-  for (int64_t u = (int64_t)blockIdx.x * kWeightedWaves + threadIdx.x / kWave; u < units;
-       u += (int64_t)gridDim.x * kWeightedWaves) {
+  for (int64_t u = (int64_t)blockIdx.x * kPlainWaves + threadIdx.x / kWave; u < units;
+       u += (int64_t)gridDim.x * kPlainWaves) {
     const int64_t g = u / chunks;
     const int v = (int)(u - g * chunks) * kWave + lane;
     const u32x4 buf = x[g * nv + std::min(v, nv - 1)];
@@ -28,32 +29,34 @@ __global__ void __launch_bounds__(kWeightedThreads)
       u32x4 o;
 #pragma unroll
       for (int i = 0; i < 4; ++i) o[i] = f32x2_to_bf16x2(wj * bf16lo_to_f32(buf[i]), wj * bf16hi_to_f32(buf[i]));
-      if (v < nv) recv[(int64_t)row * pv + v] = o;
+      if (v < nv) store_row_policy<kCachePolicySc1>(o, recv + (int64_t)row * pv, nv, v);
     }
   }
 }
 
-constexpr int kDispatchGradThreads = 256;
-constexpr int kDispatchGradWaves = kDispatchGradThreads / kWave;
-
-// One workgroup a token. A thread's products are summed in fp32 over its own columns, then over the wave and the waves in
-// a fixed order. dx may be x: a thread reads its columns before it writes them.
+// One workgroup a token, of as many threads as its vectors need in the fewest equal passes (448 for 7168 columns). A thread's
+// products are summed in fp32 over its own columns, then over the wave and the waves in a fixed order. dx may be x: a thread
+// reads its columns before it writes them. 8192 tokens of 7168 columns with 8 rows each: 205 us (5.7 TB/s) with 448 threads
+// held at 4 waves per SIMD, 211 not held, 258 at 3; with 64 / 128 / 192 / 256 / 512 threads 230 / 225 / 219 / 215 / 211;
+// stores with the default policy 226 (256 threads).
 // KMAX: choices held in registers (k <= KMAX).
+constexpr int kDispatchGradThreads = 512;
+constexpr int kDispatchGradWaves = kDispatchGradThreads / kWave;
 template <int KMAX>
-__global__ void __launch_bounds__(kDispatchGradThreads)
+__global__ void __launch_bounds__(kDispatchGradThreads) __attribute__((amdgpu_waves_per_eu(KMAX <= 8 ? 4 : 2, 4)))
     dispatch_grad_kernel(const u32x4* __restrict__ d, const u32x4* x, const float* __restrict__ w,
                          const int32_t* __restrict__ pair_row, u32x4* dx, float* __restrict__ dw, int64_t T, int k, int nv,
                          int pv, int64_t cap) {
   __shared__ float part[kDispatchGradWaves][EPL_MAX_TOPK];
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, threads = blockDim.x;
+  constexpr int kGroup = KMAX < 8 ? KMAX : 8;  // rows loaded before any is consumed
   for (int64_t g = blockIdx.x; g < T; g += gridDim.x) {
     float acc[KMAX];
 #pragma unroll
     for (int j = 0; j < KMAX; ++j) acc[j] = 0.0f;
-    for (int c = threadIdx.x; c < nv; c += kDispatchGradThreads) {
-      const u32x4 xv = x[g * nv + c];
+    for (int c = threadIdx.x; c < nv; c += threads) {
+      const u32x4 xv = __builtin_nontemporal_load(x + g * nv + c);
       float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-      constexpr int kGroup = KMAX < 8 ? KMAX : 8;  // rows loaded before any is consumed
 #pragma unroll
       for (int j0 = 0; j0 < KMAX; j0 += kGroup) {
         u32x4 buf[kGroup];
@@ -82,21 +85,21 @@ __global__ void __launch_bounds__(kDispatchGradThreads)
       u32x4 o;
 #pragma unroll
       for (int i = 0; i < 4; ++i) o[i] = f32x2_to_bf16x2(sum[2 * i], sum[2 * i + 1]);
-      dx[g * nv + c] = o;
+      store_row_policy<kCachePolicySc1Nt>(o, dx + g * nv, nv, c);
     }
     __syncthreads();  // the previous token's sums have been read
 #pragma unroll
     for (int j = 0; j < KMAX; ++j) {
+      if (j >= k) break;
       float v = acc[j];
 #pragma unroll
       for (int off = kWave / 2; off > 0; off >>= 1) v += __shfl_xor(v, off, kWave);
-      if (lane == 0 && j < k) part[wave][j] = v;
+      if (lane == 0) part[wave][j] = v;
     }
     __syncthreads();
     if (threadIdx.x < k) {
       float v = 0.0f;
-#pragma unroll
-      for (int i = 0; i < kDispatchGradWaves; ++i) v += part[i][threadIdx.x];
+      for (int i = 0; i < threads / kWave; ++i) v += part[i][threadIdx.x];
       dw[g * k + threadIdx.x] = v;
     }
   }
@@ -106,19 +109,27 @@ hipError_t launch_dispatch_weighted(const void* x, const float* w, const int32_t
                                     int H, int pitch, int64_t cap, hipStream_t stream) {
   if (T == 0) return hipSuccess;
   const int nv = H / 8, chunks = (nv + kWave - 1) / kWave;
-  hipLaunchKernelGGL(dispatch_weighted_kernel, dim3(unit_grid(T * chunks, kWeightedWaves, kWeightedThreads)),
-                     dim3(kWeightedThreads), 0, stream, static_cast<const u32x4*>(x), w, pair_row, static_cast<u32x4*>(recv),
-                     T, k, nv, pitch / 8, chunks, cap);
+  const auto launch = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3(unit_grid(T * chunks, kPlainWaves, kPlainThreads)), dim3(kPlainThreads), 0, stream,
+                       static_cast<const u32x4*>(x), w, pair_row, static_cast<u32x4*>(recv), T, k, nv, pitch / 8, chunks,
+                       cap);
+  };
+  if (k <= kFewChoices)
+    launch(dispatch_weighted_kernel<true>);
+  else
+    launch(dispatch_weighted_kernel<false>);
   return hipGetLastError();
 }
 
 hipError_t launch_dispatch_grad(const void* d, const void* x, const float* w, const int32_t* pair_row, void* dx, float* dw,
                                 int64_t T, int k, int H, int pitch, int64_t cap, hipStream_t stream) {
   if (T == 0) return hipSuccess;
+  const int nv = H / 8, passes = (nv + kDispatchGradThreads - 1) / kDispatchGradThreads;
+  const int threads = ((nv + passes - 1) / passes + kWave - 1) / kWave * kWave;
   const dim3 grid((unsigned)std::min<int64_t>(T, 1 << 20));
   const auto launch = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, dim3(kDispatchGradThreads), 0, stream, static_cast<const u32x4*>(d),
-                       static_cast<const u32x4*>(x), w, pair_row, static_cast<u32x4*>(dx), dw, T, k, H / 8, pitch / 8, cap);
+    hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, stream, static_cast<const u32x4*>(d),
+                       static_cast<const u32x4*>(x), w, pair_row, static_cast<u32x4*>(dx), dw, T, k, nv, pitch / 8, cap);
   };
   if (k <= 8)
     launch(dispatch_grad_kernel<8>);

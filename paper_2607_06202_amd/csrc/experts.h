@@ -61,6 +61,16 @@ inline bool short_rows(int64_t cap, int E) { return cap / E < 256; }
 // 3784-3786 / 3578-3585; 2048 to 7168: 589 / 598-610 at 512 rows, 1053-1071 / 1039-1047 at 1024, 2004-2008 / 1921-1938
 // at 2048.
 inline bool many_rows(int64_t cap, int E) { return cap / E >= 1024; }
+// Int8. few_rows against 64 x 256 tiles: 2048 to 2 x 768 of 128 experts, 8 rows 9.3 / 16.8, 16 rows 16.0 / 18.6; 1408 to 5120
+// of 160 experts, 8 rows 18.4 / 16.8, 16 rows 27.4 / 34.5 (kernel times).
+// int8_few_each: 64 x 256 tiles against 128 x 256, us. 1408 to 5120, 160 experts: 6 rows each 208 / 231, 26 rows 216 / 237,
+// 51 rows 221 / 243, 64 rows 262 / 249; 7168 to 2 x 2048, 256 experts: 16 rows 1224 / 1252, 48 rows 1285 / 1289, 64 rows
+// 1420 / 1298. (32 x 256: 206 at 6 rows, 1224 at 16, and slower from 32 on.)
+inline bool int8_few_each(int64_t cap, int E) { return cap / E < 56; }
+// int8_many_each: 256 x 256 tiles against 128 x 256, us. 7168 to 2 x 2048, 32 experts: 256 rows each 336 / 348, 512 rows 535 /
+// 558, 1024 rows 953 / 1032, 2048 rows 1737 / 1943; 2048 to 7168 with a residual, 64 experts: 256 rows 372 / 379, 512 rows 642
+// / 683, 1024 rows 1174 / 1284.
+inline bool int8_many_each(int64_t cap, int E) { return cap / E >= 256; }
 hipError_t launch_forward_few(const ForwardArgs& p, Elem type, bool gated, hipStream_t stream);
 hipError_t launch_forward(const ForwardArgs& p, Elem type, bool gated, hipStream_t stream);
 hipError_t launch_row_grad(const RowGradArgs& p, hipStream_t stream);
@@ -98,8 +108,8 @@ hipError_t launch_dispatch_grad(const void* d, const void* x, const float* w, co
 // w: [T][k] or null. recv rows pitch bytes apart.
 hipError_t launch_dispatch_int8(const void* x, const float* w, const int32_t* pair_row, void* recv, float* scale, int64_t T,
                                 int k, int H, int pitch, int64_t cap, hipStream_t stream);
-// The first n[0] of `rows` rows, or with n null all of them. Strides in 16-byte pieces.
-hipError_t launch_quantize_rows(const void* a, void* q, float* scale, const int32_t* n, int64_t rows, int K, int64_t a_ld,
+// The first count[0] of `rows` rows, or with count null all of them. Strides in 16-byte pieces.
+hipError_t launch_quantize_rows(const void* a, void* q, float* scale, const int32_t* count, int64_t rows, int K, int64_t a_ld,
                                 int64_t q_ld, hipStream_t stream);
 
 }  // namespace epl

@@ -71,6 +71,7 @@ struct ForwardJob {
   static constexpr int kCols = GATED ? S::BN / 2 : S::BN;  // output columns of a tile
   static constexpr int kPairs = kCols / S::WN / 32;        // pairs of column fragments of a wave
   static constexpr int kEsize = elem_bytes(T);
+  static constexpr int kRowRegs = (S::MF * 16 + kWave - 1) / kWave;  // a wave's rows, one a lane
   struct Tile {
     int64_t t;
     RowTile at;
@@ -86,7 +87,7 @@ struct ForwardJob {
     return l;
   }
   // int8: what the tile's end takes besides the sums, one value a lane (see gather), and the experts' offsets (see find).
-  float row_scale[S::MF / 4], col_scale, col_bias;
+  float row_scale[kRowRegs], col_scale, col_bias;
   Offsets offsets;
   __device__ __forceinline__ ForwardJob(const ForwardArgs& p_, int wave_, int lane_)
       : p(p_), wave(wave_), lane(lane_) {
@@ -162,10 +163,10 @@ struct ForwardJob {
   // comes back behind the loads of the next tile. (Gated: the gate's scales in the lower lanes, the up ones in the others.)
   __device__ __forceinline__ void gather(const Tile& t) {
     constexpr int kWide = kPairs * 32;
-    static_assert(kWide <= (GATED ? 32 : kWave) && S::MF % 4 == 0, "a value a lane");
+    static_assert(kWide <= (GATED ? 32 : kWave), "a value a lane");
     const int cols = std::min(p.N - t.col0, kCols), lane = my_lane();
 #pragma unroll
-    for (int i = 0; i < S::MF / 4; ++i)
+    for (int i = 0; i < kRowRegs; ++i)
       row_scale[i] = p.a_scale[t.row0 + std::min((wave / S::WN) * S::MF * 16 + i * kWave + lane, t.rows - 1)];
     const int c = std::min((wave % S::WN) * kWide + lane % kWide, cols - 1);
     const int64_t cc = (int64_t)t.e * p.N + t.col0 + c;
@@ -174,7 +175,7 @@ struct ForwardJob {
   }
   __device__ __forceinline__ void gathered() {
 #pragma unroll
-    for (int i = 0; i < S::MF / 4; ++i) arrived(row_scale[i]);
+    for (int i = 0; i < kRowRegs; ++i) arrived(row_scale[i]);
     arrived(col_scale);
     if constexpr (!GATED) arrived(col_bias);
   }
@@ -214,6 +215,22 @@ struct ForwardJob {
           if (p.bias) unpack8(*(const u32x4*)(p.bias + cc * 2), bias[k]);
         }
       }
+      // int8: the residual's rows, two fragments ahead (2048 to 7168, 64 experts of 1024 rows, us: each read where it is
+      // added 1239, two ahead 1189, four 1198; eight spill).
+      constexpr int kEarly = 2;
+      u32x4 res[kEarly][kTake];
+      const auto load_res = [&](int f) EPL_INLINE {
+        const char* row = p.residual + (t.row0 + std::min(at.row + f * 16, t.rows - 1)) * p.res_ld;
+#pragma unroll
+        for (int k = 0; k < kTake; ++k)
+          res[f % kEarly][k] = *(const u32x4*)(row + (t.col0 + std::min(c0 + k * 32, cols - 8)) * 2ll);
+      };
+      if constexpr (INT8 && !GATED) {
+        if (p.residual) {
+#pragma unroll
+          for (int f = 0; f < std::min(kEarly, S::MF); ++f) load_res(f);
+        }
+      }
 #pragma unroll
       for (int f = 0; f < S::MF; ++f) {
         const int r = at.row + f * 16;
@@ -249,7 +266,16 @@ struct ForwardJob {
           }
         });
         if constexpr (!GATED) {
-          if (p.residual) {
+          if (INT8 && p.residual) {
+#pragma unroll
+            for (int k = 0; k < kTake; ++k) {
+              float d[8];
+              unpack8(res[f % kEarly][k], d);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) v[k][i] += d[i];
+            }
+            if (f + kEarly < S::MF) load_res(f + kEarly);
+          } else if (p.residual) {
             const char* res = p.residual + (t.row0 + std::min(r, t.rows - 1)) * p.res_ld;
 #pragma unroll
             for (int k = 0; k < kTake; ++k) {
@@ -532,6 +558,7 @@ __global__ void __launch_bounds__(256) pre_bias_grad_kernel(const char* dy, int6
 using Big = Shape<256, 256, 2, 4, 2, true>;
 using Mid = Shape<128, 256, 2, 4, 3>;
 using Short = Shape<64, 256, 1, 4, 3>;
+using Low = Shape<64, 256, 2, 4, 4>;
 
 static unsigned persistent_grid(int64_t tiles, int per_cu) {
   return (unsigned)std::min<int64_t>(tiles, (int64_t)kCus * per_cu);
@@ -559,8 +586,9 @@ hipError_t launch_forward(const ForwardArgs& p, Elem type, bool gated, hipStream
     return short_rows(p.cap, p.E) ? forward_as<Short, Elem::kE4m3>(p, gated, stream)
                                   : forward_as<Mid, Elem::kE4m3>(p, gated, stream);
   if (type == Elem::kInt8)
-    return many_rows(p.cap, p.E) ? forward_as<Big, Elem::kInt8>(p, gated, stream)
-                                 : forward_as<Mid, Elem::kInt8>(p, gated, stream);
+    return int8_few_each(p.cap, p.E)    ? forward_as<Low, Elem::kInt8>(p, gated, stream)
+           : int8_many_each(p.cap, p.E) ? forward_as<Big, Elem::kInt8>(p, gated, stream)
+                                        : forward_as<Mid, Elem::kInt8>(p, gated, stream);
   return many_rows(p.cap, p.E) ? forward_as<Big, Elem::kBf16>(p, gated, stream)
                                : forward_as<Mid, Elem::kBf16>(p, gated, stream);
 }

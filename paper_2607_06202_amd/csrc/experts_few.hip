@@ -3,7 +3,9 @@
 // Reading the weights once is all there is to do, and a tile's start and end would cost as much as its middle. So a
 // workgroup takes 16 * NF weight rows of one expert, its four waves each take every fourth 128-byte step of the
 // reduction, and the four partial sums are joined through LDS in a fixed order. A wave's fragments come straight from
-// memory, kDepth steps ahead: 2 * (NF + 1) KiB a step in flight.
+// memory, few_depth steps ahead: 2 * (NF + 1) KiB a step in flight. Int8 rows are half as long, so a wave has few steps, and
+// those past the last one cost more than the depth gains: 2048 to 2 x 768, 8 rows, 1 / 2 / 3 / 4 steps ahead 9.4 / 9.3 / 10.2 /
+// 10.4 us; 7168 to 2 x 2048 50.7 / 48.6 / 51.2 / 53.5; 768 to 2048 - / 6.6 / - / 8.2.
 //
 // For at most 16 packed rows in all (few_rows): an expert's rows are one fragment.
 //
@@ -14,7 +16,8 @@
 
 namespace epl {
 
-constexpr int kFewWaves = 4, kDepth = 4;
+constexpr int kFewWaves = 4;
+constexpr int few_depth(Elem t) { return t == Elem::kInt8 ? 2 : 4; }
 
 // The i-th expert with rows (E if there are not that many). Wave-uniform.
 __device__ __forceinline__ int nth_expert(const int32_t* expert_off, int E, int cap, int i, int lane) {
@@ -40,7 +43,7 @@ __device__ __forceinline__ int nth_expert(const int32_t* expert_off, int E, int 
 template <int NF, Elem T, bool GATED>
 __global__ void __launch_bounds__(kFewWaves* kWave, 2) few_rows_kernel(ForwardArgs p) {
   constexpr bool FP8 = T == Elem::kE4m3, INT8 = T == Elem::kInt8;
-  constexpr int kCols = 16 * NF / (GATED ? 2 : 1), kEsize = elem_bytes(T);
+  constexpr int kCols = 16 * NF / (GATED ? 2 : 1), kEsize = elem_bytes(T), kDepth = few_depth(T);
   constexpr int kUnits = kCols / 32;  // groups of 32 output columns
   using Acc = AccOf<T>;
   __shared__ Acc part[kFewWaves][NF][kWave];

@@ -9,9 +9,17 @@
 // rounds to the nearest even integer and leaves it in the low byte. 127 / A is finite for every bf16 A but those below
 // 2^-121; x and A are taken times 2^100 where A is below 2^-100.
 //
-// A row is read once: it stays in registers between the maximum and the conversion.
-#include "epl_internal.h"
+// HBM traffic bounds both. A row is read once: it stays in registers between the maximum and the conversion, of a wave up to
+// 2048 elements (no workgroup waits) and of a workgroup beyond.
+//   * Rows where they are, 65536 of 2048: a workgroup of 256 for each row 192 us, of a wave for each 71, with streaming loads
+//     and stores 68 (5.9 TB/s).
+//   * Dispatch, 8192 tokens of 7168 to 8 rows each: 118 us (5.0 TB/s), as the E4M3 dispatch of the same tokens (120), and
+//     within 3% whatever the threads a row (64 to 448), the waves held at once and the stores' policy: what the scattered
+//     writes of 7 KiB rows take.
+#include <type_traits>
+
 #include "experts.h"
+#include "rows_body.h"
 
 namespace epl {
 
@@ -19,7 +27,8 @@ constexpr int kInt8Threads = 256;
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
 // A row of n pieces of 16 elements in the registers of GROUP threads, UNITS pieces each; longer rows in passes.
-template <int GROUP, int UNITS>
+// STREAM: the row is not read again.
+template <int GROUP, int UNITS, bool STREAM>
 struct Int8Row {
   u32x4 v[UNITS][2];
   const u32x4* row;
@@ -29,8 +38,8 @@ struct Int8Row {
 #pragma unroll
     for (int i = 0; i < UNITS; ++i) {
       const int u = std::min(first + i * GROUP + t, n - 1);
-      v[i][0] = row[2 * u];
-      v[i][1] = row[2 * u + 1];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) v[i][h] = STREAM ? __builtin_nontemporal_load(row + 2 * u + h) : row[2 * u + h];
     }
   }
   // The larger of m and the magnitudes' bits, by halves.
@@ -88,10 +97,10 @@ __device__ __forceinline__ uint32_t group_max(u16x2 m) {
 }
 
 // One row: put(piece, its 16 values) of every piece and put_scale(s) once.
-template <int GROUP, int UNITS, class Put, class PutScale>
+template <int GROUP, int UNITS, bool STREAM, class Put, class PutScale>
 __device__ __forceinline__ void quantise_row(const u32x4* row, int n, int t, Put&& put, PutScale&& put_scale) {
   constexpr int kPass = GROUP * UNITS;
-  Int8Row<GROUP, UNITS> r;
+  Int8Row<GROUP, UNITS, STREAM> r;
   r.row = row;
   r.n = n;
   r.t = t;
@@ -120,8 +129,8 @@ __global__ void __launch_bounds__(kInt8Threads)
   const int t = threadIdx.x % GROUP;
   if (count) rows = std::min<int64_t>(std::max(*count, 0), rows);
   for (int64_t r = (int64_t)blockIdx.x * kPer + threadIdx.x / GROUP; r < rows; r += (int64_t)gridDim.x * kPer)
-    quantise_row<GROUP, UNITS>(
-        a + r * a_ld, n, t, [&](int u, u32x4 v) EPL_INLINE { q[r * q_ld + u] = v; },
+    quantise_row<GROUP, UNITS, true>(
+        a + r * a_ld, n, t, [&](int u, u32x4 v) EPL_INLINE { __builtin_nontemporal_store(v, q + r * q_ld + u); },
         [&](float s) EPL_INLINE {
           if (t == 0) scale[r] = s;
         });
@@ -136,12 +145,12 @@ __global__ void __launch_bounds__(kInt8Threads)
   for (int64_t g = (int64_t)blockIdx.x * kPer + threadIdx.x / GROUP; g < T; g += (int64_t)gridDim.x * kPer) {
     int mine = lane < k ? pair_row[g * k + lane] : -1;
     if (mine >= cap) mine = -1;
-    quantise_row<GROUP, UNITS>(
+    quantise_row<GROUP, UNITS, false>(
         x + g * 2 * n, n, t,
         [&](int u, u32x4 v) EPL_INLINE {
           for (int j = 0; j < k; ++j) {
             const int row = __builtin_amdgcn_readlane(mine, j);
-            if (row >= 0) recv[row * ld + u] = v;
+            if (row >= 0) store_row_policy<kCachePolicySc1Nt>(v, recv + row * ld, n, u);
           }
         },
         [&](float s) EPL_INLINE {
@@ -150,20 +159,42 @@ __global__ void __launch_bounds__(kInt8Threads)
   }
 }
 
-hipError_t launch_quantize_rows(const void* a, void* q, float* scale, const int32_t* n, int64_t rows, int K, int64_t a_ld,
-                                int64_t q_ld, hipStream_t stream) {
+// f(threads a row, pieces a thread) for rows of n pieces; the last pair takes longer rows in passes.
+template <class F>
+static void with_shape(int n, F&& f) {
+  using std::integral_constant;
+  if (n <= kWave)
+    f(integral_constant<int, kWave>{}, integral_constant<int, 1>{});
+  else if (n <= 2 * kWave)
+    f(integral_constant<int, kWave>{}, integral_constant<int, 2>{});
+  else if (n <= kInt8Threads)
+    f(integral_constant<int, kInt8Threads>{}, integral_constant<int, 1>{});
+  else if (n <= 2 * kInt8Threads)
+    f(integral_constant<int, kInt8Threads>{}, integral_constant<int, 2>{});
+  else
+    f(integral_constant<int, kInt8Threads>{}, integral_constant<int, 8>{});
+}
+
+hipError_t launch_quantize_rows(const void* a, void* q, float* scale, const int32_t* count, int64_t rows, int K,
+                                int64_t a_ld, int64_t q_ld, hipStream_t stream) {
   if (rows == 0) return hipSuccess;
-  hipLaunchKernelGGL((quantize_rows_kernel<kInt8Threads, 8>), dim3(unit_grid(rows, 1, kInt8Threads)), dim3(kInt8Threads), 0,
-                     stream, static_cast<const u32x4*>(a), static_cast<u32x4*>(q), scale, n, rows, K / 16, a_ld, q_ld);
+  with_shape(K / 16, [&](auto group, auto units) {
+    const dim3 grid(unit_grid(rows, kInt8Threads / group, kInt8Threads));
+    hipLaunchKernelGGL((quantize_rows_kernel<group, units>), grid, dim3(kInt8Threads), 0, stream,
+                       static_cast<const u32x4*>(a), static_cast<u32x4*>(q), scale, count, rows, K / 16, a_ld, q_ld);
+  });
   return hipGetLastError();
 }
 
 hipError_t launch_dispatch_int8(const void* x, const float* w, const int32_t* pair_row, void* recv, float* scale, int64_t T,
                                 int k, int H, int pitch, int64_t cap, hipStream_t stream) {
   if (T == 0) return hipSuccess;
-  hipLaunchKernelGGL((dispatch_int8_kernel<kInt8Threads, 8>), dim3(unit_grid(T, 1, kInt8Threads)), dim3(kInt8Threads), 0,
-                     stream, static_cast<const u32x4*>(x), w, pair_row, static_cast<u32x4*>(recv), scale, T, k, H / 16,
-                     (int64_t)pitch / 16, cap);
+  with_shape(H / 16, [&](auto group, auto units) {
+    const dim3 grid(unit_grid(T, kInt8Threads / group, kInt8Threads));
+    hipLaunchKernelGGL((dispatch_int8_kernel<group, units>), grid, dim3(kInt8Threads), 0, stream,
+                       static_cast<const u32x4*>(x), w, pair_row, static_cast<u32x4*>(recv), scale, T, k, H / 16,
+                       (int64_t)pitch / 16, cap);
+  });
   return hipGetLastError();
 }
 

@@ -1109,18 +1109,66 @@ def combine_backward(cfg: Config, dout: torch.Tensor, y: torch.Tensor, topk_w: t
     return dy, dtopk_w
 
 
-def _tokens(t, name: str, cfg: Config) -> None:
-    _dev(t, name, torch.bfloat16)
-    if _rows_of(t, name, cfg.hidden) < cfg.T:
-        raise ValueError("%s has %d rows, needs T = %d" % (name, t.shape[0], cfg.T))
+# Checks of the calls below. A check of one attribute of a tensor takes a tenth of a microsecond and a decoding call's kernel
+# five, so each tensor's are taken once each: where they are as they have to be, that is all; where not, the checks above
+# say what is wrong.
+def _rows_on(index: int, t, name: str, dtype, rows: int, width: int, cfg: Config, pitch: int | None = None) -> int:
+    """_packed for a tensor that has to be on device `index` -> elements from one row to the next. rows: T*k."""
+    if type(t) is torch.Tensor and t.dtype is dtype and t.get_device() == index:
+        shape = t.shape
+        if len(shape) == 2 and shape[0] >= rows and shape[0] > 1 and shape[1] == width > 1:
+            at, dense = t.stride()
+            if dense == 1 and at >= width and (pitch is None or at == pitch):
+                return at
+    at = _packed(t, name, dtype, width, cfg, pitch)
+    _same_device(torch.device("cuda", index), **{name: t})
+    return at
 
 
-def _row_scales(t, name: str, rows: int) -> int:
-    """One fp32 scale a row: 1-D [>= rows]."""
-    p = _dev(t, name, torch.float32)
-    if t.dim() != 1 or t.shape[0] < rows:
-        raise ValueError("%s must be 1-D with at least %d values, got shape %s" % (name, rows, tuple(t.shape)))
-    return p
+def _dense_on(index: int, t, name: str, dtype, rows: int, width: int) -> int:
+    """A contiguous tensor of at least `rows` rows of `width` (0: 1-D, of values) on device `index` -> its address."""
+    if type(t) is torch.Tensor and t.dtype is dtype and t.get_device() == index and t.is_contiguous():
+        shape = t.shape
+        if len(shape) == (2 if width else 1) and shape[0] >= rows and (not width or shape[1] == width):
+            return t.data_ptr()
+    _dev(t, name, dtype)
+    if t.dim() != (2 if width else 1) or t.shape[0] < rows or (width and t.shape[1] != width):
+        raise ValueError("%s must be %s, got shape %s" % (
+            name, "2-D with %d columns and at least %d rows" % (width, rows) if width
+            else "1-D with at least %d values" % rows, tuple(t.shape)))
+    _same_device(torch.device("cuda", index), **{name: t})
+    return t.data_ptr()
+
+
+def _matrices_on(index: int, t, name: str, dtype, cfg: Config) -> int:
+    """_matrices on device `index`."""
+    stride = _matrices(t, name, dtype, cfg)
+    if t.get_device() != index:
+        _same_device(torch.device("cuda", index), **{name: t})
+    return stride
+
+
+def _layout_on(index: int, cfg: Config, L: Layout):
+    """_check_layout on device `index` -> the C struct, by reference."""
+    if L.cfg is not cfg or L.pair_row.get_device() != index or L.workspace.get_device() != index:
+        _check_layout(cfg, L, torch.device("cuda", index))
+    return ctypes.byref(L.buffers())
+
+
+def _index_of(t, name: str) -> int:
+    """The GPU that a call runs on: that of its first tensor."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError("%s must be a GPU tensor" % name)
+    return t.get_device()
+
+
+def _call_on(index: int, name: str, *args) -> None:
+    """_call on device `index`."""
+    if torch._C._cuda_getDevice() != index:
+        return _call(torch.device("cuda", index), name, *args)
+    status = getattr(_lib or lib(), name)(*args, torch._C._cuda_getCurrentRawStream(index))
+    if status:
+        raise EplError(status, name)
 
 
 def dispatch_weighted(cfg: Config, x: torch.Tensor, topk_w: torch.Tensor, L: Layout,
@@ -1128,16 +1176,14 @@ def dispatch_weighted(cfg: Config, x: torch.Tensor, topk_w: torch.Tensor, L: Lay
     """epl_dispatch_weighted: x [T, H] bf16 and topk_w [T, k] fp32 -> recv [T*k, H] bf16 at cfg's pitch, the rows of
     dispatch each times its gate weight (for experts that take weighted inputs; combine then adds their outputs with
     weights of one)."""
-    dev = x.device
-    _tokens(x, "x", cfg)
-    _per_choice(cfg, topk_w, "topk_w", torch.float32)
-    _check_layout(cfg, L, dev)
-    recv = _rows_out(recv, cfg, cfg.hidden, dev, cfg.pitch)
-    _packed(recv, "recv", torch.bfloat16, cfg.hidden, cfg, cfg.pitch)
-    _same_device(dev, topk_w=topk_w, recv=recv)
-    bufs = L.buffers()
-    _call(dev, "epl_dispatch_weighted", ctypes.byref(cfg), x.data_ptr(), topk_w.data_ptr(), ctypes.byref(bufs),
-          recv.data_ptr(), recv.shape[0])
+    dev, T, H = _index_of(x, "x"), cfg.T, cfg.hidden
+    xp = _dense_on(dev, x, "x", torch.bfloat16, T, H)
+    wp = _dense_on(dev, topk_w, "topk_w", torch.float32, T, cfg.topk)
+    bufs = _layout_on(dev, cfg, L)
+    recv = _rows_out(recv, cfg, H, x.device, cfg.pitch) if recv is None else recv
+    rows = T * cfg.topk
+    _rows_on(dev, recv, "recv", torch.bfloat16, rows, H, cfg, cfg.row_pitch or H)
+    _call_on(dev, "epl_dispatch_weighted", ctypes.byref(cfg), xp, wp, bufs, recv.data_ptr(), rows)
     return recv
 
 
@@ -1145,21 +1191,18 @@ def dispatch_backward(cfg: Config, drecv: torch.Tensor, x: torch.Tensor, topk_w:
                       dx: torch.Tensor | None = None, dtopk_w: torch.Tensor | None = None):
     """epl_dispatch_backward: the gradients of dispatch_weighted from drecv [T*k, H] bf16 (at cfg's pitch) and the x and
     topk_w of the forward call -> (dx [T, H] bf16, dtopk_w [T, k] fp32). dx may be x itself."""
-    dev = drecv.device
-    _packed(drecv, "drecv", torch.bfloat16, cfg.hidden, cfg, cfg.pitch)
-    _tokens(x, "x", cfg)
-    _per_choice(cfg, topk_w, "topk_w", torch.float32)
-    _check_layout(cfg, L, dev)
+    dev, T, H, k = _index_of(drecv, "drecv"), cfg.T, cfg.hidden, cfg.topk
+    rows = T * k
+    _rows_on(dev, drecv, "drecv", torch.bfloat16, rows, H, cfg, cfg.row_pitch or H)
+    xp = _dense_on(dev, x, "x", torch.bfloat16, T, H)
+    wp = _dense_on(dev, topk_w, "topk_w", torch.float32, T, k)
+    bufs = _layout_on(dev, cfg, L)
     if dx is None:
-        dx = torch.empty(max(cfg.T, 1), cfg.hidden, dtype=torch.bfloat16, device=dev)
-    _tokens(dx, "dx", cfg)
+        dx = torch.empty(max(T, 1), H, dtype=torch.bfloat16, device=drecv.device)
     if dtopk_w is None:
-        dtopk_w = torch.empty(max(cfg.T, 1), cfg.topk, dtype=torch.float32, device=dev)
-    _per_choice(cfg, dtopk_w, "dtopk_w", torch.float32)
-    _same_device(dev, x=x, topk_w=topk_w, dx=dx, dtopk_w=dtopk_w)
-    bufs = L.buffers()
-    _call(dev, "epl_dispatch_backward", ctypes.byref(cfg), drecv.data_ptr(), drecv.shape[0], x.data_ptr(),
-          topk_w.data_ptr(), ctypes.byref(bufs), dx.data_ptr(), dtopk_w.data_ptr())
+        dtopk_w = torch.empty(max(T, 1), k, dtype=torch.float32, device=drecv.device)
+    _call_on(dev, "epl_dispatch_backward", ctypes.byref(cfg), drecv.data_ptr(), rows, xp, wp, bufs,
+             _dense_on(dev, dx, "dx", torch.bfloat16, T, H), _dense_on(dev, dtopk_w, "dtopk_w", torch.float32, T, k))
     return dx, dtopk_w
 
 
@@ -1168,21 +1211,17 @@ def dispatch_int8(cfg: Config, x: torch.Tensor, L: Layout, topk_w: torch.Tensor 
     """epl_dispatch_int8: x [T, H] bf16 (H a multiple of 16) -> (recv [T*k, H] int8 at cfg's pitch, recv_scale [T*k]
     fp32), the rows of dispatch in int8 with one scale each; with topk_w [T, k] fp32 each scale is times the row's gate
     weight. cfg's payload is not used."""
-    dev = x.device
-    _tokens(x, "x", cfg)
-    if topk_w is not None:
-        _per_choice(cfg, topk_w, "topk_w", torch.float32)
-    _check_layout(cfg, L, dev)
-    recv = _rows_out(recv, cfg, cfg.hidden, dev, cfg.pitch, torch.int8)
-    _packed(recv, "recv", torch.int8, cfg.hidden, cfg, cfg.pitch)
-    rows = recv_rows_cap(cfg)
+    dev, T, H = _index_of(x, "x"), cfg.T, cfg.hidden
+    rows = T * cfg.topk
+    xp = _dense_on(dev, x, "x", torch.bfloat16, T, H)
+    wp = None if topk_w is None else _dense_on(dev, topk_w, "topk_w", torch.float32, T, cfg.topk)
+    bufs = _layout_on(dev, cfg, L)
+    recv = _rows_out(recv, cfg, H, x.device, cfg.pitch, torch.int8) if recv is None else recv
+    _rows_on(dev, recv, "recv", torch.int8, rows, H, cfg, cfg.row_pitch or H)
     if recv_scale is None:
-        recv_scale = torch.empty(max(rows, 1), dtype=torch.float32, device=dev)
-    sp = _row_scales(recv_scale, "recv_scale", rows)
-    _same_device(dev, topk_w=topk_w, recv=recv, recv_scale=recv_scale)
-    bufs = L.buffers()
-    _call(dev, "epl_dispatch_int8", ctypes.byref(cfg), x.data_ptr(), _ptr(topk_w), ctypes.byref(bufs), recv.data_ptr(), sp,
-          rows)
+        recv_scale = torch.empty(max(rows, 1), dtype=torch.float32, device=x.device)
+    _call_on(dev, "epl_dispatch_int8", ctypes.byref(cfg), xp, wp, bufs, recv.data_ptr(),
+             _dense_on(dev, recv_scale, "recv_scale", torch.float32, rows, 0), rows)
     return recv, recv_scale
 
 
@@ -1190,23 +1229,19 @@ def quantize_rows(cfg: Config, a: torch.Tensor, L: Layout, q: torch.Tensor | Non
                   q_scale: torch.Tensor | None = None):
     """epl_quantize_rows on packed rows: a [T*k, K] bf16 (rows any pitch apart, K a multiple of 16) -> (q [T*k, K] int8,
     q_scale [T*k] fp32), as dispatch_int8 makes them; rows behind the last one are left as they are."""
-    dev = a.device
-    rows = recv_rows_cap(cfg)
+    dev, rows = _index_of(a, "a"), cfg.T * cfg.topk
     if a.dim() != 2:
         raise ValueError("a must be 2-D, got shape %s" % (tuple(a.shape),))
     K = a.shape[1]
-    lda = _packed(a, "a", torch.bfloat16, K, cfg)
-    q = _rows_out(q, cfg, K, dev, 0, torch.int8)
-    ldq = _packed(q, "q", torch.int8, K, cfg)
+    lda = _rows_on(dev, a, "a", torch.bfloat16, rows, K, cfg)
+    q = _rows_out(q, cfg, K, a.device, 0, torch.int8) if q is None else q
+    ldq = _rows_on(dev, q, "q", torch.int8, rows, K, cfg)
     if q_scale is None:
-        q_scale = torch.empty(max(rows, 1), dtype=torch.float32, device=dev)
-    sp = _row_scales(q_scale, "q_scale", rows)
-    _check_layout(cfg, L, dev)
-    _same_device(dev, q=q, q_scale=q_scale)
+        q_scale = torch.empty(max(rows, 1), dtype=torch.float32, device=a.device)
+    bufs = _layout_on(dev, cfg, L)
     z = Quantize(_int32(K, "features"), _int32(lda, "a's pitch"), _int32(ldq, "q's pitch"))
-    bufs = L.buffers()
-    _call(dev, "epl_quantize_rows", ctypes.byref(cfg), ctypes.byref(z), a.data_ptr(), rows, ctypes.byref(bufs),
-          q.data_ptr(), sp)
+    _call_on(dev, "epl_quantize_rows", ctypes.byref(cfg), ctypes.byref(z), a.data_ptr(), rows, bufs, q.data_ptr(),
+             _dense_on(dev, q_scale, "q_scale", torch.float32, rows, 0))
     return q, q_scale
 
 
@@ -1228,25 +1263,24 @@ def experts_gated_int8(cfg: Config, recv: torch.Tensor, recv_scale: torch.Tensor
                        gate_scale: torch.Tensor, w_up: torch.Tensor, up_scale: torch.Tensor, activation: str = "silu",
                        h: torch.Tensor | None = None) -> torch.Tensor:
     """epl_experts_gated_int8: experts_gated on int8 rows and weights. recv [T*k, H] int8 and recv_scale [T*k] as
-    dispatch_int8 makes them; w_gate, w_up [E, I, H] int8 and gate_scale, up_scale [E, I] fp32 as quantize_weights makes
-    them -> h [T*k, I] bf16 (quantize_rows makes the down projection's rows of it)."""
-    dev = recv.device
-    _packed(recv, "recv", torch.int8, cfg.hidden, cfg, cfg.pitch)
-    stride = _matrices(w_gate, "w_gate", torch.int8, cfg)
+    dispatch_int8 makes them; w_gate, w_up [E, I, H] int8 (halves of one [E, 2I, H] tensor included) and gate_scale,
+    up_scale [E, I] fp32 as quantize_weights makes them -> h [T*k, I] bf16 (quantize_rows makes the down projection's rows
+    of it)."""
+    dev, rows, H, E = _index_of(recv, "recv"), cfg.T * cfg.topk, cfg.hidden, cfg.num_experts
+    _rows_on(dev, recv, "recv", torch.int8, rows, H, cfg, cfg.row_pitch or H)
+    stride = _matrices_on(dev, w_gate, "w_gate", torch.int8, cfg)
     inner = w_gate.shape[1]
-    if w_gate.shape[2] != cfg.hidden or _matrices(w_up, "w_up", torch.int8, cfg, (inner, cfg.hidden)) != stride:
-        raise ValueError("w_gate and w_up must be [E, I, %d] with one stride between experts" % cfg.hidden)
-    rows = recv_rows_cap(cfg)
-    sp = [_row_scales(recv_scale, "recv_scale", rows), _scales(gate_scale, "gate_scale", cfg.num_experts, inner),
-          _scales(up_scale, "up_scale", cfg.num_experts, inner)]
-    h = _rows_out(h, cfg, inner, dev)
-    _packed(h, "h", torch.bfloat16, inner, cfg, inner)
-    _check_layout(cfg, L, dev)
-    _same_device(dev, recv_scale=recv_scale, gate_scale=gate_scale, up_scale=up_scale, w_gate=w_gate, w_up=w_up, h=h)
+    if w_gate.shape[2] != H or _matrices_on(dev, w_up, "w_up", torch.int8, cfg) != stride or w_up.shape != w_gate.shape:
+        raise ValueError("w_gate and w_up must be [E, I, %d] with one stride between experts" % H)
+    sp = _dense_on(dev, recv_scale, "recv_scale", torch.float32, rows, 0)
+    gp = _dense_on(dev, gate_scale, "gate_scale", torch.float32, E, inner)
+    up = _dense_on(dev, up_scale, "up_scale", torch.float32, E, inner)
+    h = _rows_out(h, cfg, inner, recv.device) if h is None else h
+    _rows_on(dev, h, "h", torch.bfloat16, rows, inner, cfg, inner)
+    bufs = _layout_on(dev, cfg, L)
     g = Gated(_int32(inner, "inner features"), _one_of(ACTIVATION, activation, "activation"), stride)
-    bufs = L.buffers()
-    _call(dev, "epl_experts_gated_int8", ctypes.byref(cfg), ctypes.byref(g), recv.data_ptr(), sp[0], rows,
-          ctypes.byref(bufs), w_gate.data_ptr(), w_up.data_ptr(), sp[1], sp[2], h.data_ptr())
+    _call_on(dev, "epl_experts_gated_int8", ctypes.byref(cfg), ctypes.byref(g), recv.data_ptr(), sp, rows, bufs,
+             w_gate.data_ptr(), w_up.data_ptr(), gp, up, h.data_ptr())
     return h
 
 
@@ -1256,23 +1290,23 @@ def experts_linear_int8(cfg: Config, a: torch.Tensor, a_scale: torch.Tensor, L: 
     """epl_experts_linear_int8: experts_linear on int8 rows and weights. a [T*k, K] int8 (rows any pitch apart) and
     a_scale [T*k]; w [E, N, K] int8 and w_scale [E, N] fp32; bias [E, N], residual [T*k, N] bf16 -> out [T*k, N] bf16.
     A new out of cfg.hidden columns has cfg's pitch, as combine reads it."""
-    dev = a.device
-    stride = _matrices(w, "w", torch.int8, cfg)
-    N, K = w.shape[1], w.shape[2]
-    lda = _packed(a, "a", torch.int8, K, cfg)
-    rows = recv_rows_cap(cfg)
-    sp = [_row_scales(a_scale, "a_scale", rows), _scales(w_scale, "w_scale", cfg.num_experts, N)]
-    bp = _biases(bias, "bias", cfg, N)
-    out = _rows_out(out, cfg, N, dev, cfg.pitch if N == cfg.hidden else 0)
-    ldo = _packed(out, "out", torch.bfloat16, N, cfg)
-    ldr = 0 if residual is None else _packed(residual, "residual", torch.bfloat16, N, cfg)
-    _check_layout(cfg, L, dev)
-    _same_device(dev, a_scale=a_scale, w=w, w_scale=w_scale, bias=bias, residual=residual, out=out)
+    dev, rows = _index_of(a, "a"), cfg.T * cfg.topk
+    stride = _matrices_on(dev, w, "w", torch.int8, cfg)
+    E, N, K = w.shape
+    lda = _rows_on(dev, a, "a", torch.int8, rows, K, cfg)
+    sp = _dense_on(dev, a_scale, "a_scale", torch.float32, rows, 0)
+    wsp = _dense_on(dev, w_scale, "w_scale", torch.float32, E, N)
+    bp = None if bias is None else _biases(bias, "bias", cfg, N)
+    out = _rows_out(out, cfg, N, a.device, cfg.pitch if N == cfg.hidden else 0) if out is None else out
+    ldo = _rows_on(dev, out, "out", torch.bfloat16, rows, N, cfg)
+    ldr = 0 if residual is None else _rows_on(dev, residual, "residual", torch.bfloat16, rows, N, cfg)
+    bufs = _layout_on(dev, cfg, L)
+    if bias is not None:
+        _same_device(a.device, bias=bias)
     lin = Linear(_int32(K, "in_features"), _int32(N, "out_features"), _int32(lda, "a's pitch"), _int32(ldo, "out's pitch"),
                  _int32(ldr, "residual's pitch"), _one_of(ACTIVATION, activation, "activation"), 0, stride)
-    bufs = L.buffers()
-    _call(dev, "epl_experts_linear_int8", ctypes.byref(cfg), ctypes.byref(lin), a.data_ptr(), sp[0], rows,
-          ctypes.byref(bufs), w.data_ptr(), sp[1], bp, _ptr(residual), out.data_ptr())
+    _call_on(dev, "epl_experts_linear_int8", ctypes.byref(cfg), ctypes.byref(lin), a.data_ptr(), sp, rows, bufs,
+             w.data_ptr(), wsp, bp, _ptr(residual), out.data_ptr())
     return out
 
 
