@@ -314,6 +314,7 @@ __device__ __forceinline__ void run_tiles(Job& job, uint32_t lds, int wave, int 
   constexpr int kLoads = A::kLoads + B::kLoads + (FP8 ? 1 : 0);
   constexpr int kLater = S::STAGES - 2;  // steps loading behind the one that a step waits for
   constexpr bool kStream = T == Elem::kInt8;  // loads run on into the next tile
+  constexpr int kEvery = std::max(1, kTail / A::kLoads);
   static_assert(kGroups % kRing == 0, "ring of row fragments");
   static_assert(T == Elem::kBf16 || (!ACOLS && !BCOLS), "8-bit operands are rows");
   static_assert(kHalves == 2 || S::STAGES == 3, "steps() gives an fp8 tile one step more than the written-out three");
@@ -376,12 +377,13 @@ __device__ __forceinline__ void run_tiles(Job& job, uint32_t lds, int wave, int 
         static_for<0, A::kLoads>([&](auto j) EPL_INLINE { a.template load<j>(t, wave); });
         static_for<0, B::kLoads>([&](auto j) EPL_INLINE { b.template load<j>(t + A::kBytes, wave); });
       } else {
-        static_for<0, kLoads>([&](auto j) EPL_INLINE { load(t, t + A::kBytes, j); });
+        static_for<0, kStream && i == S::STAGES - 1 ? B::kLoads : kLoads>(
+            [&](auto j) EPL_INLINE { load(t, t + A::kBytes, j); });
       }
       job.turn(tile, at, a, b);
       ++at;
     });
-    if constexpr (S::RING)
+    if constexpr (S::RING && !kStream)
       static_for<0, A::kLoads>([&](auto j) EPL_INLINE { a.template load<j>(lds + 4 * A::kBytes, wave); });
   };
 
@@ -429,9 +431,11 @@ __device__ __forceinline__ void run_tiles(Job& job, uint32_t lds, int wave, int 
         // What follows this product in the instruction stream.
         if constexpr (g < kTail) {
           if constexpr (n == 0) read_a(std::integral_constant<int, g + kAhead>{});
+          if constexpr (kStream && n == 2 && g % kEvery == kEvery - 1 && g / kEvery < A::kLoads)
+            a.template load<g / kEvery>(S::RING ? ahead(here, 4) : here == lds ? lds + (S::STAGES - 1) * kStage : here - kStage, wave);
           // The second half's column fragments, spread over the first half's groups.
-          constexpr int kSpread = std::min(S::MF, kTail), per = (S::NF + kSpread - 1) / kSpread;
-          if constexpr (kHalves == 2 && g < kSpread && n == S::NF / 2)
+          constexpr int kOver = std::min(S::MF, kTail), per = (S::NF + kOver - 1) / kOver;
+          if constexpr (kHalves == 2 && g < kOver && n == S::NF / 2)
             static_for<g * per, std::min((g + 1) * per, S::NF)>([&](auto i) EPL_INLINE { read_b(One{}, i, One{}); });
         } else if constexpr (left > 0 || kStream) {
           constexpr int slot = (g - kTail) * S::NF + n, kSlots = kAhead * S::NF;
@@ -443,7 +447,7 @@ __device__ __forceinline__ void run_tiles(Job& job, uint32_t lds, int wave, int 
           if constexpr (FP8 && slot == S::NF)
             static_for<0, S::MF>([&](auto f) EPL_INLINE { read_scale(std::integral_constant<int, to>{}, f, cur); });
           // The freed tiles: in a ring they take B of the step after the next and then A of the one behind it.
-          constexpr int issue = left == S::kFinal || kStream ? kLoads : S::RING && left == 2 ? B::kLoads : 0;
+          constexpr int issue = kStream ? B::kLoads : left == S::kFinal ? kLoads : S::RING && left == 2 ? B::kLoads : 0;
           if constexpr (issue > 0) {
             constexpr int per = (issue + kSlots - 1) / kSlots, begin = kSlots - (issue + per - 1) / per;
             if constexpr (slot >= begin)
@@ -464,7 +468,8 @@ __device__ __forceinline__ void run_tiles(Job& job, uint32_t lds, int wave, int 
 
   if (!job.first(tile)) return;
   begin_tile();
-  constexpr int kFirst = S::RING ? 2 * A::kLoads + B::kLoads : kLoads * (S::STAGES - 1);  // loads behind the first step's
+  constexpr int kFirst = kStream ? (S::RING ? kLoads : kLoads * (S::STAGES - 2) + B::kLoads)
+                         : S::RING ? 2 * A::kLoads + B::kLoads : kLoads * (S::STAGES - 1);  // loads behind the first step's
   if constexpr (kStream) job.template wait<kFirst>(false);
   while (true) {
 #pragma unroll
@@ -493,9 +498,9 @@ __device__ __forceinline__ void run_tiles(Job& job, uint32_t lds, int wave, int 
         if constexpr (i == 0) {
           more = job.next(other);
           if (!more) job.none(other);
-          job.begin_a(other, a);
         }
         if constexpr (i == (S::RING ? 1 : 0)) job.begin_b(other, b);
+        if constexpr (i == 1) job.begin_a(other, a);
         if constexpr (i == S::kFinal - 1) job.gather(tile);
       }
       step(std::integral_constant<int, kHalves == 2 ? 0 : (kOdd + i) % 2>{},
@@ -516,7 +521,7 @@ __device__ __forceinline__ void run_tiles(Job& job, uint32_t lds, int wave, int 
       job.finish(other, acc);
       if (!more) return;
     }
-    stored = S::STAGES - 1;
+    stored = kStream && !S::RING ? S::STAGES - 2 : S::STAGES - 1;
   }
 }
 
