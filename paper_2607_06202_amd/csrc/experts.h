@@ -63,14 +63,15 @@ inline bool short_rows(int64_t cap, int E) { return cap / E < 256; }
 inline bool many_rows(int64_t cap, int E) { return cap / E >= 1024; }
 // Int8. few_rows against 64 x 256 tiles: 2048 to 2 x 768 of 128 experts, 8 rows 9.3 / 16.8, 16 rows 16.0 / 18.6; 1408 to 5120
 // of 160 experts, 8 rows 18.4 / 16.8, 16 rows 27.4 / 34.5 (kernel times).
-// int8_few_each: 64 x 256 tiles against 128 x 256, us. 1408 to 5120, 160 experts: 6 rows each 208 / 231, 26 rows 216 / 237,
-// 51 rows 221 / 243, 64 rows 262 / 249; 7168 to 2 x 2048, 256 experts: 16 rows 1224 / 1252, 48 rows 1285 / 1289, 64 rows
-// 1420 / 1298. (32 x 256: 206 at 6 rows, 1224 at 16, and slower from 32 on.)
+// int8_few_each: 64 x 256 tiles against 128 x 256, us. 1408 to 5120, 160 experts: 6 rows each 228 / 245, 26 rows 216 / 235,
+// 51 rows 221 / 238, 64 rows 258 / 246; 7168 to 2 x 2048, 256 experts: 16 rows 1232 / 1241, 48 rows 1285 / 1280, 64 rows
+// 1409 / 1287. (32 x 256, before the loads were spread: as 64 x 256 up to 25 rows, slower beyond.)
 inline bool int8_few_each(int64_t cap, int E) { return cap / E < 56; }
-// int8_many_each: 256 x 256 tiles against 128 x 256, us. 7168 to 2 x 2048, 32 experts: 256 rows each 336 / 348, 512 rows 535 /
-// 558, 1024 rows 953 / 1032, 2048 rows 1737 / 1943; 2048 to 7168 with a residual, 64 experts: 256 rows 372 / 379, 512 rows 642
-// / 683, 1024 rows 1174 / 1284.
-inline bool int8_many_each(int64_t cap, int E) { return cap / E >= 256; }
+// int8_many_each: 256 x 256 tiles against 128 x 256, us. 7168 to 2 x 2048, 32 experts: 96 rows each 227 / 175, 128 rows 219 /
+// 216, 160 rows 221 / 254, 256 rows 315 / 321, 512 rows 487 / 542, 1024 rows 884 / 991, 2048 rows 1608 / 1881; 2048 to 7168
+// with a residual, 64 experts: 128 rows 265 / 260, 160 rows 265 / 309, 256 rows 345 / 363, 512 rows 592 / 656, 1024 rows 1104
+// / 1237.
+inline bool int8_many_each(int64_t cap, int E) { return cap / E >= 144; }
 hipError_t launch_forward_few(const ForwardArgs& p, Elem type, bool gated, hipStream_t stream);
 hipError_t launch_forward(const ForwardArgs& p, Elem type, bool gated, hipStream_t stream);
 hipError_t launch_row_grad(const RowGradArgs& p, hipStream_t stream);

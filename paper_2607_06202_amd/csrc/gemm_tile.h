@@ -280,6 +280,7 @@ __device__ __forceinline__ void arrived(T& v) {
 //   begin(t, a, b)                sets the operands up for step 0 of tile t;
 //   turn(t, step, a, b)           the same for a later step at which a source changes;
 //   load_scales(t, step, lds)     fp8: one load per wave that brings the step's row scales to lds;
+//   begin_a, begin_b, none(t), gather(t), gathered()   int8, see below;
 //   finish(t, acc)                the end of a tile: a known number of buffer stores per wave, whatever is masked;
 //   wait<N>(stored)               wait_tiles<N>, or with the number of stores added.
 //
@@ -301,6 +302,20 @@ __device__ __forceinline__ void arrived(T& v) {
 //
 // The next tile's first steps are loaded before this one's results are worked out and stored. Loads and stores leave
 // one in-order counter, so the first steps of a tile wait for all but the stores behind their loads.
+//
+// Int8 (kStream): a product takes half the time of a bf16 one's for its bytes, so what stands between tiles weighs twice as
+// much, and in 65536 rows of 7168 to 2 x 2048 it took a tenth of the time (a tile of 262000 cycles: 8000 of finding the next
+// tile and waiting, 9200 until its first loads were issued, 8100 of results). There the loads never stop:
+//   * They run on into the next tile. Its place is worked out before the last steps, which load its first ones, and the ring
+//     or the stages go round without a new start. After the last tile they load nothing (none: out of range).
+//   * Step t issues the row operand's loads of step t + STAGES - 1 (ring: t + 2) among its first products, into the place that
+//     step t - 1 left, and B's of step t + STAGES (ring: t + 2) after its barrier, into its own. All of them after the barrier
+//     took 1714 us where this takes 1580. A step still waits for the next one's: behind them may be the loads of
+//     STAGES - 2 steps (ring: of A for one), and the last tile's stores as long as those loads are older than the stores:
+//     one step in a ring, else STAGES - 2.
+//   * What the end of a tile reads besides (gather) is loaded before its last step and waited for there: later it would come
+//     behind the next tile's loads.
+// 65536 rows of 7168 to 2 x 2048 1776 -> 1580 us (2440 TOPS), of 2048 to 7168 with a residual 1378 -> 1067.
 template <class S, bool ACOLS, bool BCOLS, Elem T, bool SPLIT, class Job>
 __device__ __forceinline__ void run_tiles(Job& job, uint32_t lds, int wave, int lane) {
   constexpr bool FP8 = T == Elem::kE4m3;
@@ -314,7 +329,8 @@ __device__ __forceinline__ void run_tiles(Job& job, uint32_t lds, int wave, int 
   constexpr int kLoads = A::kLoads + B::kLoads + (FP8 ? 1 : 0);
   constexpr int kLater = S::STAGES - 2;  // steps loading behind the one that a step waits for
   constexpr bool kStream = T == Elem::kInt8;  // loads run on into the next tile
-  constexpr int kEvery = std::max(1, kTail / A::kLoads);
+  constexpr int kEvery = std::max(1, kTail / A::kLoads);  // groups from one of A's loads to the next
+  static_assert(!kStream || A::kLoads <= kTail, "A's loads are issued before the barrier");
   static_assert(kGroups % kRing == 0, "ring of row fragments");
   static_assert(T == Elem::kBf16 || (!ACOLS && !BCOLS), "8-bit operands are rows");
   static_assert(kHalves == 2 || S::STAGES == 3, "steps() gives an fp8 tile one step more than the written-out three");
@@ -432,7 +448,10 @@ __device__ __forceinline__ void run_tiles(Job& job, uint32_t lds, int wave, int 
         if constexpr (g < kTail) {
           if constexpr (n == 0) read_a(std::integral_constant<int, g + kAhead>{});
           if constexpr (kStream && n == 2 && g % kEvery == kEvery - 1 && g / kEvery < A::kLoads)
-            a.template load<g / kEvery>(S::RING ? ahead(here, 4) : here == lds ? lds + (S::STAGES - 1) * kStage : here - kStage, wave);
+            a.template load<g / kEvery>(S::RING      ? ahead(here, 4)
+                                        : here == lds ? lds + (S::STAGES - 1) * kStage
+                                                      : here - kStage,
+                                        wave);
           // The second half's column fragments, spread over the first half's groups.
           constexpr int kOver = std::min(S::MF, kTail), per = (S::NF + kOver - 1) / kOver;
           if constexpr (kHalves == 2 && g < kOver && n == S::NF / 2)
@@ -494,7 +513,6 @@ __device__ __forceinline__ void run_tiles(Job& job, uint32_t lds, int wave, int 
     bool more = false;
     static_for<0, S::kFinal>([&](auto i) EPL_INLINE {
       if constexpr (kStream) {
-        // A step loads B of the second and, in a ring, A of the third step after it, else both of the third.
         if constexpr (i == 0) {
           more = job.next(other);
           if (!more) job.none(other);

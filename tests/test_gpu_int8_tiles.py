@@ -15,7 +15,8 @@ pytestmark = pytest.mark.gpu
 ONE = 2.0 ** -24
 
 # (experts, rows each about, K, N): 64, 128 and 256 rows a tile by the rows each.
-SHAPES = [(200, 20, 16, 1032), (200, 30, 272, 1544), (130, 45, 1040, 520), (70, 100, 144, 1288), (66, 200, 528, 776),
+SHAPES = [(200, 20, 16, 1032), (200, 30, 272, 1544), (130, 45, 1040, 520), (70, 100, 144, 1288), (66, 135, 528, 776),
+          (66, 200, 528, 776),
           (66, 300, 144, 1032), (20, 900, 656, 1544), (5, 5000, 16, 2056), (3, 6000, 2064, 776)]
 
 
@@ -125,7 +126,7 @@ def test_activations(name, E):
         v = torch.linspace(-LIMIT[name] * 0.9, LIMIT[name] * 0.1, 16).bfloat16() if name in ("silu", "gelu") else v[::500][:16]
     pk = rows_of(v, E)
     T, per = v.numel(), v.numel() // E
-    assert (T <= 16) == (E == 16) and (E != 160 or per < 56) and (E != 64 or 56 <= per < 256) and (E != 8 or per >= 256)
+    assert (T <= 16) == (E == 16) and (E != 160 or per < 56) and (E != 64 or 56 <= per < 144) and (E != 8 or per >= 144)
     x = torch.zeros(T, 128, dtype=torch.int8, device=pk.dev)
     x[:, 0] = 1
     w = torch.zeros(E, 8, 128, dtype=torch.int8, device=pk.dev)
