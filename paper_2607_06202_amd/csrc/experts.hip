@@ -79,6 +79,7 @@ struct ForwardJob {
   };
   const ForwardArgs& p;
   int wave, lane, nt, steps;
+  LanePlace<S, GATED> place_at;
   // The lane, for int8 not to be seen through: what follows from it is worked out for each tile. Once for all tiles would
   // be cheaper but for the registers (all offsets of a tile's loads and stores), of which the steps leave too few.
   __device__ __forceinline__ int my_lane() const {
@@ -90,7 +91,7 @@ struct ForwardJob {
   float row_scale[kRowRegs], col_scale, col_bias;
   Offsets offsets;
   __device__ __forceinline__ ForwardJob(const ForwardArgs& p_, int wave_, int lane_)
-      : p(p_), wave(wave_), lane(lane_) {
+      : p(p_), wave(wave_), lane(lane_), place_at(wave_, lane_) {
     nt = (p.N + kCols - 1) / kCols;
     steps = S::steps(p.K * kEsize, FP8);
   }
@@ -182,7 +183,7 @@ struct ForwardJob {
   __device__ __forceinline__ void finish(const Tile& t, AccOf<T> (&acc)[S::MF][S::NF]) const {
     const int cols = std::min(p.N - t.col0, kCols);
     const int lane = my_lane();
-    const LanePlace<S, GATED> at(wave, lane);
+    const LanePlace<S, GATED> at = INT8 ? LanePlace<S, GATED>(wave, lane) : place_at;
     const TileOut out(p.out, t.row0, p.out_ld, t.col0, t.rows, cols);
     const int64_t pre_ld = (int64_t)p.N * (GATED ? 4 : 2);
     const TileOut pre(p.pre, t.row0, pre_ld, t.col0, t.rows, cols);

@@ -532,12 +532,12 @@ __device__ __forceinline__ void run_tiles(Job& job, uint32_t lds, int wave, int 
       }
       tile = other;
     } else {
-      other = tile;
-      more = job.next(tile);
+      const typename Job::Tile done = tile;
+      const bool some = job.next(tile);
       wait_tiles<0>();  // every wave has read the last stages
-      if (more) begin_tile();
-      job.finish(other, acc);
-      if (!more) return;
+      if (some) begin_tile();
+      job.finish(done, acc);
+      if (!some) return;
     }
     stored = kStream && !S::RING ? S::STAGES - 2 : S::STAGES - 1;
   }
