@@ -409,6 +409,30 @@ def test_layer(shape, before):
     assert float((out.cpu().double() - want).norm() / want.norm()) <= 3 * 2.0 ** -8
 
 
+def test_no_tokens():
+    dev = device()
+    cfg = epl.config(2, 8, 2, 64, 0)
+    L = epl.layout(cfg, torch.zeros(0, 2, dtype=torch.int32, device=dev))
+    w, ws = epl.quantize_weights(torch.ones(8, 64, 64, dtype=torch.bfloat16, device=dev))
+    q, s = epl.dispatch_int8(cfg, torch.zeros(0, 64, dtype=torch.bfloat16, device=dev), L)
+    h = epl.experts_gated_int8(cfg, q, s, L, w, ws, w, ws)
+    y = epl.experts_linear_int8(cfg, *epl.quantize_rows(cfg, h, L), L, w, ws)
+    torch.cuda.synchronize()
+    assert y.shape[1] == 64
+    q, s = epl.quantize_weights(torch.ones(0, 64, 64, dtype=torch.bfloat16, device=dev))
+    assert q.shape == (0, 64, 64) and s.shape == (0, 64)
+
+
+def test_what_a_layout_of_all_padding_leaves():
+    dev = device()
+    pk = Packed(np.full((9, 2), -1, np.int32), 8, 64, dev, row_pitch=128)
+    q, s = int8_out(pk, 64, 128), torch.full((18,), 77.0, device=dev)
+    epl.dispatch_int8(pk.cfg, torch.ones(9, 64, dtype=torch.bfloat16, device=dev), pk.L, recv=q, recv_scale=s)
+    epl.quantize_rows(pk.cfg, pk.out(64), pk.L, q=q, q_scale=s)
+    torch.cuda.synchronize()
+    assert_behind(pk, q, s, "padding")
+
+
 def test_another_stream_and_a_captured_graph():
     layer = Layer(seed=8)
     torch.cuda.synchronize()
