@@ -245,12 +245,12 @@ struct ForwardJob {
         for (int j = 0; j < kTake * 8; ++j) {
           const int k = j / 8, i = j % 8, at_n = (g0 + k) * 2 + i / 4;
           v[k][i] = (float)acc[f][at_n][i % 4];
-          if constexpr (INT8) v[k][i] *= rs;
           if constexpr (FP8 || INT8) v[k][i] *= s1[k][i];
+          if constexpr (INT8) v[k][i] *= rs;  // last: the largest bf16 row's is 2.7e36
           if constexpr (GATED) {
             u[k][i] = (float)acc[f][S::NF / 2 + at_n][i % 4];
-            if constexpr (INT8) u[k][i] *= rs;
             if constexpr (FP8 || INT8) u[k][i] *= s2[k][i];
+            if constexpr (INT8) u[k][i] *= rs;
           } else if (p.bias) {
             v[k][i] += bias[k][i];
           }

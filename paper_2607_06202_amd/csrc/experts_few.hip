@@ -154,9 +154,9 @@ __global__ void __launch_bounds__(kFewWaves* kWave, 2) few_rows_kernel(ForwardAr
       const float rs = INT8 ? p.a_scale[row] : 1.0f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        if constexpr (INT8) v[i] *= rs, u[i] *= rs;
         v[i] *= p.w_scale[cc + i];
         if constexpr (GATED) u[i] *= p.w2_scale[cc + i];
+        if constexpr (INT8) v[i] *= rs, u[i] *= rs;
       }
     }
     if constexpr (!GATED) {

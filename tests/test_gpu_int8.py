@@ -342,6 +342,28 @@ def test_a_row_that_was_not_finite():
             assert torch.equal(torch.isnan(t).all(1), bad) and torch.equal(torch.isnan(t).any(1), bad)
 
 
+def test_the_largest_and_the_smallest_rows():
+    """Rows near fp32's ends, whose sums times the row's scale alone would leave them: the product with the weights' small
+    (large) scales is well inside."""
+    dev = device()
+    g = torch.Generator().manual_seed(4)
+    for rows in (9, 40, 700, 2400):
+        pk = Packed(np.zeros((rows, 1), np.int32), 1, 64, dev)
+        for size, ws in ((2.0 ** 127, 2.0 ** -40), (2.0 ** -120, 2.0 ** 30)):
+            x = (torch.randn(rows, 64, generator=g).clamp(-1.9, 1.9).double() * size).bfloat16()
+            q, s = epl.dispatch_int8(pk.cfg, x.to(dev), pk.L)
+            w = torch.randint(-127, 128, (1, 16, 64), generator=g, dtype=torch.int8)
+            out = epl.experts_linear_int8(pk.cfg, q, s, pk.L, w.to(dev), torch.full((1, 16), ws, device=dev))
+            h = epl.experts_gated_int8(pk.cfg, q, s, pk.L, w.to(dev), torch.full((1, 16), ws, device=dev), w.to(dev),
+                                       torch.full((1, 16), 2.0 ** -100 * ws if size > 1 else ws, device=dev), "none")
+            torch.cuda.synchronize()
+            want = (q.cpu().double() @ w[0].double().T) * ws * s.cpu().double()[:, None]
+            assert_within(out, want, rounded(want, 4 * ONE * want.abs()), "out")
+            if size > 1:
+                both = want * want * 2.0 ** -100
+                assert_within(h, both, rounded(both, 10 * ONE * both.abs()), "h")
+
+
 # ---------------------------------------------------------------- the layer as it is used
 class Layer:
     """Router, int8 dispatch, gated product, int8 rows of it, the way down, combine."""
