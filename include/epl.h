@@ -460,7 +460,8 @@ epl_status epl_dispatch_backward(const epl_config *cfg, const void *drecv, int64
  *   exact quotient (so |q| <= 127; -128 never occurs); s = 0 and q = 0 for a row of zeros; s = NaN and q = 0 for a
  *   row that holds an infinity or a NaN, so that every product with it is NaN.
  * Features and pitches of int8 rows and expert_stride are multiples of 16 (EPL_ERR_UNSUPPORTED for features that are
- * multiples of 8 alone). The calls do not look at cfg's payload.                                            */
+ * multiples of 8 alone), pitches of bf16 rows of 8; matrices, rows and biases are 16-byte aligned, scales and weights 4-byte.
+ * The calls do not look at cfg's payload.                                                                   */
 
 /* Dispatch to int8 rows: every valid pair's row of x, quantised, into its packed receive row.
  *   x, L, recv_rows_cap  as epl_dispatch.   recv  int8 rows of H, cfg's pitch apart.
