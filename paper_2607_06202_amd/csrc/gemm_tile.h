@@ -310,12 +310,12 @@ __device__ __forceinline__ void arrived(T& v) {
 //     or the stages go round without a new start. After the last tile they load nothing (none: out of range).
 //   * Step t issues the row operand's loads of step t + STAGES - 1 (ring: t + 2) among its first products, into the place that
 //     step t - 1 left, and B's of step t + STAGES (ring: t + 2) after its barrier, into its own. All of them after the barrier
-//     took 1714 us where this takes 1580. A step still waits for the next one's: behind them may be the loads of
+//     took 1705 us where this takes 1586. A step still waits for the next one's: behind them may be the loads of
 //     STAGES - 2 steps (ring: of A for one), and the last tile's stores as long as those loads are older than the stores:
 //     one step in a ring, else STAGES - 2.
 //   * What the end of a tile reads besides (gather) is loaded before its last step and waited for there: later it would come
 //     behind the next tile's loads.
-// 65536 rows of 7168 to 2 x 2048 1776 -> 1580 us (2440 TOPS), of 2048 to 7168 with a residual 1378 -> 1067.
+// 65536 rows of 7168 to 2 x 2048 1790 -> 1586 us (2430 TOPS), of 2048 to 7168 with a residual 1395 -> 1073 (one card).
 template <class S, bool ACOLS, bool BCOLS, Elem T, bool SPLIT, class Job>
 __device__ __forceinline__ void run_tiles(Job& job, uint32_t lds, int wave, int lane) {
   constexpr bool FP8 = T == Elem::kE4m3;
