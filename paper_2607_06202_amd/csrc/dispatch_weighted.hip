@@ -34,11 +34,12 @@ __global__ void __launch_bounds__(kPlainThreads) __attribute__((amdgpu_waves_per
   }
 }
 
-// One workgroup a token, of as many threads as its vectors need in the fewest equal passes (448 for 7168 columns). A thread's
-// products are summed in fp32 over its own columns, then over the wave and the waves in a fixed order. dx may be x: a thread
-// reads its columns before it writes them. 8192 tokens of 7168 columns with 8 rows each: 205 us (5.7 TB/s) with 448 threads
-// held at 4 waves per SIMD, 211 not held, 258 at 3; with 64 / 128 / 192 / 256 / 512 threads 230 / 225 / 219 / 215 / 211;
-// stores with the default policy 226 (256 threads).
+// One workgroup a token. A thread's products are summed in fp32 over its own columns, then over the wave and the waves in a
+// fixed order. dx may be x: a thread reads its columns before it writes them. 8192 tokens of 7168 columns with 8 rows each:
+// 205 us (5.7 TB/s) with 448 threads held at 4 waves per SIMD, 211 not held, 258 at 3; stores with the default policy cost 5%.
+// grad_threads: as many as the vectors need in the fewest equal passes of at most 256, or of at most 512 where that gives
+// whole ones of 448 or more. us with at most 512 / 256: 8 rows a token, 512 vectors 118 / 126, 896 215 / 223, 1024 238 / 259,
+// but 448 118 / 112, 513 162 / 134, 640 (320 threads) 167 / 151, 768 189 / 189; one row a token, 896 278 / 234.
 // KMAX: choices held in registers (k <= KMAX).
 constexpr int kDispatchGradThreads = 512;
 constexpr int kDispatchGradWaves = kDispatchGradThreads / kWave;
@@ -121,11 +122,19 @@ hipError_t launch_dispatch_weighted(const void* x, const float* w, const int32_t
   return hipGetLastError();
 }
 
+static int grad_threads(int nv, int k) {
+  const auto equal = [&](int most) {
+    const int passes = (nv + most - 1) / most;
+    return ((nv + passes - 1) / passes + kWave - 1) / kWave * kWave;
+  };
+  const int wide = equal(kDispatchGradThreads);
+  return k > kFewChoices && nv >= kDispatchGradThreads && wide >= 448 ? wide : equal(256);
+}
+
 hipError_t launch_dispatch_grad(const void* d, const void* x, const float* w, const int32_t* pair_row, void* dx, float* dw,
                                 int64_t T, int k, int H, int pitch, int64_t cap, hipStream_t stream) {
   if (T == 0) return hipSuccess;
-  const int nv = H / 8, passes = (nv + kDispatchGradThreads - 1) / kDispatchGradThreads;
-  const int threads = ((nv + passes - 1) / passes + kWave - 1) / kWave * kWave;
+  const int nv = H / 8, threads = grad_threads(nv, k);
   const dim3 grid((unsigned)std::min<int64_t>(T, 1 << 20));
   const auto launch = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, stream, static_cast<const u32x4*>(d),

@@ -12,7 +12,8 @@ from tests.products_util import BF16_HALF_STEP, Packed, assert_within, sum_error
 pytestmark = pytest.mark.gpu
 
 SHAPES = [(1, 8, 1, 1, 8, 0), (2, 8, 2, 9, 264, 320), (4, 16, 8, 33, 1024, 0), (4, 64, 8, 16, 7168, 7936),
-          (1, 40, 12, 21, 2056, 0), (2, 64, 32, 5, 520, 576), (8, 32, 4, 300, 72, 0), (1, 8, 2, 3, 70000, 0)]
+          (1, 40, 12, 21, 2056, 0), (2, 64, 32, 5, 520, 576), (8, 32, 4, 300, 72, 0), (1, 8, 2, 3, 70000, 0),
+          (1, 16, 4, 9, 5120, 0), (1, 16, 3, 5, 8192, 8256), (1, 16, 6, 7, 4104, 0), (1, 16, 1, 40, 7168, 0)]
 
 
 def inputs(R, E, k, Tr, H, pitch):

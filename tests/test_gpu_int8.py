@@ -48,7 +48,8 @@ def assert_behind(pk, q, s, what):
 
 
 # ---------------------------------------------------------------- rows
-@pytest.mark.parametrize("K", [16, 32, 1008, 1024, 1040, 2048, 4080, 4096, 4112, 7168, 8192, 8208, 32768, 32784, 70000])
+@pytest.mark.parametrize("K", [16, 32, 240, 256, 272, 512, 528, 1008, 1024, 1040, 2048, 2064, 4080, 4096, 4112, 7168, 8192, 8208,
+                               16384, 16400, 32768, 32784, 70000])
 def test_quantize_weights_at_the_ends_of_pieces_and_passes(K):
     g = torch.Generator().manual_seed(K)
     w = (torch.randn(3, 5, K, generator=g) * torch.exp(torch.randn(3, 5, 1, generator=g) * 3)).bfloat16()
@@ -94,7 +95,7 @@ def test_subnormals_and_the_largest():
     assert_rows(q[0], s[0], x, "subnormals")
 
 
-@pytest.mark.parametrize("K", [16, 2048, 9216])
+@pytest.mark.parametrize("K", [16, 384, 768, 2048, 9216])
 def test_infinities_and_nan(K):
     x = torch.randn(5, K, generator=torch.Generator().manual_seed(1)).bfloat16()
     x[0, 3], x[1, -1], x[2, 0], x[3, 5] = INF, -INF, float("nan"), 0.0
@@ -106,7 +107,7 @@ def test_infinities_and_nan(K):
 
 
 @pytest.mark.parametrize("T,k,K,pitch,qpitch", [(1, 1, 16, 0, 0), (9, 2, 784, 800, 832), (3, 4, 4112, 0, 0),
-                                                (700, 2, 64, 72, 0), (40, 8, 16400, 0, 16448), (2100, 1, 2048, 0, 0)])
+                                                (700, 2, 64, 72, 0), (333, 3, 400, 0, 448), (40, 8, 16400, 0, 16448), (2100, 1, 2048, 0, 0)])
 def test_quantize_packed_rows(T, k, K, pitch, qpitch):
     g = torch.Generator().manual_seed(K)
     rng = np.random.default_rng(T)
