@@ -485,8 +485,9 @@ epl_status epl_quantize_rows(const epl_config *cfg, const epl_quantize *quantize
 
 /* The experts' products of int8 rows and weights, forward: as epl_experts_gated and epl_experts_linear for E4M3, but
  * with one scale for each row (recv_scale, a_scale [rows]) and one for each output feature (gate_scale, up_scale
- * [E*I], w_scale [E*N]). A product's sum is exact in 32 bits, times the feature's scale, times the row's; what follows is
- * fp32, rounded once to bf16. Nothing is kept for a backward pass. lin's payload is not used.
+ * [E*I], w_scale [E*N]). A product's sum is exact in 32 bits, times the feature's scale, times the row's (with a bias: and
+ * the bias, in one rounding); what follows is fp32, rounded once to bf16. A row's result does not depend on the other rows,
+ * bit for bit. Nothing is kept for a backward pass. lin's payload is not used.
  * EPL_ERR_UNSUPPORTED for more than EPL_MAX_INT8_FEATURES features in (then 128 * 128 * K could pass 2^31 - 1).   */
 #define EPL_MAX_INT8_FEATURES 131056
 epl_status epl_experts_gated_int8(const epl_config *cfg, const epl_gated *gated, const void *recv,

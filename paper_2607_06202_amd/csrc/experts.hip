@@ -172,7 +172,8 @@ struct ForwardJob {
     const int c = std::min((wave % S::WN) * kWide + lane % kWide, cols - 1);
     const int64_t cc = (int64_t)t.e * p.N + t.col0 + c;
     col_scale = (GATED && lane >= 32 ? p.w2_scale : p.w_scale)[cc];
-    if constexpr (!GATED) col_bias = p.bias ? bf16lo_to_f32(((const uint16_t*)p.bias)[cc]) : 0.0f;
+    // (Without a bias -0: nothing to add, the sign of a zero included.)
+    if constexpr (!GATED) col_bias = p.bias ? bf16lo_to_f32(((const uint16_t*)p.bias)[cc]) : -0.0f;
   }
   __device__ __forceinline__ void gathered() {
 #pragma unroll

@@ -156,10 +156,19 @@ __global__ void __launch_bounds__(kFewWaves* kWave, 2) few_rows_kernel(ForwardAr
       for (int i = 0; i < 8; ++i) {
         v[i] *= p.w_scale[cc + i];
         if constexpr (GATED) u[i] *= p.w2_scale[cc + i];
-        if constexpr (INT8) v[i] *= rs, u[i] *= rs;
+        if constexpr (GATED && INT8) v[i] *= rs, u[i] *= rs;
+      }
+      // The row's scale and the bias in one rounding, as on the tiles: a row's bits do not depend on how many there are.
+      if constexpr (!GATED && INT8) {
+        float d[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[i] = -0.0f;  // nothing to add, the sign of a zero included
+        if (p.bias) unpack8(*(const u32x4*)(p.bias + cc * 2), d);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = fmaf(v[i], rs, d[i]);
       }
     }
-    if constexpr (!GATED) {
+    if constexpr (!GATED && !INT8) {
       if (p.bias) {
         float d[8];
         unpack8(*(const u32x4*)(p.bias + cc * 2), d);
