@@ -305,7 +305,7 @@ __device__ __forceinline__ void arrived(T& v) {
 //
 // Int8 (kStream): a product takes half the time of a bf16 one's for its bytes, so what stands between tiles weighs twice as
 // much, and in 65536 rows of 7168 to 2 x 2048 it took a tenth of the time (a tile of 262000 cycles: 8000 of finding the next
-// tile and waiting, 9200 until its first loads were issued, 8100 of results). There the loads never stop:
+// tile and waiting, 9200 until its first loads were issued, 8100 of results). There the loads run on:
 //   * They run on into the next tile. Its place is worked out before the last steps, which load its first ones, and the ring
 //     or the stages go round without a new start. After the last tile they load nothing (none: out of range).
 //   * Step t issues the row operand's loads of step t + STAGES - 1 (ring: t + 2) among its first products, into the place that
@@ -313,8 +313,12 @@ __device__ __forceinline__ void arrived(T& v) {
 //     took 1705 us where this takes 1586. A step still waits for the next one's: behind them may be the loads of
 //     STAGES - 2 steps (ring: of A for one), and the last tile's stores as long as those loads are older than the stores:
 //     one step in a ring, else STAGES - 2.
-//   * What the end of a tile reads besides (gather) is loaded before its last step and waited for there: later it would come
-//     behind the next tile's loads.
+//   * What the end of a tile reads besides (gather) is loaded before its last step and waited for at that step's barrier:
+//     later it would come behind the next tile's loads.
+// They pause where the compiler waits for something of its own: it does not see the loads to LDS, so it lets everything
+// land. That is once a tile at the last step's barrier (gather); where the next tile is in another group of 64 experts
+// (find); and in the gated 256 x 256 kernel, whose steps leave seven registers too few, twice more around the first
+// written-out step, where those come back.
 // 65536 rows of 7168 to 2 x 2048 1790 -> 1586 us (2430 TOPS), of 2048 to 7168 with a residual 1395 -> 1073 (one card).
 template <class S, bool ACOLS, bool BCOLS, Elem T, bool SPLIT, class Job>
 __device__ __forceinline__ void run_tiles(Job& job, uint32_t lds, int wave, int lane) {
