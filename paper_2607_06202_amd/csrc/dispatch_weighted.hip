@@ -91,7 +91,7 @@ __global__ void __launch_bounds__(kDispatchGradThreads) __attribute__((amdgpu_wa
     __syncthreads();  // the previous token's sums have been read
 #pragma unroll
     for (int j = 0; j < KMAX; ++j) {
-      if (j >= k) break;
+      if (j >= k) continue;
       float v = acc[j];
 #pragma unroll
       for (int off = kWave / 2; off > 0; off >>= 1) v += __shfl_xor(v, off, kWave);
