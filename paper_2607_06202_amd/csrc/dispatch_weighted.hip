@@ -37,9 +37,13 @@ __global__ void __launch_bounds__(kPlainThreads) __attribute__((amdgpu_waves_per
 // One workgroup a token. A thread's products are summed in fp32 over its own columns, then over the wave and the waves in a
 // fixed order. dx may be x: a thread reads its columns before it writes them. 8192 tokens of 7168 columns with 8 rows each:
 // 205 us (5.7 TB/s) with 448 threads held at 4 waves per SIMD, 211 not held, 258 at 3; stores with the default policy cost 5%.
-// grad_threads: as many as the vectors need in the fewest equal passes of at most 256, or of at most 512 where that gives
-// whole ones of 448 or more. us with at most 512 / 256: 8 rows a token, 512 vectors 118 / 126, 896 215 / 223, 1024 238 / 259,
-// but 448 118 / 112, 513 162 / 134, 640 (320 threads) 167 / 151, 768 189 / 189; one row a token, 896 278 / 234.
+// grad_threads: as many as the vectors need in the fewest equal passes of at most 256, or of at most 512 where those make
+// workgroups of seven or eight waves: two of them take 14 or all of a compute unit's 16 places, two of five or six 10 or 12.
+// us with at most 512 / 256, of seven or eight waves: 8 choices, 512 vectors 205 / 218, 832 215 / 224, 896 216 / 224, 1024 217 /
+// 226, 1280 218 / 228, 1536 221 / 229, 2048 223 / 228; 4 choices, 512 251 / 248, 832 246 / 259, 1024 239 / 260, 1536 246 / 265,
+// 2048 251 / 265. Of five or six: 8 choices, 640 231 / 220, 768 221 / 222, 1152 219 / 226. Rows of one pass: 448 230 / 217. Fewer
+// choices have too little to load: 3, 512 295 / 269, 896 288 / 282, 1024 272 / 279; the instance for more is not the faster for it: 16, 512 206 /
+// 205, 896 215 / 213, 1024 203 / 211; 32, 512 231 / 219, 896 242 / 214, 1024 223 / 214.
 // KMAX: choices held in registers (k <= KMAX).
 constexpr int kDispatchGradThreads = 512;
 constexpr int kDispatchGradWaves = kDispatchGradThreads / kWave;
@@ -128,7 +132,7 @@ static int grad_threads(int nv, int k) {
     return ((nv + passes - 1) / passes + kWave - 1) / kWave * kWave;
   };
   const int wide = equal(kDispatchGradThreads);
-  return k > kFewChoices && nv >= kDispatchGradThreads && wide >= 448 ? wide : equal(256);
+  return k >= 4 && k <= 8 && nv >= kDispatchGradThreads && wide / kWave >= 7 ? wide : equal(256);
 }
 
 hipError_t launch_dispatch_grad(const void* d, const void* x, const float* w, const int32_t* pair_row, void* dx, float* dw,
