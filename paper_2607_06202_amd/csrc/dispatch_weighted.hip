@@ -7,7 +7,7 @@
 namespace epl {
 
 // As the plain bf16 dispatch: one (token, 1 KiB column chunk) a wave, two waves a workgroup, held at 4 waves per SIMD (6 with
-// one or two choices). 8192 tokens of 7168 columns to 8 rows each: 191 us, as without the weights; not held 198, held at 2 / 3
+// one or two choices). 8192 tokens of 7168 columns to 8 rows each: 191 us (without the weights 190); not held 198, held at 2 / 3
 // / 5 / 6 228 / 193 / 192 / 195; with default stores 214, with streaming ones 194.
 template <bool FEW>
 __global__ void __launch_bounds__(kPlainThreads) __attribute__((amdgpu_waves_per_eu(FEW ? 6 : 4, FEW ? 6 : 4)))
@@ -41,9 +41,9 @@ __global__ void __launch_bounds__(kPlainThreads) __attribute__((amdgpu_waves_per
 // workgroups of seven or eight waves: two of them take 14 or all of a compute unit's 16 places, two of five or six 10 or 12.
 // us with at most 512 / 256, of seven or eight waves: 8 choices, 512 vectors 205 / 218, 832 215 / 224, 896 216 / 224, 1024 217 /
 // 226, 1280 218 / 228, 1536 221 / 229, 2048 223 / 228; 4 choices, 512 251 / 248, 832 246 / 259, 1024 239 / 260, 1536 246 / 265,
-// 2048 251 / 265. Of five or six: 8 choices, 640 231 / 220, 768 221 / 222, 1152 219 / 226. Rows of one pass: 448 230 / 217. Fewer
-// choices have too little to load: 3, 512 295 / 269, 896 288 / 282, 1024 272 / 279; the instance for more is not the faster for it: 16, 512 206 /
-// 205, 896 215 / 213, 1024 203 / 211; 32, 512 231 / 219, 896 242 / 214, 1024 223 / 214.
+// 2048 251 / 265. Of five or six: 8 choices, 640 231 / 220, 768 221 / 222, 1152 219 / 226. Rows of one pass: 448 230 / 217.
+// Fewer choices have too little to load: 3, 512 295 / 269, 896 288 / 282, 1024 272 / 279. The instance for more is seldom faster
+// for it: 16, 512 206 / 205, 896 215 / 213, 1024 203 / 211; 32, 512 231 / 219, 896 242 / 214, 1024 223 / 214.
 // KMAX: choices held in registers (k <= KMAX).
 constexpr int kDispatchGradThreads = 512;
 constexpr int kDispatchGradWaves = kDispatchGradThreads / kWave;

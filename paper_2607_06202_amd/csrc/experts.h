@@ -63,6 +63,8 @@ inline bool short_rows(int64_t cap, int E) { return cap / E < 256; }
 inline bool many_rows(int64_t cap, int E) { return cap / E >= 1024; }
 // Int8. few_rows against 64 x 256 tiles: 2048 to 2 x 768 of 128 experts, 8 rows 9.3 / 16.8, 16 rows 16.0 / 18.6; 1408 to 5120
 // of 160 experts, 8 rows 18.4 / 16.8, 16 rows 27.4 / 34.5 (kernel times).
+// int8_few_each and int8_many_each were measured with two tiles a compute unit or more; with fewer, a shape that makes more of
+// them may be faster, which the rules do not look at.
 // int8_few_each: 64 x 256 tiles against 128 x 256, us. 1408 to 5120, 160 experts: 6 rows each 228 / 245, 26 rows 216 / 235,
 // 51 rows 221 / 238, 64 rows 258 / 246; 7168 to 2 x 2048, 256 experts: 16 rows 1232 / 1241, 48 rows 1285 / 1280, 64 rows
 // 1409 / 1287. (32 x 256, before the loads were spread: as 64 x 256 up to 25 rows, slower beyond.)

@@ -4,8 +4,9 @@
 // workgroup takes 16 * NF weight rows of one expert, its four waves each take every fourth 128-byte step of the
 // reduction, and the four partial sums are joined through LDS in a fixed order. A wave's fragments come straight from
 // memory, few_depth steps ahead: 2 * (NF + 1) KiB a step in flight. Int8 rows are half as long, so a wave has few steps, and
-// those past the last one cost more than the depth gains: 2048 to 2 x 768, 8 rows, 1 / 2 / 3 / 4 steps ahead 9.4 / 9.3 / 10.2 /
-// 10.4 us; 7168 to 2 x 2048 50.7 / 48.6 / 51.2 / 53.5; 768 to 2048 - / 6.6 / - / 8.2.
+// those past the last one (whose loads are issued too, out of range) cost more than the depth gains: 2048 to 2 x 768, 8 rows,
+// 1 / 2 / 3 / 4 steps ahead 9.4 / 9.3 / 10.2 / 10.4 us; 7168 to 2 x 2048 50.7 / 48.6 / 51.2 / 53.5; 768 to 2048 - / 6.6 / - /
+// 8.2.
 //
 // For at most 16 packed rows in all (few_rows): an expert's rows are one fragment.
 //

@@ -305,7 +305,7 @@ __device__ __forceinline__ void arrived(T& v) {
 //
 // Int8 (kStream): a product takes half the time of a bf16 one's for its bytes, so what stands between tiles weighs twice as
 // much, and in 65536 rows of 7168 to 2 x 2048 it took a tenth of the time (a tile of 262000 cycles: 8000 of finding the next
-// tile and waiting, 9200 until its first loads were issued, 8100 of results). There the loads run on:
+// tile and waiting, 9200 until its first loads were issued, 8100 of results). There the loads go on between tiles:
 //   * They run on into the next tile. Its place is worked out before the last steps, which load its first ones, and the ring
 //     or the stages go round without a new start. After the last tile they load nothing (none: out of range).
 //   * Step t issues the row operand's loads of step t + STAGES - 1 (ring: t + 2) among its first products, into the place that
